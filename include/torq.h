@@ -33,7 +33,7 @@ enum {
     TORQ_OK          =  0,
     TORQ_EINVAL      = -1,  /* null pointer, negative size, d % 32 != 0, G does not divide d/32,
                                G not a multiple of 16 or above TORQ_MAX_G, N or d beyond the limits below */
-    TORQ_EALIGN      = -2,  /* a device pointer is not 16-byte aligned */
+    TORQ_EALIGN      = -2,  /* a device pointer is not 16-byte aligned (arrays of 32- or 64-bit integers: not aligned to their elements) */
     TORQ_EWORKSPACE  = -3,  /* workspace smaller than torq_linear_workspace_bytes() */
     TORQ_EHIP        = -4,  /* the HIP runtime reported an error (allocation, copy or launch) */
     TORQ_ENODEVICE   = -5,  /* no gfx950 device is current */
@@ -256,6 +256,83 @@ int torq_linear_single_launch_gave_up(const torq_rotation_t *r, int *gave_up);
 int torq_linear_single_launch_probe(const torq_rotation_t *r, const void *x_bf16, const uint8_t *W_q,
                                     const uint8_t *W_s, void *out_bf16, int64_t M, int64_t N, void *workspace,
                                     size_t workspace_bytes, int spin_limit, int withhold_ready, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* The attention side of a decoder block: the residual norm ahead of the linear layers above, and one
+ * new token's attention over a paged key-value cache.  Values of all of them are bf16 or MXFP8:
+ *   TORQ_FMT_BF16   bf16 elements, no scales
+ *   TORQ_FMT_MXFP8  OCP FP8 E4M3 elements, one E8M0 byte for each block of 32 along the last dimension:
+ *                   2^(byte-127) is the least power of two (from 2^-127 on) that leaves no element of the
+ *                   block above 448, E4M3's largest value; element = E4M3 nearest to x / 2^(byte-127),
+ *                   ties to the even code.  (Rounding log2 amax down instead, as MXFP4 above, would put
+ *                   maxima of up to 511 on 448.)  A block with an infinity or NaN: byte 0xFF, every element NaN (0x7F).
+ * The 4-bit formats above are not among them, nor these among those of torq_rotate_quantize_fmt. */
+#define TORQ_FMT_BF16  8
+#define TORQ_FMT_MXFP8 9
+
+/* A paged cache of keys and values: `pages` pages of page_size tokens for each of `heads` heads, in memory that the
+ * caller owns.  Element (page, head, token in the page, i) of k and of v lies at page * page_stride + head *
+ * head_stride + token * token_stride + i, so a page's heads may lie ahead of its tokens or behind, and k and v in one
+ * array or two; the scale byte of a block of 32 lies at a 32nd of the block's place, counted from k_scales or v_scales.
+ *   format     TORQ_FMT_BF16 or TORQ_FMT_MXFP8
+ *   head_dim   at most TORQ_MAX_HEAD_DIM, a multiple of 8 (bf16) or 32 (MXFP8)
+ *   page_size  a multiple of 16, at most 65536
+ *   strides    in elements, not negative, multiples of 8 (bf16) or 32 (MXFP8); token_stride * page_size < 2^29
+ * k and v 16-byte aligned.  The struct is read during a call only. */
+#define TORQ_MAX_HEAD_DIM 256
+typedef struct torq_kv_cache {
+    void *k, *v;
+    uint8_t *k_scales, *v_scales;   /* MXFP8 only */
+    int64_t pages, page_stride, head_stride, token_stride;
+    int format, heads, head_dim, page_size;
+} torq_kv_cache_t;
+
+/* Pages and slots of a step, from the requests' lengths.  Request b has held[b] tokens in the cache and lengths[b] after
+ * the step, the new ones at positions held[b] ... lengths[b] - 1 (none where lengths[b] <= held[b]; held[b] < 0 counts as 0).  The pages
+ * that this takes beyond the ceil(held[b] / page_size) that the request has are handed out in the order of the requests
+ * from free_pages, of which *cursor have been handed out before:
+ *   block_tables  [B] rows of `width` entries, table_stride apart: entries of pages handed out are written, no other
+ *                 is; entries of pages held are read.  A request never has more than `width` pages.
+ *   slots         [tokens]: page * page_size + place in it, for each new token, request after request in order; -1 for a
+ *                 token without a page and past the last token
+ *   cursor_out    *cursor + pages wanted; may be `cursor`.  Above free_count: the list ran out, and the entries that it
+ *                 has no page for are -1.
+ * All arrays on the device.  Nothing is copied to the host, so the call can be captured; `tokens` is the host's bound. */
+int torq_block_tables(const int32_t *held, const int32_t *lengths, int64_t B, const int32_t *free_pages, int64_t free_count,
+                      const int32_t *cursor, int32_t *cursor_out, int32_t *block_tables, int64_t table_stride, int width,
+                      int page_size, int64_t *slots, int64_t tokens, void *stream);
+
+/* key and value [tokens][heads][head_dim] bf16 (strides in elements, multiples of 8, not negative) into the cache: token t at
+ * slot slots[t] = page * page_size + place in the page.  A slot outside the cache (-1 among them) is passed over.
+ * Two tokens with one slot: either's values, block by block. */
+int torq_cache_append(const torq_kv_cache_t *cache, const void *key_bf16, int64_t key_token_stride, int64_t key_head_stride,
+                      const void *value_bf16, int64_t value_token_stride, int64_t value_head_stride,
+                      const int64_t *slots, int64_t tokens, void *stream);
+
+/* Attention of one new token of each request over its cached tokens (the new one's among them):
+ *   out[b][h] = sum_t p_t v_t,  p = softmax over t < lengths[b] of scale * q[b][h] . k_t,
+ * k_t, v_t: position t of request b under key head h / (heads / cache->heads).  A request without tokens: zeros.
+ *   q_bf16        [B][heads][head_dim], strides in elements, multiples of 8, not negative; heads a multiple of cache->heads
+ *   block_tables  as torq_block_tables leaves them, width * page_size at most 2^30.  A position past `width` pages counts as past the length; tokens of
+ *                 a page outside [0, pages) are left out.  What lies in a page behind the length is not used, NaN or not.
+ *   out_bf16      [B][heads][head_dim], contiguous
+ *   workspace     16-byte aligned, torq_paged_attention_workspace_bytes() of the same sizes; contents do not matter
+ * Products of bf16 values with fp32 sums (MXFP8 values are bf16 values), softmax statistics in fp32, the weights p as two bf16 parts in
+ * the product with v: the output's is the only rounding to bf16.  The same inputs give the same bits.  scale has to be finite.  All pointers 16-byte aligned, tables and lengths 4. */
+size_t torq_paged_attention_workspace_bytes(const torq_kv_cache_t *cache, int heads, int64_t B, int width);
+int torq_paged_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads,
+                         const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths, int64_t B,
+                         float scale, void *out_bf16, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Residual addition and root-mean-square norm of rows of d values, d a multiple of 32, at most TORQ_MAX_NORM_D:
+ *   s = x + residual,  residual_out = bf16(s),  out = s / sqrt(mean(s^2) + eps) * weight
+ * x, residual, weight, residual_out bf16; arithmetic in fp32 on s as it is before its rounding.  residual and
+ * residual_out NULL: s = x.  residual_out may be residual or x.
+ *   out     TORQ_FMT_BF16: [M][d] bf16, what torq_linear reads; may be x.  TORQ_FMT_MXFP8: [M][d] bytes
+ *   scales  TORQ_FMT_MXFP8: [M][d/32] bytes; else ignored */
+#define TORQ_MAX_NORM_D 32768
+int torq_add_rms_norm(const void *x_bf16, const void *residual_bf16, const void *weight_bf16, int64_t M, int d, float eps,
+                      int format, void *residual_out_bf16, void *out, uint8_t *scales, void *stream);
 
 /* ------------------------------------------------------------------------ */
 /* Calibration of the inter-block rotation (Section 5.1, Algorithm 1).  Not part of the online

@@ -24,6 +24,7 @@ EXPORTS = [
     "torq_linear_workspace_bytes_n", "torq_block_gram_workspace_bytes", "torq_block_gram", "torq_block_gram_positions",
     "torq_equalize_inter", "torq_code_histogram_workspace_bytes", "torq_code_histogram", "torq_intra_pair_scores",
     "torq_intra_best_angle", "torq_calibrate_intra", "torq_diag_mfma_burn", "torq_linear_static",
+    "torq_block_tables", "torq_cache_append", "torq_paged_attention", "torq_paged_attention_workspace_bytes", "torq_add_rms_norm",
     "torq_diag_copy", "torq_diag_gemm_ablation", "torq_diag_gemm_persistent", "torq_diag_gemm_plan", "torq_diag_gemm_ring", "torq_diag_gemm_form", "torq_diag_rotate_ablation", "torq_linear_single_launch_reset", "torq_linear_single_launch_gave_up", "torq_linear_single_launch_probe",
 ]
 
@@ -34,6 +35,13 @@ TORQ_BUTTERFLY_MAX_TAN = 256.0
 TORQ_STATIC_SCRATCH_BYTES = 4 << 20
 
 _lib = None
+
+
+class _KVCacheStruct(C.Structure):
+    """torq_kv_cache_t of include/torq.h."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("pages", C.c_int64), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("format", C.c_int), ("heads", C.c_int), ("head_dim", C.c_int), ("page_size", C.c_int)]
 
 
 class TorqError(RuntimeError):
@@ -121,6 +129,16 @@ def lib():
                                             C.POINTER(i64)]
         L.torq_calibrate_intra.restype = i32
         L.torq_calibrate_intra.argtypes = [vp, i64, i32, i32, i32, C.c_double, C.c_double, vp, vp, C.POINTER(i32)]
+        L.torq_block_tables.restype = i32
+        L.torq_block_tables.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, i64, i32, i32, vp, i64, vp]
+        L.torq_cache_append.restype = i32
+        L.torq_cache_append.argtypes = [vp, vp, i64, i64, vp, i64, i64, vp, i64, vp]
+        L.torq_paged_attention_workspace_bytes.restype = sz
+        L.torq_paged_attention_workspace_bytes.argtypes = [vp, i32, i64, i32]
+        L.torq_paged_attention.restype = i32
+        L.torq_paged_attention.argtypes = [vp, vp, i64, i64, i32, vp, i64, i32, vp, i64, C.c_float, vp, vp, sz, vp]
+        L.torq_add_rms_norm.restype = i32
+        L.torq_add_rms_norm.argtypes = [vp, vp, vp, i64, i32, C.c_float, i32, vp, vp, vp, vp]
         L.torq_diag_mfma_burn.restype = i32
         L.torq_diag_mfma_burn.argtypes = [i32, vp, sz, i32, vp, vp]
         L.torq_diag_gemm_ablation.restype = i32
@@ -183,6 +201,7 @@ def _scratch(like: torch.Tensor, nbytes: int, stream) -> torch.Tensor:
 class _Interpreted:
     """In the place of the C++ module where there is none for this interpreter and torch: it takes no call."""
     linear = rotate_quantize = gram = histogram = staticmethod(lambda *args: None)
+    block_tables = cache_append = paged_attention = add_rms_norm = staticmethod(lambda *args: None)
 
 
 _host = None
@@ -207,7 +226,8 @@ def _native():
             return _host
         names = ["torq_linear", "torq_linear_workspace_bytes_n", "torq_rotate_quantize", "torq_rotate_quantize_fmt",
                  "torq_block_gram", "torq_block_gram_positions", "torq_block_gram_workspace_bytes", "torq_code_histogram",
-                 "torq_code_histogram_workspace_bytes"]
+                 "torq_code_histogram_workspace_bytes", "torq_block_tables", "torq_cache_append", "torq_paged_attention",
+                 "torq_paged_attention_workspace_bytes", "torq_add_rms_norm"]
         module.bind({n: C.cast(getattr(L, n), C.c_void_p).value for n in names}, _stream, _check)
         _host = module
     return _host
@@ -684,3 +704,153 @@ def torq_calibrate_intra(X, max_iter: int, k_top: int, P: int, lam: float, eps: 
                                       float(lam), float(eps), R.ctypes.data_as(C.c_void_p),
                                       losses.ctypes.data_as(C.c_void_p), C.byref(k)), "torq_calibrate_intra")
     return R, losses[: k.value].copy()
+
+
+# ---- the attention side of a decoder block -----------------------------------------------------
+
+TORQ_FMT_BF16, TORQ_FMT_MXFP8 = 8, 9
+TORQ_MAX_HEAD_DIM, TORQ_MAX_NORM_D = 256, 32768
+_E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
+def _rows(t: torch.Tensor, dtype, dims: int, what):
+    """The address of a device tensor of that type whose last dimension is contiguous."""
+    if t.is_cuda and t.dtype == dtype and t.dim() == dims and (t.numel() == 0 or t.shape[-1] == 1 or t.stride(-1) == 1):
+        return t.data_ptr()
+    raise ValueError(f"{what}: expected a {dtype} device tensor of {dims} dimensions, contiguous along the last")
+
+
+class KVCache:
+    """A paged cache of keys and values: k and v [pages, heads, page_size, head_dim], bf16 or float8_e4m3fn, the latter with scales
+    [pages, heads, page_size, head_dim / 32] float8_e8m0fnu (or the same bytes as uint8).  k and v may be views, with a page's
+    tokens ahead of its heads or the two in one tensor, but lie alike; the scales lie like the elements.  The tensors are the
+    caller's: the cache keeps them alive, and what they hold may change at any time."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales=None, v_scales=None):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.dtype not in (torch.bfloat16, _E4M3):
+            raise ValueError("k and v must be [pages, heads, page_size, head_dim], both bfloat16 or both float8_e4m3fn")
+        mx = k.dtype == _E4M3
+        scales = [t for t in (k_scales, v_scales) if t is not None]
+        if len(scales) != (2 if mx else 0):
+            raise ValueError("float8_e4m3fn keys and values come with scales for both, bfloat16 ones without")
+        # a dimension of one entry has no stride to speak of
+        strides = [st if n > 1 else 0 for n, st in zip(k.shape, k.stride())]
+        alike = lambda t, unit: all(n <= 1 or st * unit == mine for n, st, mine in zip(t.shape[:3], t.stride()[:3], strides))
+        if (k.shape[3] > 1 and (k.stride(3) != 1 or v.stride(3) != 1)) or not alike(v, 1):
+            raise ValueError("k and v must have the same strides and be contiguous along the last dimension")
+        for t in scales:
+            if t.dtype not in (_E8M0, torch.uint8) or t.shape != (*k.shape[:3], k.shape[3] // 32) or t.device != k.device:
+                raise ValueError("scales must be [pages, heads, page_size, head_dim / 32], float8_e8m0fnu or uint8")
+            if not alike(t, 32) or (t.shape[3] > 1 and t.stride(3) != 1):
+                raise ValueError("scales must lie like the elements, a 32nd of the strides")
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        pages, self.heads, self.page_size, self.head_dim = k.shape
+        self.format = TORQ_FMT_MXFP8 if mx else TORQ_FMT_BF16
+        self._struct = _KVCacheStruct(k.data_ptr(), v.data_ptr(), *((t.data_ptr() for t in scales) if mx else (None, None)),
+                                      pages, *strides[:3], self.format, self.heads, self.head_dim, self.page_size)
+        self.kv_handle = C.c_void_p(C.addressof(self._struct))
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_size: int, head_dim: int, fmt: int = TORQ_FMT_BF16, device="cuda"):
+        """A cache of its own, not initialised."""
+        if fmt == TORQ_FMT_BF16:
+            return cls(*(torch.empty((pages, heads, page_size, head_dim), dtype=torch.bfloat16, device=device) for _ in "kv"))
+        if fmt != TORQ_FMT_MXFP8 or head_dim % 32:
+            raise ValueError("a cache is TORQ_FMT_BF16, or TORQ_FMT_MXFP8 with a head_dim that is a multiple of 32")
+        return cls(*(torch.empty((pages, heads, page_size, n), dtype=t, device=device)
+                     for t, n in ((_E4M3, head_dim), (_E8M0, head_dim // 32)) for _ in "kv"))
+
+
+def torq_block_tables(held, lengths, free_pages, cursor, block_tables, page_size: int, tokens: int, slots=None, cursor_out=None,
+                      stream=None):
+    """Pages and slots of a step whose requests go from held [B] to lengths [B] tokens (see include/torq.h).  int32 device
+    tensors; block_tables [B, width] is written in place, cursor_out may be cursor.  Returns (slots int64 [tokens], cursor_out)."""
+    pair = (_host or _native()).block_tables(held, lengths, free_pages, cursor, block_tables, page_size, tokens, slots, cursor_out, stream)
+    if pair is not None:
+        return pair
+    B, width = block_tables.shape
+    if held.shape != (B,) or lengths.shape != (B,) or free_pages.dim() != 1 or cursor.shape != (1,):
+        raise ValueError("held and lengths must be [B], block_tables [B, width], free_pages [n], cursor [1]")
+    if slots is None:
+        slots = torch.empty((tokens,), dtype=torch.int64, device=held.device)
+    if cursor_out is None:
+        cursor_out = torch.empty_like(cursor)
+    if slots.shape != (tokens,) or cursor_out.shape != (1,):
+        raise ValueError("slots must be [tokens], cursor_out [1]")
+    i32 = torch.int32
+    _check(lib().torq_block_tables(_dev(held, i32, "held"), _dev(lengths, i32, "lengths"), B, _dev(free_pages, i32, "free_pages"),
+                                   free_pages.numel(), _dev(cursor, i32, "cursor"), _dev(cursor_out, i32, "cursor_out"),
+                                   _rows(block_tables, i32, 2, "block_tables"), block_tables.stride(0) if B > 1 else width, width,
+                                   int(page_size), _dev(slots, torch.int64, "slots"), tokens, _stream(stream)), "torq_block_tables")
+    return slots, cursor_out
+
+
+def torq_cache_append(cache: KVCache, key, value, slots, stream=None):
+    """key and value [tokens, heads, head_dim] bf16 (views of a projection's output will do) to the cache's slots [tokens] int64."""
+    if (_host or _native()).cache_append(cache, key, value, slots, stream):
+        return
+    T = slots.numel()
+    if key.shape != (T, cache.heads, cache.head_dim) or value.shape != key.shape or slots.dim() != 1:
+        raise ValueError("key and value must be [tokens, heads, head_dim], slots [tokens]")
+    at = lambda t: [st if n > 1 else 0 for n, st in zip(t.shape[:2], t.stride())]
+    _check(lib().torq_cache_append(cache.kv_handle, _rows(key, torch.bfloat16, 3, "key"), *at(key), _rows(value, torch.bfloat16, 3, "value"),
+                                   *at(value), _dev(slots, torch.int64, "slots"), T, _stream(stream)), "torq_cache_append")
+
+
+def torq_paged_attention_workspace_bytes(cache: KVCache, heads: int, B: int, width: int) -> int:
+    return int(lib().torq_paged_attention_workspace_bytes(cache.kv_handle, heads, B, width))
+
+
+def torq_paged_attention(q, cache: KVCache, block_tables, lengths, scale: float, out=None, workspace=None, stream=None):
+    """q [B, heads, head_dim] bf16 (a view will do), one new token of each request, over its first lengths[b] tokens, which
+    block_tables [B, width] finds in the cache.  Returns out [B, heads, head_dim] bf16."""
+    y = (_host or _native()).paged_attention(q, cache, block_tables, lengths, scale, out, workspace, stream)
+    if y is not None:
+        return y
+    B, heads, dim = q.shape
+    width = block_tables.shape[-1]
+    if dim != cache.head_dim or block_tables.shape != (B, width) or lengths.shape != (B,):
+        raise ValueError("q must be [B, heads, head_dim], block_tables [B, width], lengths [B]")
+    if workspace is None:
+        workspace = _scratch(q, max(torq_paged_attention_workspace_bytes(cache, heads, B, width), 16), stream)
+    if out is None:
+        out = torch.empty((B, heads, dim), dtype=torch.bfloat16, device=q.device)
+    if out.shape != q.shape:
+        raise ValueError("out must be [B, heads, head_dim]")
+    at = [st if n > 1 else 0 for n, st in zip(q.shape[:2], q.stride())]
+    _check(lib().torq_paged_attention(cache.kv_handle, _rows(q, torch.bfloat16, 3, "q"), *at, heads,
+                                      _rows(block_tables, torch.int32, 2, "block_tables"), block_tables.stride(0) if B > 1 else width,
+                                      width, _dev(lengths, torch.int32, "lengths"), B, float(scale), _dev(out, torch.bfloat16, "out"),
+                                      _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)),
+           "torq_paged_attention")
+    return out
+
+
+def torq_add_rms_norm(x, residual, weight, eps: float, fmt: int = TORQ_FMT_BF16, residual_out=None, out=None, scales=None, stream=None):
+    """x [M, d] (+ residual [M, d], or None), normalised and times weight [d], all bf16.  Returns (out, scales, residual_out): out bf16
+    and scales None, or with TORQ_FMT_MXFP8 float8_e4m3fn and float8_e8m0fnu [M, d / 32]; residual_out, bf16(x + residual), is None
+    where residual is.  residual_out may be residual or x."""
+    got = (_host or _native()).add_rms_norm(x, residual, weight, eps, fmt, residual_out, out, scales, stream)
+    if got is not None:
+        return got
+    M, d = x.shape
+    mx = fmt == TORQ_FMT_MXFP8
+    bf16 = torch.bfloat16
+    if weight.shape != (d,) or (residual is not None and residual.shape != (M, d)):
+        raise ValueError("x and residual must be [M, d], weight [d]")
+    if residual is None and residual_out is not None:
+        raise ValueError("residual_out without a residual")
+    if residual is not None and residual_out is None:
+        residual_out = torch.empty((M, d), dtype=bf16, device=x.device)
+    if out is None:
+        out = torch.empty((M, d), dtype=_E4M3 if mx else bf16, device=x.device)
+    if mx and scales is None:
+        scales = torch.empty((M, d // 32), dtype=_E8M0, device=x.device)
+    if out.shape != (M, d) or (residual_out is not None and residual_out.shape != (M, d)) or (mx and scales.shape != (M, d // 32)):
+        raise ValueError("out and residual_out must be [M, d], scales [M, d / 32]")
+    _check(lib().torq_add_rms_norm(_dev(x, bf16, "x"), None if residual is None else _dev(residual, bf16, "residual"),
+                                   _dev(weight, bf16, "weight"), M, d, float(eps), int(fmt),
+                                   None if residual is None else _dev(residual_out, bf16, "residual_out"),
+                                   _dev(out, _E4M3 if mx else bf16, "out"), _dev(scales, _E8M0, "scales") if mx else None,
+                                   _stream(stream)), "torq_add_rms_norm")
+    return out, scales if mx else None, residual_out

@@ -836,4 +836,107 @@ int torq_calibrate_intra(const float *X_host, int64_t n, int max_iter, int k_top
   return guarded([&] { return torq_calibrate_intra_impl(X_host, n, max_iter, k_top, P, lambda, eps, R_intra_host, losses_host, n_eval); });
 }
 
+// ---- the attention side of a decoder block -----------------------------------------------------
+namespace {
+
+inline bool misaligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
+
+// TORQ_OK, or what is wrong with the sizes of a cache (its arrays are looked at by the calls that touch them)
+int cache_sizes(const torq_kv_cache_t *c) {
+  if (!c || (c->format != TORQ_FMT_BF16 && c->format != TORQ_FMT_MXFP8)) return TORQ_EINVAL;
+  const int unit = c->format == TORQ_FMT_BF16 ? 8 : 32;
+  if (c->heads <= 0 || c->head_dim <= 0 || c->head_dim > TORQ_MAX_HEAD_DIM || c->head_dim % unit) return TORQ_EINVAL;
+  if (c->page_size <= 0 || c->page_size % 16 || c->page_size > 65536 || c->pages < 0 || c->pages > 0x7FFFFFFF) return TORQ_EINVAL;
+  for (int64_t stride : {c->page_stride, c->head_stride, c->token_stride})
+    if (stride < 0 || stride % unit) return TORQ_EINVAL;
+  if (c->token_stride >= ((int64_t)1 << 29) / c->page_size) return TORQ_EINVAL;
+  return TORQ_OK;
+}
+int cache_arrays(const torq_kv_cache_t *c) {
+  if (c->pages == 0) return TORQ_OK;                 // (nothing of them is touched)
+  if (!c->k || !c->v || (c->format == TORQ_FMT_MXFP8 && (!c->k_scales || !c->v_scales))) return TORQ_EINVAL;
+  return misaligned(c->k) || misaligned(c->v) ? TORQ_EALIGN : TORQ_OK;
+}
+inline bool bad_stride(int64_t stride) { return stride < 0 || stride % 8; }
+
+// B requests of `heads` query heads over `width` pages: what the grid and 32-bit positions hold
+bool attention_sizes(const torq_kv_cache_t *c, int heads, int64_t B, int width) {
+  return heads > 0 && heads % c->heads == 0 && heads <= (1 << 20) && B >= 0 && width >= 0 &&
+         (int64_t)width * c->page_size <= (int64_t)1 << 30 && B <= 0x7FFFFFFF / heads;
+}
+
+}  // namespace
+
+int torq_block_tables(const int32_t *held, const int32_t *lengths, int64_t B, const int32_t *free_pages, int64_t free_count,
+                      const int32_t *cursor, int32_t *cursor_out, int32_t *block_tables, int64_t table_stride, int width,
+                      int page_size, int64_t *slots, int64_t tokens, void *stream) {
+  if (B < 0 || free_count < 0 || tokens < 0 || width < 0 || table_stride < width || page_size <= 0) return TORQ_EINVAL;
+  if (!cursor || !cursor_out || (B > 0 && (!held || !lengths || (width > 0 && !block_tables)))) return TORQ_EINVAL;
+  if ((free_count > 0 && !free_pages) || (tokens > 0 && !slots)) return TORQ_EINVAL;
+  for (const void *p : {(const void *)held, (const void *)lengths, (const void *)free_pages, (const void *)cursor,
+                        (const void *)cursor_out, (const void *)block_tables})
+    if (misaligned_to(p, 4)) return TORQ_EALIGN;
+  if (misaligned_to(slots, 8)) return TORQ_EALIGN;
+  hipError_t e = torq::launch_block_tables(held, lengths, B, free_pages, free_count, cursor, cursor_out, block_tables, table_stride,
+                                           width, page_size, slots, tokens, (hipStream_t)stream);
+  return e == hipSuccess ? TORQ_OK : hip_fail(e);
+}
+
+int torq_cache_append(const torq_kv_cache_t *cache, const void *key_bf16, int64_t key_token_stride, int64_t key_head_stride,
+                      const void *value_bf16, int64_t value_token_stride, int64_t value_head_stride,
+                      const int64_t *slots, int64_t tokens, void *stream) {
+  int status = cache_sizes(cache);
+  if (status != TORQ_OK) return status;
+  if (tokens < 0 || bad_stride(key_token_stride) || bad_stride(key_head_stride) || bad_stride(value_token_stride) ||
+      bad_stride(value_head_stride))
+    return TORQ_EINVAL;
+  if (cache->heads > (1 << 20)) return TORQ_EINVAL;
+  if (tokens == 0) return TORQ_OK;
+  status = cache_arrays(cache);
+  if (status == TORQ_EINVAL || !key_bf16 || !value_bf16 || !slots) return TORQ_EINVAL;
+  if (status != TORQ_OK || misaligned(key_bf16) || misaligned(value_bf16) || misaligned_to(slots, 8)) return TORQ_EALIGN;
+  hipError_t e = torq::launch_cache_append(*cache, key_bf16, key_token_stride, key_head_stride, value_bf16, value_token_stride,
+                                           value_head_stride, slots, tokens, (hipStream_t)stream);
+  return e == hipSuccess ? TORQ_OK : hip_fail(e);
+}
+
+size_t torq_paged_attention_workspace_bytes(const torq_kv_cache_t *cache, int heads, int64_t B, int width) {
+  if (cache_sizes(cache) != TORQ_OK || !attention_sizes(cache, heads, B, width) || B == 0) return 0;
+  return torq::paged_attention_workspace_bytes(*cache, heads, B, width);
+}
+
+int torq_paged_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads,
+                         const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths, int64_t B,
+                         float scale, void *out_bf16, void *workspace, size_t workspace_bytes, void *stream) {
+  int status = cache_sizes(cache);
+  if (status != TORQ_OK) return status;
+  if (!attention_sizes(cache, heads, B, width) || table_stride < width || bad_stride(q_stride) || bad_stride(q_head_stride) ||
+      !std::isfinite(scale))
+    return TORQ_EINVAL;
+  if (B == 0) return TORQ_OK;
+  const size_t need = torq::paged_attention_workspace_bytes(*cache, heads, B, width);
+  status = cache_arrays(cache);
+  if (status == TORQ_EINVAL || !q_bf16 || (width > 0 && !block_tables) || !lengths || !out_bf16 || (need && !workspace)) return TORQ_EINVAL;
+  if (status != TORQ_OK || misaligned(q_bf16) || misaligned(out_bf16) || misaligned(workspace)) return TORQ_EALIGN;
+  if (misaligned_to(block_tables, 4) || misaligned_to(lengths, 4)) return TORQ_EALIGN;
+  if (workspace_bytes < need) return TORQ_EWORKSPACE;
+  hipError_t e = torq::launch_paged_attention(*cache, q_bf16, q_stride, q_head_stride, heads, block_tables, table_stride, width,
+                                              lengths, B, scale, out_bf16, workspace, (hipStream_t)stream);
+  return e == hipSuccess ? TORQ_OK : hip_fail(e);
+}
+
+int torq_add_rms_norm(const void *x_bf16, const void *residual_bf16, const void *weight_bf16, int64_t M, int d, float eps,
+                      int format, void *residual_out_bf16, void *out, uint8_t *scales, void *stream) {
+  if (M < 0 || d <= 0 || d % TORQ_BLOCK != 0 || d > TORQ_MAX_NORM_D || !(eps >= 0.0f) || !std::isfinite(eps)) return TORQ_EINVAL;
+  if (format != TORQ_FMT_BF16 && format != TORQ_FMT_MXFP8) return TORQ_EINVAL;
+  if (!residual_bf16 != !residual_out_bf16) return TORQ_EINVAL;
+  if (M == 0) return TORQ_OK;
+  if (!x_bf16 || !weight_bf16 || !out || (format == TORQ_FMT_MXFP8 && !scales)) return TORQ_EINVAL;
+  if (misaligned(x_bf16) || misaligned(residual_bf16) || misaligned(weight_bf16) || misaligned(residual_out_bf16) || misaligned(out))
+    return TORQ_EALIGN;
+  hipError_t e = torq::launch_add_rms_norm(x_bf16, residual_bf16, weight_bf16, M, d, eps, format, residual_out_bf16, out, scales,
+                                           (hipStream_t)stream);
+  return e == hipSuccess ? TORQ_OK : hip_fail(e);
+}
+
 }  // extern "C"

@@ -1,5 +1,6 @@
 // The calls of the binding that a program makes again and again, marshalled in C++ (module _host): torq_linear,
-// torq_rotate_quantize (and _fmt), torq_block_gram (and _positions) and torq_code_histogram.  The kernels of the smallest of
+// torq_rotate_quantize (and _fmt), torq_block_gram (and _positions), torq_code_histogram, torq_block_tables, torq_cache_append,
+// torq_paged_attention and torq_add_rms_norm.  The kernels of the smallest of
 // them take 3 to 6 us, the interpreter 8 to 13 for the attribute look-ups, checks, allocations and a ctypes call.  One row
 // through a 4096 x 4096 layer, a call among others: 10.2 us -> 5.6 or 6.4 from one process to the next (the kernel, replayed from a
 // graph, 5.7).
@@ -19,6 +20,8 @@
 #include <cstdint>
 #include <optional>
 
+#include "../../include/torq.h"
+
 namespace {
 
 using at::Tensor;
@@ -33,8 +36,13 @@ int (*f_gram_positions)(const void *, int64_t, int, int, void *, void *, size_t,
 size_t (*f_gram_bytes)(int);
 int (*f_histogram)(const void *, int64_t, int, void *, void *, size_t, void *);
 size_t (*f_histogram_bytes)();
+decltype(&torq_block_tables) f_tables;
+decltype(&torq_cache_append) f_append;
+decltype(&torq_paged_attention) f_attention;
+decltype(&torq_paged_attention_workspace_bytes) f_attention_bytes;
+decltype(&torq_add_rms_norm) f_norm;
 PyObject *py_stream, *py_check;
-PyObject *s_handle, *s_value, *s_d;
+PyObject *s_handle, *s_kv_handle, *s_value, *s_d;
 
 struct NotPlain {};
 
@@ -73,9 +81,9 @@ void *pointer(PyObject *o) {
   if (!p && PyErr_Occurred()) throw NotPlain{};
   return p;
 }
-// Rotation.handle, a ctypes pointer (None once it is closed)
-void *handle_of(PyObject *rot) {
-  Ref h(PyObject_GetAttr(rot, s_handle));
+// an attribute that is a ctypes pointer: Rotation.handle (None once it is closed), KVCache.kv_handle
+void *handle_of(PyObject *owner, PyObject *name) {
+  Ref h(PyObject_GetAttr(owner, name));
   if (h.p == Py_None) throw NotPlain{};
   Ref v(PyObject_GetAttr(h.p, s_value));
   return pointer(v.p);
@@ -148,7 +156,7 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (x.dim() != 2 || W_q.dim() != 2 || W_s.dim() != 2) throw NotPlain{};
     const int64_t M = x.size(0), d = x.size(1), N = W_q.size(0);
     if (d != d_of(a[0]) || W_q.size(1) != d / 2 || W_s.size(0) != N || W_s.size(1) != d / 32) throw NotPlain{};
-    void *const handle = handle_of(a[0]), *const xp = address(x, at::kBFloat16), *const qp = address(W_q, at::kByte),
+    void *const handle = handle_of(a[0], s_handle), *const xp = address(x, at::kBFloat16), *const qp = address(W_q, at::kByte),
                 *const sp = address(W_s, at::kByte), *const stream = stream_of(a[6]);
     const std::optional<c10::Stream> user = user_of(a[6], ws_in);
     Tensor out;
@@ -175,7 +183,7 @@ PyObject *rotate_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const float global_scale = (float)PyFloat_AS_DOUBLE(a[3]);
     const int64_t M = x.size(0), d = x.size(1);
     if (d != d_of(a[0])) throw NotPlain{};
-    void *const handle = handle_of(a[0]), *const xp = address(x, at::kBFloat16), *const stream = stream_of(a[6]);
+    void *const handle = handle_of(a[0], s_handle), *const xp = address(x, at::kBFloat16), *const stream = stream_of(a[6]);
     Tensor codes, scales;
     int status;
     {
@@ -242,6 +250,162 @@ PyObject *histogram(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// a tensor of that type and number of dimensions, contiguous along the last
+void *rows(const Tensor &t, at::ScalarType type, int64_t dims) {
+  if (!t.is_cuda() || t.scalar_type() != type || t.dim() != dims || (t.numel() && t.size(dims - 1) > 1 && t.stride(dims - 1) != 1)) throw NotPlain{};
+  return t.data_ptr();
+}
+void shape(const Tensor &t, at::IntArrayRef sizes) {
+  if (t.sizes() != sizes) throw NotPlain{};
+}
+// a dimension of one entry has no stride to speak of
+int64_t step(const Tensor &t, int64_t dim) { return t.size(dim) > 1 ? t.stride(dim) : 0; }
+double number(PyObject *o) {
+  if (!PyFloat_CheckExact(o)) throw NotPlain{};
+  return PyFloat_AS_DOUBLE(o);
+}
+const torq_kv_cache_t *cache_of(PyObject *cache) {
+  const torq_kv_cache_t *c = static_cast<const torq_kv_cache_t *>(handle_of(cache, s_kv_handle));
+  if (!c) throw NotPlain{};
+  return c;
+}
+PyObject *packed(std::initializer_list<PyObject *> items) {
+  PyObject *t = PyTuple_New((Py_ssize_t)items.size());
+  Py_ssize_t i = 0;
+  bool fine = t != nullptr;
+  for (PyObject *o : items) {
+    fine = fine && o;
+    if (t && o) PyTuple_SET_ITEM(t, i++, o);
+    else Py_XDECREF(o);
+  }
+  if (!fine) Py_CLEAR(t);
+  return t;
+}
+
+// block_tables(held, lengths, free_pages, cursor, block_tables, page_size, tokens, slots, cursor_out, stream)
+PyObject *block_tables(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return plain_or_none([&]() -> PyObject * {
+    if (n != 10) throw NotPlain{};
+    const Tensor &held = tensor(a[0]), &lengths = tensor(a[1]), &pages = tensor(a[2]), &cursor = tensor(a[3]), &tables = tensor(a[4]);
+    const Tensor *slots_in = optional(a[7]), *cursor_in = optional(a[8]);
+    const int page_size = small_integer(a[5]);
+    const int64_t tokens = integer(a[6]);
+    int32_t *const tp = static_cast<int32_t *>(rows(tables, at::kInt, 2));
+    const int64_t B = tables.size(0), width = tables.size(1);
+    shape(held, {B});
+    shape(lengths, {B});
+    shape(cursor, {1});
+    if (pages.dim() != 1 || width > 0x7FFFFFFF || tokens < 0) throw NotPlain{};
+    if (slots_in) shape(*slots_in, {tokens});
+    if (cursor_in) shape(*cursor_in, {1});
+    auto ints = [](const Tensor &t) { return static_cast<int32_t *>(address(t, at::kInt)); };
+    const int32_t *const hp = ints(held), *const lp = ints(lengths), *const fp = ints(pages), *const cp = ints(cursor);
+    void *const stream_p = stream_of(a[9]);
+    Tensor slots, after;
+    int status;
+    {
+      Unlocked unlocked;
+      slots = given_or_new(slots_in, held, {tokens}, at::kLong);
+      after = given_or_new(cursor_in, held, {1}, at::kInt);
+      status = f_tables(hp, lp, B, fp, pages.numel(), cp, ints(after), tp, B > 1 ? tables.stride(0) : width, (int)width, page_size,
+                        static_cast<int64_t *>(address(slots, at::kLong)), tokens, stream_p);
+    }
+    return ok(status, "torq_block_tables") ? packed({wrapped(a[7], slots), wrapped(a[8], after)}) : nullptr;
+  });
+}
+
+// cache_append(cache, key, value, slots, stream): True
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return plain_or_none([&]() -> PyObject * {
+    if (n != 5) throw NotPlain{};
+    const torq_kv_cache_t *const cache = cache_of(a[0]);
+    const Tensor &key = tensor(a[1]), &value = tensor(a[2]), &slots = tensor(a[3]);
+    const void *const kp = rows(key, at::kBFloat16, 3), *const vp = rows(value, at::kBFloat16, 3);
+    const int64_t *const sp = static_cast<const int64_t *>(address(slots, at::kLong)), T = slots.numel();
+    shape(slots, {T});
+    shape(key, {T, cache->heads, cache->head_dim});
+    shape(value, key.sizes());
+    void *const stream_p = stream_of(a[4]);
+    int status;
+    {
+      Unlocked unlocked;
+      status = f_append(cache, kp, step(key, 0), step(key, 1), vp, step(value, 0), step(value, 1), sp, T, stream_p);
+    }
+    if (!ok(status, "torq_cache_append")) return nullptr;
+    Py_RETURN_TRUE;
+  });
+}
+
+// paged_attention(q, cache, block_tables, lengths, scale, out, workspace, stream)
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return plain_or_none([&]() -> PyObject * {
+    if (n != 8) throw NotPlain{};
+    const Tensor &q = tensor(a[0]), &tables = tensor(a[2]), &lengths = tensor(a[3]);
+    const torq_kv_cache_t *const cache = cache_of(a[1]);
+    const float scale = (float)number(a[4]);
+    const Tensor *out_in = optional(a[5]), *ws_in = optional(a[6]);
+    const void *const qp = rows(q, at::kBFloat16, 3);
+    const int32_t *const tp = static_cast<const int32_t *>(rows(tables, at::kInt, 2)), *const lp = static_cast<const int32_t *>(address(lengths, at::kInt));
+    const int64_t B = q.size(0), heads = q.size(1), width = tables.size(1);
+    shape(lengths, {B});
+    shape(q, {B, heads, cache->head_dim});
+    if (tables.size(0) != B || heads > 0x7FFFFFFF || width > 0x7FFFFFFF) throw NotPlain{};
+    if (out_in) shape(*out_in, q.sizes());
+    void *const stream_p = stream_of(a[7]);
+    const std::optional<c10::Stream> user = user_of(a[7], ws_in);
+    Tensor out;
+    int status;
+    {
+      Unlocked unlocked;
+      const Tensor ws = scratch(ws_in, q, ws_in ? 1 : std::max<int64_t>((int64_t)f_attention_bytes(cache, (int)heads, B, (int)width), 16), user);
+      out = given_or_new(out_in, q, q.sizes(), at::kBFloat16);
+      status = f_attention(cache, qp, step(q, 0), step(q, 1), (int)heads, tp, B > 1 ? tables.stride(0) : width, (int)width, lp, B, scale,
+                           address(out, at::kBFloat16), address(ws, at::kByte), (size_t)ws.numel(), stream_p);
+    }
+    return ok(status, "torq_paged_attention") ? wrapped(a[5], out) : nullptr;
+  });
+}
+
+// add_rms_norm(x, residual, weight, eps, format, residual_out, out, scales, stream)
+PyObject *add_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return plain_or_none([&]() -> PyObject * {
+    if (n != 9) throw NotPlain{};
+    const Tensor &x = tensor(a[0]), &weight = tensor(a[2]);
+    const Tensor *residual = optional(a[1]), *sum_in = optional(a[5]), *out_in = optional(a[6]), *scales_in = optional(a[7]);
+    const float eps = (float)number(a[3]);
+    const int format = small_integer(a[4]);
+    const bool mx = format == TORQ_FMT_MXFP8;
+    if (x.dim() != 2 || x.size(1) > 0x7FFFFFFF || (sum_in && !residual) || (scales_in && !mx)) throw NotPlain{};
+    const int64_t M = x.size(0), d = x.size(1);
+    shape(weight, {d});
+    if (residual) shape(*residual, {M, d});
+    if (sum_in) shape(*sum_in, {M, d});
+    if (out_in) shape(*out_in, {M, d});
+    if (scales_in) shape(*scales_in, {M, d / 32});
+    const void *const xp = address(x, at::kBFloat16), *const wp = address(weight, at::kBFloat16);
+    const void *const rp = residual ? address(*residual, at::kBFloat16) : nullptr;
+    void *const stream_p = stream_of(a[8]);
+    Tensor sum, out, scales;
+    int status;
+    {
+      Unlocked unlocked;
+      if (residual) sum = given_or_new(sum_in, x, {M, d}, at::kBFloat16);
+      out = given_or_new(out_in, x, {M, d}, mx ? at::kFloat8_e4m3fn : at::kBFloat16);
+      if (mx) scales = given_or_new(scales_in, x, {M, d / 32}, at::kFloat8_e8m0fnu);
+      status = f_norm(xp, rp, wp, M, (int)d, eps, format, residual ? address(sum, at::kBFloat16) : nullptr,
+                      address(out, mx ? at::kFloat8_e4m3fn : at::kBFloat16),
+                      mx ? static_cast<uint8_t *>(address(scales, at::kFloat8_e8m0fnu)) : nullptr, stream_p);
+    }
+    if (!ok(status, "torq_add_rms_norm")) return nullptr;
+    auto or_none = [](bool there, PyObject *given, const Tensor &t) {
+      if (there) return wrapped(given, t);
+      Py_INCREF(Py_None);
+      return Py_None;
+    };
+    return packed({wrapped(a[6], out), or_none(mx, a[7], scales), or_none(residual != nullptr, a[5], sum)});
+  });
+}
+
 // bind({entry point: address}, stream function, check function)
 PyObject *bind(PyObject *, PyObject *args) {
   PyObject *entries, *stream, *check;
@@ -262,6 +426,11 @@ PyObject *bind(PyObject *, PyObject *args) {
   TORQ_BIND(f_gram_bytes, "torq_block_gram_workspace_bytes")
   TORQ_BIND(f_histogram, "torq_code_histogram")
   TORQ_BIND(f_histogram_bytes, "torq_code_histogram_workspace_bytes")
+  TORQ_BIND(f_tables, "torq_block_tables")
+  TORQ_BIND(f_append, "torq_cache_append")
+  TORQ_BIND(f_attention, "torq_paged_attention")
+  TORQ_BIND(f_attention_bytes, "torq_paged_attention_workspace_bytes")
+  TORQ_BIND(f_norm, "torq_add_rms_norm")
 #undef TORQ_BIND
   Py_INCREF(stream);
   Py_INCREF(check);
@@ -278,6 +447,10 @@ PyMethodDef methods[] = {
     {"rotate_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotate_quantize)), METH_FASTCALL, nullptr},
     {"gram", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gram)), METH_FASTCALL, nullptr},
     {"histogram", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(histogram)), METH_FASTCALL, nullptr},
+    {"block_tables", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(block_tables)), METH_FASTCALL, nullptr},
+    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_append)), METH_FASTCALL, nullptr},
+    {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attention)), METH_FASTCALL, nullptr},
+    {"add_rms_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(add_rms_norm)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -285,9 +458,10 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, null
 
 PyMODINIT_FUNC PyInit__host() {
   s_handle = PyUnicode_InternFromString("handle");
+  s_kv_handle = PyUnicode_InternFromString("kv_handle");
   s_value = PyUnicode_InternFromString("value");
   s_d = PyUnicode_InternFromString("d");
-  if (!s_handle || !s_value || !s_d) return nullptr;
+  if (!s_handle || !s_kv_handle || !s_value || !s_d) return nullptr;
   PyObject *m = PyModule_Create(&module);
   // (binding.py binds no module built against another torch)
   if (m && PyModule_AddStringConstant(m, "torch_version", TORQ_TORCH_VERSION) != 0) Py_CLEAR(m);

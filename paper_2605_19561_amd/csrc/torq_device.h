@@ -155,6 +155,7 @@ __device__ __forceinline__ float amax8(const float z[8]) {
 // them without defining them; the readings are those of include/torq.h.
 
 constexpr int FMT_NONE = -1, FMT_MXFP4 = 0, FMT_MXINT4 = 1, FMT_NVFP4 = 2;
+constexpr int FMT_BF16 = 8, FMT_MXFP8 = 9;
 
 // MXINT4: eight values -> eight two's-complement nibbles.  inv_scale = 2^(127 - byte) (the product is
 // exact), round to nearest even, clamp to [-7, 7].
@@ -257,6 +258,42 @@ __device__ __forceinline__ void pack_nvfp4(const float *v, float f, float S, uin
 #undef TORQ_DIVIDE_PAIR
     c[n] = r;
   }
+}
+
+// ---------------------------------------------------------------------------
+// MXFP8 (E4M3 elements, E8M0 scale of a block of 32): the scale byte is the least with amax <= 448 * 2^(byte-127).
+// amax = 1.m * 2^E is at most 1.75 * 2^8 * 2^(E-8); beyond m = .75 the sum below carries into the exponent field.
+// 0xFF for an infinity or NaN.
+__device__ __forceinline__ uint32_t mxfp8_scale_from_amax(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  if (u >= 0x7F800000u) return 0xFFu;
+  const int b = (int)((u + 0x1FFFFFu) >> 23) - 8;
+  return (uint32_t)(b < 0 ? 0 : b);
+}
+// Eight elements -> eight E4M3 bytes.  The product with the scale's inverse is exact (or far below E4M3's
+// least value), at most 448 in magnitude, and the conversion rounds to nearest even.
+__device__ __forceinline__ uint2 pack8_e4m3(const float z[8], uint32_t byte) {
+  if (byte == 0xFFu) return make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
+  const float f = e8m0_inverse_f32(byte);
+  int a = __builtin_amdgcn_cvt_pk_fp8_f32(z[0] * f, z[1] * f, 0, false);
+  a = __builtin_amdgcn_cvt_pk_fp8_f32(z[2] * f, z[3] * f, a, true);
+  int b = __builtin_amdgcn_cvt_pk_fp8_f32(z[4] * f, z[5] * f, 0, false);
+  b = __builtin_amdgcn_cvt_pk_fp8_f32(z[6] * f, z[7] * f, b, true);
+  return make_uint2((uint32_t)a, (uint32_t)b);
+}
+// maximum that knows NaN: magnitudes compared as integers, where a NaN lies above infinity
+__device__ __forceinline__ float amax8_nan(const float z[8]) {
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(z[i]) & 0x7FFFFFFFu);
+  return __uint_as_float(a);
+}
+// over the four lanes of a quad, the same way: xor 1 (quad_perm [1,0,3,2]), then xor 2 ([2,3,0,1])
+__device__ __forceinline__ float quad_amax_nan(float v) {
+  uint32_t a = __float_as_uint(v);
+  a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0xB1, 0xF, 0xF, true));
+  a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x4E, 0xF, 0xF, true));
+  return __uint_as_float(a);
 }
 
 // bf16 <-> fp32 bit moves

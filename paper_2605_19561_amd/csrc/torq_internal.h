@@ -182,6 +182,25 @@ int64_t intra_best_angle(const double *u, const double *v, int64_t n, const uint
 void intra_rotation(const float *X, int64_t n, int max_iter, int k_top, int P, double lambda, double eps,
                     double *R_out, double *losses, int *n_eval);
 
+// Pages and slots of a step, and a step's keys and values into a paged cache (paged_cache.hip).
+hipError_t launch_block_tables(const int32_t *held, const int32_t *lengths, int64_t B, const int32_t *free_pages,
+                               int64_t free_count, const int32_t *cursor, int32_t *cursor_out, int32_t *block_tables,
+                               int64_t table_stride, int width, int page_size, int64_t *slots, int64_t tokens,
+                               hipStream_t stream);
+hipError_t launch_cache_append(const torq_kv_cache_t &cache, const void *key, int64_t key_token_stride, int64_t key_head_stride,
+                               const void *value, int64_t value_token_stride, int64_t value_head_stride,
+                               const int64_t *slots, int64_t tokens, hipStream_t stream);
+
+// Attention of one new token over a paged cache (paged_attention.hip).
+size_t paged_attention_workspace_bytes(const torq_kv_cache_t &cache, int heads, int64_t B, int width);
+hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, int64_t q_stride, int64_t q_head_stride, int heads,
+                                  const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths,
+                                  int64_t B, float scale, void *out, void *workspace, hipStream_t stream);
+
+// Residual addition and RMS norm (rms_norm.hip).
+hipError_t launch_add_rms_norm(const void *x, const void *residual, const void *weight, int64_t M, int d, float eps,
+                               int format, void *residual_out, void *out, uint8_t *scales, hipStream_t stream);
+
 // 1024 x 256 lanes issue iters x 16 MFMAs each on operands taken from `words` (see diag.hip).
 hipError_t launch_mfma_burn(int kind, const uint32_t *words, uint32_t n_words, int iters, float *sink,
                             hipStream_t stream);
