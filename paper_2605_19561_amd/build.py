@@ -29,6 +29,7 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
 # else in that kernel uses it.
 EXTRA = {"rotate_quant.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
          "mxfp4_gemm_ring.hip": ["-Wno-inline-asm"],
+         "paged_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "rotate_butterfly.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "mxfp4_gemm_skinny.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
          "mxfp4_gemm_stream.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"]}

@@ -849,7 +849,7 @@ int cache_sizes(const torq_kv_cache_t *c) {
   if (c->page_size <= 0 || c->page_size % 16 || c->page_size > 65536 || c->pages < 0 || c->pages > 0x7FFFFFFF) return TORQ_EINVAL;
   for (int64_t stride : {c->page_stride, c->head_stride, c->token_stride})
     if (stride < 0 || stride % unit) return TORQ_EINVAL;
-  if (c->token_stride >= ((int64_t)1 << 29) / c->page_size) return TORQ_EINVAL;
+  if (c->token_stride < c->head_dim || c->token_stride >= ((int64_t)1 << 29) / c->page_size) return TORQ_EINVAL;
   return TORQ_OK;
 }
 int cache_arrays(const torq_kv_cache_t *c) {
@@ -859,10 +859,12 @@ int cache_arrays(const torq_kv_cache_t *c) {
 }
 inline bool bad_stride(int64_t stride) { return stride < 0 || stride % 8; }
 
-// B requests of `heads` query heads over `width` pages: what the grid and 32-bit positions hold
+// B requests of `heads` query heads over `width` pages: what the grid and 32-bit numbers of tokens (and of tiles of 32, under
+// every 16 query heads of a key head) hold
 bool attention_sizes(const torq_kv_cache_t *c, int heads, int64_t B, int width) {
-  return heads > 0 && heads % c->heads == 0 && heads <= (1 << 20) && B >= 0 && width >= 0 &&
-         (int64_t)width * c->page_size <= (int64_t)1 << 30 && B <= 0x7FFFFFFF / heads;
+  if (heads <= 0 || heads % c->heads || heads > (1 << 20) || B < 0 || width < 0 || B > 0x7FFFFFFF / heads) return false;
+  const int64_t most = (int64_t)width * c->page_size, columns = B * c->heads * ((heads / c->heads + 15) / 16);
+  return most <= (int64_t)1 << 30 && columns <= 0x7FFFFFFF / (most / 32 + 1);
 }
 
 }  // namespace
