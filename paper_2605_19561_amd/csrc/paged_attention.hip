@@ -22,6 +22,8 @@
 // moment that O is.  The loads are buffer loads over the 16 tokens of a group (a group lies in one page) as far as they are tokens of
 // the request: what is past the length, in no page or past the last tile has no records, costs no traffic and comes back as
 // zeros, so the loop knows no other case (and a NaN behind the length is not read).
+#include <algorithm>
+
 #include "torq_device.h"
 #include "torq_internal.h"
 
@@ -79,191 +81,207 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t records(const void *base, int6
   const uint64_t u = (uint32_t)__builtin_amdgcn_readfirstlane((int)p) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32;
   return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(u), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
-template <int N>
+template <int N, bool ONCE>
 __device__ __forceinline__ auto buffer_load(__amdgpu_buffer_rsrc_t r, int at) {
-  if constexpr (N == 16) return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
-  else if constexpr (N == 8) return __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0);
-  else return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+  if constexpr (N == 16) return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, LOAD_POLICY<ONCE>);
+  else if constexpr (N == 8) return __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, LOAD_POLICY<ONCE>);
+  else return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, LOAD_POLICY<ONCE>);
 }
 
-__device__ __forceinline__ int tiles_of(const AttentionArgs &a, int b) {
-  const int64_t n = a.lengths[b];
-  return (int)(((n < 0 ? 0 : n < a.most ? n : a.most) + ATT_TILE - 1) / ATT_TILE);
-}
+// Tokens of a request, and its tiles.
+__device__ __forceinline__ int length_of(const AttentionArgs &a, int n) { return n < 0 ? 0 : n < a.most ? n : (int)a.most; }
+__device__ __forceinline__ int tiles_of(const AttentionArgs &a, int n) { return (length_of(a, n) + ATT_TILE - 1) / ATT_TILE; }
 
-// DP: head_dim rounded up to what the operands hold.
-template <int DP, bool F8>
+// DP: head_dim rounded up to what the operands hold.  SOLO: a workgroup for each (request, key head, rows), which is its run.
+template <int DP, bool F8, bool ONCE, bool SOLO>
 __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   constexpr int KS = DP / 32;                       // k-steps of S
   constexpr int E = DP < 128 ? DP / 16 : 8;         // consecutive values of V in a lane
   constexpr int NH = DP / (16 * E);                 // such pieces of a row
   constexpr int BYTES = F8 ? 1 : 2;
   constexpr int KL = DP * BYTES / 64;               // 16-byte loads of a lane for a group of 16 rows of K
-  __shared__ float o_all[ATT_WAVES][ATT_ROWS][16 * E + 4];      // a piece of O at a time
+  __shared__ f32x4 o_all[ATT_WAVES][ATT_ROWS][4 * E + 1];       // a piece of O at a time
   __shared__ float m_all[ATT_WAVES][ATT_ROWS], l_all[ATT_WAVES][ATT_ROWS];
-  __shared__ int wave_tiles[ATT_WAVES], found_b, found_before;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
   const int columns = a.kv_heads * a.row_groups;    // (key head, rows) of a request
-
-  // tiles of one column, request by request: a thread adds up `per` of them
-  const int per = (a.B + 255) / 256;
-  int mine = 0;
-  for (int i = 0; i < per; ++i)
-    if (tid * per + i < a.B) mine += tiles_of(a, tid * per + i);
-  int sum = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int up = __shfl_up(sum, o);
-    if (lane >= o) sum += up;
-  }
-  if (lane == 63) wave_tiles[wave] = sum;
-  __syncthreads();
-  int total = 0;
-#pragma unroll
-  for (int w = 0; w < ATT_WAVES; ++w) {
-    if (w < wave) sum += wave_tiles[w];
-    total += wave_tiles[w];
-  }
-  total = __builtin_amdgcn_readfirstlane(total);
-  if (blockIdx.x == 0) {                            // (for the join)
-    int at = sum - mine;
-    for (int i = 0; i < per; ++i)
-      if (tid * per + i < a.B) {
-        a.before[tid * per + i] = at;
-        at += tiles_of(a, tid * per + i);
-      }
-    if (tid == 0) a.before[a.B] = total;
-  }
-  const Runs runs(total * columns, gridDim.x);
-  if ((int)blockIdx.x >= runs.runs) return;
-  const int run_begin = runs.begin(blockIdx.x), run_end = runs.begin(blockIdx.x + 1);
-  if (run_begin == run_end) return;                 // (nothing at all)
-  // the request in which the run begins
-  if ((sum - mine) * columns <= run_begin && run_begin < sum * columns) {
-    int at = sum - mine, b = tid * per;
-    for (int t; (at + (t = tiles_of(a, b))) * columns <= run_begin; ++b) at += t;
-    found_b = b, found_before = at;
-  }
-  __syncthreads();
-  int b = __builtin_amdgcn_readfirstlane(found_b), before = __builtin_amdgcn_readfirstlane(found_before);
   const uniform_ints lengths = (uniform_ints)(uintptr_t)a.lengths;
+
+  // one (request, key head, rows), as far as it lies in the run: its tiles first ... last - 1 of `tiles`
+  struct Segment {
+    int b, before, tiles, length, kv_head, rows_at, first, last, end;      // end: the tile of the run behind it
+  };
+  int run_begin = 0, run_end = 0;
+  auto segment = [&](int at, int b, int before) {
+    Segment s;
+    for (;; ++b) {
+      s.length = length_of(a, lengths[b]);
+      s.tiles = (s.length + ATT_TILE - 1) / ATT_TILE;
+      if (at < (before + s.tiles) * columns) break;
+      before += s.tiles;
+    }
+    s.b = b, s.before = before;
+    const int column = __builtin_amdgcn_readfirstlane((at - before * columns) / s.tiles), begin = before * columns + column * s.tiles;
+    s.rows_at = __builtin_amdgcn_readfirstlane(column % a.row_groups), s.kv_head = __builtin_amdgcn_readfirstlane(column / a.row_groups);
+    s.first = at - begin, s.last = min(run_end - begin, s.tiles), s.end = begin + s.last;
+    return s;
+  };
+  Segment seg;
+  if constexpr (SOLO) {
+    const int b = blockIdx.x / columns, column = blockIdx.x - b * columns;
+    const int length = length_of(a, lengths[b]), tiles = (length + ATT_TILE - 1) / ATT_TILE;
+    seg = Segment{b, 0, tiles, length, column / a.row_groups, column % a.row_groups, 0, tiles, 0};
+  } else {
+    // tiles of one column, request by request: every wave adds them up, a lane `per` of them
+    const int per = (a.B + 63) / 64;
+    int mine = 0;
+    for (int i = 0; i < per; ++i)
+      if (lane * per + i < a.B) mine += tiles_of(a, a.lengths[lane * per + i]);
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(sum, o);
+      if (lane >= o) sum += up;
+    }
+    const int total = __builtin_amdgcn_readlane(sum, 63);
+    if (blockIdx.x == 0 && wave == 0) {             // (for the join)
+      int at = sum - mine;
+      for (int i = 0; i < per; ++i)
+        if (lane * per + i < a.B) {
+          a.before[lane * per + i] = at;
+          at += tiles_of(a, a.lengths[lane * per + i]);
+        }
+      if (lane == 0) a.before[a.B] = total;
+    }
+    const Runs runs(total * columns, gridDim.x);
+    if ((int)blockIdx.x >= runs.runs) return;
+    run_begin = runs.begin(blockIdx.x), run_end = runs.begin(blockIdx.x + 1);
+    if (run_begin == run_end) return;               // (nothing at all)
+    // the lane whose requests the run begins in
+    const int owner = __builtin_ctzll(__ballot(run_begin < sum * columns));
+    seg = segment(run_begin, owner * per, __builtin_amdgcn_readlane(sum - mine, owner));
+  }
 
   // what a lane reads of a group of 16 tokens, in bytes from its first token
   const int k_at = n * a.token_bytes + 16 * g, v_at = 4 * g * a.token_bytes + E * n * BYTES;
-
-  for (int at = run_begin; at < run_end;) {
-    // one (request, key head, rows), as far as it lies in the run
-    int length = lengths[b];
-    length = length < 0 ? 0 : length < a.most ? length : (int)a.most;
-    const int tiles = (length + ATT_TILE - 1) / ATT_TILE;
-    if (at >= (before + tiles) * columns) {
-      before += tiles;
-      ++b;
-      continue;
-    }
-    const int column = (at - before * columns) / tiles, rows_at = column % a.row_groups, kv_head = column / a.row_groups;
-    const int column_begin = before * columns + column * tiles;
-    const int first = at - column_begin, last = min(run_end - column_begin, tiles);     // tiles of it
-    const uniform_ints table = (uniform_ints)(uintptr_t)(a.tables + b * a.table_stride);
-    const int row = rows_at * ATT_ROWS + n;         // query head of this lane's column within the group
-    const bool real = row < a.group;
-
-    // Q^T as the B operand: column n, the i of this lane's K values
-    bf16x8 q[KS];
+  // Q^T as the B operand: column n, the i of this lane's K values
+  bf16x8 q[KS];
+  auto load_q = [&](const Segment &s) {
+    const int row = s.rows_at * ATT_ROWS + n;       // query head of this lane's column within the group
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int i = F8 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
+    for (int t = 0; t < KS; ++t) {
+      const int i = F8 ? 64 * (t / 2) + 16 * g + 8 * (t % 2) : 32 * t + 8 * g;
       u32x4 v = {0, 0, 0, 0};
-      if (real && i < a.dim)
-        v = *reinterpret_cast<const u32x4 *>(a.q + b * a.q_stride + (int64_t)(kv_head * a.group + row) * a.q_head_stride + i);
-      q[s] = as_bf16(v);
+      if (row < a.group && i < a.dim)
+        v = *reinterpret_cast<const u32x4 *>(a.q + s.b * a.q_stride + (int64_t)(s.kv_head * a.group + row) * a.q_head_stride + i);
+      q[t] = as_bf16(v);
     }
-    // the pages of a tile's two groups of 16 tokens; how many of a group are tokens; where they lie, in bytes
-    auto look_up = [&](int tile, int (&page)[2]) {
+  };
+  // the pages of a tile's two groups of 16 tokens; how many of a group are tokens; where they lie, in bytes
+  struct Pages {
+    int page[2];
+  };
+  auto look_up = [&](const Segment &s, int tile) {
+    Pages p;
+    const uniform_ints table = (uniform_ints)(uintptr_t)(a.tables + s.b * a.table_stride);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int t16 = min(2 * tile + u, (length - 1) / 16);
-        page[u] = table[(int)((uint64_t)t16 * (uint64_t)a.page16_magic >> 38)];
-      }
-    };
-    struct Place {
-      int count[2];
-      int64_t at[2];
-    };
-    auto place = [&](int tile, const int (&page)[2]) {
-      Place p;
+    for (int u = 0; u < 2; ++u) {
+      const int t16 = min(2 * tile + u, (s.length - 1) / 16);
+      p.page[u] = t16 >= 0 && s.length > 0 ? table[(int)((uint64_t)t16 * (uint64_t)a.page16_magic >> 38)] : -1;
+    }
+    return p;
+  };
+  struct Place {
+    int count[2];
+    int64_t at[2];
+  };
+  auto place = [&](const Segment &s, int tile, const Pages &p) {
+    Place w;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int t = tile * ATT_TILE + 16 * u, t16 = 2 * tile + u;
-        const int in_page = (t16 - (int)((uint64_t)t16 * (uint64_t)a.page16_magic >> 38) * (a.page_size / 16)) * 16;
-        const bool there = tile < last && t < length && page[u] >= 0 && page[u] < a.pages;
-        p.count[u] = there ? min(length - t, 16) : 0;
-        p.at[u] = ((there ? page[u] : 0) * a.page_stride + kv_head * a.head_stride) * BYTES + (int64_t)in_page * a.token_bytes;
-      }
-      return p;
-    };
-    auto rows_of = [&](const char *base, const Place &p, int u) {
-      const int bytes = p.count[u] ? (p.count[u] - 1) * a.token_bytes + a.dim * BYTES : 0;
-      return records(base, p.at[u], bytes);
-    };
-    u32x4 k[2][KL];
-    uint32_t v[2][NH][4][E * BYTES / 4];
-    uint32_t k_scales[2][KL], v_scales[2][NH][4];
-    auto load_k = [&](const Place &p) {
+    for (int u = 0; u < 2; ++u) {
+      const int t = tile * ATT_TILE + 16 * u, t16 = 2 * tile + u;
+      const int in_page = (t16 - (int)((uint64_t)t16 * (uint64_t)a.page16_magic >> 38) * (a.page_size / 16)) * 16;
+      const bool there = tile < s.last && t < s.length && p.page[u] >= 0 && p.page[u] < a.pages;
+      w.count[u] = there ? min(s.length - t, 16) : 0;
+      w.at[u] = ((there ? p.page[u] : 0) * a.page_stride + s.kv_head * a.head_stride) * BYTES + (int64_t)in_page * a.token_bytes;
+    }
+    return w;
+  };
+  auto rows_of = [&](const char *base, const Place &p, int u) {
+    return records(base, p.at[u], p.count[u] ? (p.count[u] - 1) * a.token_bytes + a.dim * BYTES : 0);
+  };
+  auto scales_of = [&](const uint8_t *base, const Place &p, int u) {
+    return records(base, p.at[u] / 32, p.count[u] ? (p.count[u] - 1) * (a.token_bytes / 32) + a.dim / 32 : 0);
+  };
+  u32x4 k[2][KL];
+  uint32_t v[2][NH][4][E * BYTES / 4];
+  uint32_t k_scales[2][KL], v_scales[2][NH][4];
+  auto load_k = [&](const Place &p) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const __amdgpu_buffer_rsrc_t r = rows_of(a.k, p, u);
+    for (int u = 0; u < 2; ++u) {
+      const __amdgpu_buffer_rsrc_t r = rows_of(a.k, p, u);
+#pragma unroll
+      for (int s = 0; s < KL; ++s)
+        k[u][s] = buffer_load<16, ONCE>(r, (64 * s + 16 * g) < a.dim * BYTES ? k_at + 64 * s : ATT_FAR);
+      if constexpr (F8) {
+        const __amdgpu_buffer_rsrc_t rs = scales_of(a.k_scales, p, u);
 #pragma unroll
         for (int s = 0; s < KL; ++s)
-          k[u][s] = buffer_load<16>(r, (64 * s + 16 * g) < a.dim * BYTES ? k_at + 64 * s : ATT_FAR);
-        if constexpr (F8) {
-          const int bytes = p.count[u] ? (p.count[u] - 1) * (a.token_bytes / 32) + a.dim / 32 : 0;
-          const __amdgpu_buffer_rsrc_t rs = records(a.k_scales, p.at[u] / 32, bytes);
-#pragma unroll
-          for (int s = 0; s < KL; ++s)
-            k_scales[u][s] = __builtin_amdgcn_raw_buffer_load_b8(rs, 64 * s + 16 * g < a.dim ? (k_at + 64 * s) / 32 : ATT_FAR, 0, 0);
-        }
+          k_scales[u][s] = __builtin_amdgcn_raw_buffer_load_b8(rs, 64 * s + 16 * g < a.dim ? (k_at + 64 * s) / 32 : ATT_FAR, 0, 0);
       }
-    };
-    auto load_v = [&](const Place &p) {
+    }
+  };
+  auto load_v = [&](const Place &p) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const __amdgpu_buffer_rsrc_t r = rows_of(a.v, p, u);
-        __amdgpu_buffer_rsrc_t rs;
-        if constexpr (F8) {
-          const int bytes = p.count[u] ? (p.count[u] - 1) * (a.token_bytes / 32) + a.dim / 32 : 0;
-          rs = records(a.v_scales, p.at[u] / 32, bytes);
+    for (int u = 0; u < 2; ++u) {
+      const __amdgpu_buffer_rsrc_t r = rows_of(a.v, p, u);
+      __amdgpu_buffer_rsrc_t rs;
+      if constexpr (F8) rs = scales_of(a.v_scales, p, u);
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int where = v_at + e * a.token_bytes + 16 * E * h * BYTES;
+          const bool in = 16 * E * h + E * n < a.dim;
+          const auto x = buffer_load<E * BYTES, ONCE>(r, in ? where : ATT_FAR);
+          if constexpr (E * BYTES == 4) v[u][h][e][0] = x;
+          else
+#pragma unroll
+            for (int c = 0; c < E * BYTES / 4; ++c) v[u][h][e][c] = x[c];
+          if constexpr (F8) v_scales[u][h][e] = __builtin_amdgcn_raw_buffer_load_b8(rs, in ? where / 32 : ATT_FAR, 0, 0);
         }
-#pragma unroll
-        for (int h = 0; h < NH; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int where = v_at + e * a.token_bytes + 16 * E * h * BYTES;
-            const bool in = 16 * E * h + E * n < a.dim;
-            const auto x = buffer_load<E * BYTES>(r, in ? where : ATT_FAR);
-            if constexpr (E * BYTES == 4) v[u][h][e][0] = x;
-            else
-#pragma unroll
-              for (int c = 0; c < E * BYTES / 4; ++c) v[u][h][e][c] = x[c];
-            if constexpr (F8) v_scales[u][h][e] = __builtin_amdgcn_raw_buffer_load_b8(rs, in ? where / 32 : ATT_FAR, 0, 0);
-          }
-      }
-    };
+    }
+  };
+
+  Pages pages = look_up(seg, seg.first + wave);
+  Place here = place(seg, seg.first + wave, pages);
+  load_q(seg);
+  __builtin_amdgcn_sched_barrier(0);                // (K ahead of V, as in the loop, whose waits count them)
+  load_k(here);
+  __builtin_amdgcn_sched_barrier(0);
+  load_v(here);
+  for (;;) {
+    // what comes behind this segment: its first tile is on the way when this one's last is worked on
+    const bool more = !SOLO && seg.end < run_end;
+    Segment behind = seg;
+    behind.last = 0;                                // (no tile of it is there)
+    if (more) behind = segment(seg.end, seg.b, seg.before);
+    Pages pages_behind = look_up(behind, behind.first + wave);
+    pages = look_up(seg, seg.first + wave + ATT_WAVES);
     f32x4 o[NH * E];
 #pragma unroll
     for (int i = 0; i < NH * E; ++i) o[i] = f32x4{0, 0, 0, 0};
     float m = -INFINITY, l = 0.0f;
-
-    int page[2];
-    look_up(first + wave, page);
-    Place here = place(first + wave, page);
-    load_k(here);
-    __builtin_amdgcn_sched_barrier(0);              // (in the order of the loop's own, whose waits count them)
-    load_v(here);
-    look_up(first + wave + ATT_WAVES, page);
-    for (int tile = first + wave; tile < last; tile += ATT_WAVES) {
-      const Place next = place(tile + ATT_WAVES, page);
-      look_up(tile + 2 * ATT_WAVES, page);
+    if (seg.first + wave >= seg.last) {             // (nothing for this wave)
+      here = place(behind, behind.first + wave, pages_behind);
+      load_k(here);
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(here);
+    }
+    for (int tile = seg.first + wave; tile < seg.last; tile += ATT_WAVES) {
+      Place next;
+      if (tile + ATT_WAVES < seg.last) next = place(seg, tile + ATT_WAVES, pages);
+      else next = place(behind, behind.first + wave, pages_behind);
+      pages = look_up(seg, tile + 2 * ATT_WAVES);
       f32x4 st[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -341,48 +359,54 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       load_v(next);
       here = next;
     }
-    // the lanes of a column hold the sums of their own tokens
+    // the four waves' put together.  The lanes of a column hold the sums of their own tokens.
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     if (g == 0) m_all[wave][n] = m, l_all[wave][n] = l;
-    const int rows = min(ATT_ROWS, a.group - rows_at * ATT_ROWS);
-    const bool whole = first == 0 && last == tiles;
-    uint16_t *const out = a.out + ((int64_t)b * a.kv_heads * a.group + kv_head * a.group + rows_at * ATT_ROWS) * a.dim;
+    const int rows = min(ATT_ROWS, a.group - seg.rows_at * ATT_ROWS);
+    const bool whole = seg.first == 0 && seg.last == seg.tiles;
+    uint16_t *const out = a.out + ((int64_t)seg.b * a.kv_heads * a.group + seg.kv_head * a.group + seg.rows_at * ATT_ROWS) * a.dim;
     // where the run begins within a column: its first place in the workspace, else its second
-    const int64_t part = ((int64_t)blockIdx.x * 2 + (at == run_begin ? 0 : 1)) * ATT_ROWS;
+    const int64_t part = ((int64_t)blockIdx.x * 2 + (seg.end - (seg.last - seg.first) == run_begin ? 0 : 1)) * ATT_ROWS;
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
       // lane (n, g), o[h E + j][r] = O[head n][16 E h + E (4 g + r) + j]
 #pragma unroll
-      for (int j = 0; j < E; ++j)
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o_all[wave][n][E * (4 * g + r) + j] = o[h * E + j][r];
+        for (int j = 0; j < E; j += 4)
+          o_all[wave][n][(E * (4 * g + r) + j) / 4] = f32x4{o[h * E + j][r], o[h * E + j + 1][r], o[h * E + j + 2][r], o[h * E + j + 3][r]};
       __syncthreads();
-      const int begin = 16 * E * h, count = min(16 * E, a.dim - begin);
-      for (int x = tid; x < rows * count; x += 256) {
-        const int r = x / count, i = x - r * count;
+      const int begin = 16 * E * h, quads = min(16 * E, a.dim - begin) / 4;
+      for (int x = tid; x < rows * quads; x += 256) {
+        const int r = x / quads, c = x - r * quads;
         float top = -INFINITY;
 #pragma unroll
         for (int w = 0; w < ATT_WAVES; ++w) top = fmaxf(top, m_all[w][r]);
         const float base = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f, value = 0.0f;
+        float sum = 0.0f;
+        f32x4 value = {0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < ATT_WAVES; ++w) {
           const float f = __builtin_amdgcn_exp2f(m_all[w][r] - base);
           sum += f * l_all[w][r];
-          value += f * o_all[w][r][i];
+          value += f * o_all[w][r][c];
         }
         if (whole) {
-          const __bf16 y = (__bf16)(sum != 0.0f ? value / sum : 0.0f);
-          out[r * a.dim + begin + i] = __builtin_bit_cast(uint16_t, y);
+          bf16x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = (__bf16)(sum != 0.0f ? value[e] / sum : 0.0f);
+          *reinterpret_cast<bf16x4 *>(out + r * a.dim + begin + 4 * c) = y;
         } else {
-          a.part[(part + r) * a.dim + begin + i] = value;
-          if (begin + i == 0) a.part_ml[2 * (part + r)] = top, a.part_ml[2 * (part + r) + 1] = sum;
+          *reinterpret_cast<f32x4 *>(a.part + (part + r) * a.dim + begin + 4 * c) = value;
+          if (begin + c == 0) a.part_ml[2 * (part + r)] = top, a.part_ml[2 * (part + r) + 1] = sum;
         }
       }
-      __syncthreads();
+      if (h + 1 < NH || more) __syncthreads();
     }
-    at = column_begin + last;
+    if (!more) break;
+    seg = behind;
+    load_q(seg);
   }
 }
 
@@ -457,10 +481,19 @@ int groups_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   const int64_t groups = (tiles + ATT_WAVES - 1) / ATT_WAVES;
   return (int)(groups < 1 ? 1 : groups < ATT_GROUPS ? groups : ATT_GROUPS);
 }
+// Every request within so few tokens that a workgroup each (four rounds of its waves) is done before runs would be made out
+bool solo_of(const torq_kv_cache_t &cache, int width) { return (int64_t)width * cache.page_size <= 16 * ATT_TILE; }
+// Past the cache: rows of whole lines, and more of them than the cache holds
+bool once_of(const torq_kv_cache_t &cache, int64_t B, int width) {
+  const int bytes = cache.format == FMT_BF16 ? 2 : 1;
+  const double pages = (double)std::min<int64_t>(cache.pages, B * (int64_t)width);
+  return cache.head_dim * bytes % 128 == 0 && 2.0 * pages * cache.page_size * cache.heads * cache.head_dim * bytes > ONE_PASS_WEIGHT_BYTES;
+}
 size_t before_bytes(int64_t B) { return ((size_t)(B + 1) * sizeof(int) + 255) & ~(size_t)255; }
 }  // namespace
 
 size_t paged_attention_workspace_bytes(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
+  if (solo_of(cache, width)) return 0;
   return before_bytes(B) + (size_t)groups_of(cache, heads, B, width) * 2 * ATT_ROWS * (cache.head_dim + 2) * sizeof(float);
 }
 
@@ -470,19 +503,27 @@ hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, i
   const int row_groups = row_groups_of(cache, heads), groups = groups_of(cache, heads, B, width);
   if (cache.pages == 0) width = 0;                  // no token has a page: nothing of the cache is touched
   const int page16 = cache.page_size / 16;
-  float *const part = (float *)((char *)workspace + before_bytes(B));
+  float *const part = (float *)((uintptr_t)workspace + before_bytes(B));
   AttentionArgs a{(const char *)cache.k, (const char *)cache.v, cache.k_scales, cache.v_scales, cache.pages, cache.page_stride,
                   cache.head_stride, (int)cache.token_stride * (cache.format == FMT_BF16 ? 2 : 1), (const uint16_t *)q, q_stride,
                   q_head_stride, block_tables, lengths, table_stride, ((int64_t)1 << 38) / page16 + 1,
                   (int64_t)width * cache.page_size, (int)B, cache.page_size, cache.heads, heads / cache.heads, row_groups,
                   cache.head_dim, scale * 1.44269504088896340736f, (uint16_t *)out, part, part + (size_t)groups * 2 * ATT_ROWS * cache.head_dim,
                   (int *)workspace};
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, stream, a); };
-  const bool f8 = cache.format == FMT_MXFP8;
-  if (cache.head_dim <= 64) go(f8 ? paged_attention_kernel<64, true> : paged_attention_kernel<64, false>);
-  else if (cache.head_dim <= 128) go(f8 ? paged_attention_kernel<128, true> : paged_attention_kernel<128, false>);
-  else go(f8 ? paged_attention_kernel<256, true> : paged_attention_kernel<256, false>);
-  hipLaunchKernelGGL(paged_attention_join_kernel, dim3((unsigned)(B * heads)), dim3(256), 0, stream, a, groups);
+  const bool f8 = cache.format == FMT_MXFP8, solo = solo_of(cache, width), once = once_of(cache, B, width);
+  const unsigned items = (unsigned)(B * cache.heads * row_groups);
+  auto go = [&](auto dp, auto of8) {
+    constexpr int DP = decltype(dp)::value;
+    constexpr bool F8 = decltype(of8)::value;
+    if (solo) hipLaunchKernelGGL((paged_attention_kernel<DP, F8, false, true>), dim3(items), dim3(256), 0, stream, a);
+    else if (once) hipLaunchKernelGGL((paged_attention_kernel<DP, F8, true, false>), dim3(groups), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((paged_attention_kernel<DP, F8, false, false>), dim3(groups), dim3(256), 0, stream, a);
+  };
+  auto of_format = [&](auto dp) { f8 ? go(dp, std::true_type{}) : go(dp, std::false_type{}); };
+  if (cache.head_dim <= 64) of_format(std::integral_constant<int, 64>{});
+  else if (cache.head_dim <= 128) of_format(std::integral_constant<int, 128>{});
+  else of_format(std::integral_constant<int, 256>{});
+  if (!solo) hipLaunchKernelGGL(paged_attention_join_kernel, dim3((unsigned)(B * heads)), dim3(256), 0, stream, a, groups);
   return hipGetLastError();
 }
 

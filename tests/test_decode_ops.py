@@ -333,6 +333,17 @@ def test_paged_attention(tq, either_way, heads, kv_heads, dim, page, lengths, fm
 
 
 @gpu
+@pytest.mark.parametrize("heads,kv_heads,dim,page,lengths,fmt,layout", ATTENTION)
+def test_paged_attention_with_tables_for_long_requests(tq, heads, kv_heads, dim, page, lengths, fmt, layout):
+    # the same requests where the tables would hold long ones: the tokens are cut into runs by the lengths
+    cache, q, tables, lens, pages = attention_case(tq, len(lengths), heads, kv_heads, dim, page, lengths, fmt, layout, 1)
+    want = attention_reference(q, values_of(cache, "k"), values_of(cache, "v"), tables, lens, dim ** -0.5, pages)
+    tables = torch.cat([tables, torch.full((len(lengths), 8192 // page + 1), -1, dtype=torch.int32)], 1)
+    got = tq.torq_paged_attention(q.to(DEV), cache, tables.to(DEV), lens.to(DEV), dim ** -0.5)
+    check_attention(got, *want)
+
+
+@gpu
 @pytest.mark.parametrize("fmt", ["bf16", "mxfp8"])
 def test_paged_attention_of_many_ragged_requests(tq, fmt):
     g = np.random.default_rng(5)
