@@ -32,8 +32,16 @@ namespace torq {
 constexpr int ATT_TILE = 32;          // tokens of a wave's step
 constexpr int ATT_WAVES = 4;
 constexpr int ATT_ROWS = 16;          // query heads of a workgroup
-constexpr int ATT_GROUPS = 768;       // workgroups, three for each CU
+constexpr int ATT_GROUPS = 512;       // workgroups, two for each CU
+constexpr int ATT_JOIN = 512;         // threads of a workgroup that joins, at most
+constexpr int ATT_WAYS_ITEMS = 768;  // columns from which each wave has one of its own
 constexpr int ATT_FAR = 0x7FFFFF00;   // an offset past every buffer
+
+// What begins in a run and does not end there: a request, which of the columns that a workgroup works on at a time, in how many runs
+// (0: in none), and the place of the first part; the others are first in their runs.
+struct Cut {
+  int b, columns, parts, place;
+};
 
 struct AttentionArgs {
   const char *k, *v;
@@ -46,17 +54,21 @@ struct AttentionArgs {
   int64_t table_stride, page16_magic; // t / page_size = (t / 16) * page16_magic >> 38
   int64_t most;                       // width * page_size
   int B, page_size, kv_heads, group, row_groups, dim;
+  int solo;                           // a workgroup for each (request, columns that it works on), which is its run
   float scale_log2;                   // scale * log2(e): the softmax is taken to base 2
   uint16_t *out;
   float *part, *part_ml;              // [run][2][16][dim] and [run][2][16][2]: O, and m and l, of a (request, key head) not whole in a run
-  int *before;                        // [B + 1]: tiles of one key head ahead of each request
+  Cut *cuts;                          // [run], or [request][columns that a workgroup works on at a time]
+  int by_item;
 };
 
-// The runs: `tiles` tiles over `runs` workgroups, the first `more` of which have one more than the others.
+// The runs: `tiles` tiles (of a column, or of several side by side) over `runs` workgroups, the first `more` of which have one more
+// than the others; a tile at least for each wave.
 struct Runs {
   int each, more, runs;
-  __device__ Runs(int tiles, int groups) {
-    runs = max(1, min(groups, (tiles + ATT_WAVES - 1) / ATT_WAVES));
+  __device__ Runs(int each, int more) : each(each), more(more), runs(0) {}
+  __device__ Runs(int tiles, int groups, int ways) {
+    runs = max(1, min(groups, (tiles + ways - 1) / ways));
     each = tiles / runs, more = tiles - each * runs;
   }
   __device__ int begin(int run) const { return run * each + min(run, more); }
@@ -92,27 +104,38 @@ __device__ __forceinline__ auto buffer_load(__amdgpu_buffer_rsrc_t r, int at) {
 __device__ __forceinline__ int length_of(const AttentionArgs &a, int n) { return n < 0 ? 0 : n < a.most ? n : (int)a.most; }
 __device__ __forceinline__ int tiles_of(const AttentionArgs &a, int n) { return (length_of(a, n) + ATT_TILE - 1) / ATT_TILE; }
 
-// DP: head_dim rounded up to what the operands hold.  SOLO: a workgroup for each (request, key head, rows), which is its run.
-template <int DP, bool F8, bool ONCE, bool SOLO>
+// DP: head_dim rounded up to what the operands hold.  WAYS: 4, the waves take turns at the tiles of a column; 1, each has a column
+// of its own and all of its tiles in the run.
+template <int DP, bool F8, bool ONCE, int WAYS>
 __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   constexpr int KS = DP / 32;                       // k-steps of S
   constexpr int E = DP < 128 ? DP / 16 : 8;         // consecutive values of V in a lane
   constexpr int NH = DP / (16 * E);                 // such pieces of a row
   constexpr int BYTES = F8 ? 1 : 2;
   constexpr int KL = DP * BYTES / 64;               // 16-byte loads of a lane for a group of 16 rows of K
-  __shared__ f32x4 o_all[ATT_WAVES][ATT_ROWS][4 * E + 1];       // a piece of O at a time
-  __shared__ float m_all[ATT_WAVES][ATT_ROWS], l_all[ATT_WAVES][ATT_ROWS];
+  __shared__ f32x4 o_all[WAYS][ATT_ROWS][WAYS > 1 ? 4 * E + 1 : 1];       // a piece of O at a time
+  __shared__ float m_all[WAYS][ATT_ROWS], l_all[WAYS][ATT_ROWS];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-  const int columns = a.kv_heads * a.row_groups;    // (key head, rows) of a request
+  // (key head, rows) of a request, as many at a time as the workgroup works on
+  const int columns = (a.kv_heads * a.row_groups + ATT_WAVES / WAYS - 1) / (ATT_WAVES / WAYS), way = WAYS > 1 ? wave : 0;
   const uniform_ints lengths = (uniform_ints)(uintptr_t)a.lengths;
 
   // one (request, key head, rows), as far as it lies in the run: its tiles first ... last - 1 of `tiles`
   struct Segment {
     int b, before, tiles, length, kv_head, rows_at, first, last, end;      // end: the tile of the run behind it
   };
-  int run_begin = 0, run_end = 0;
+  const int run = (int)blockIdx.x;
+  int run_begin = 0, run_end = 0, tiles_each = 1, tiles_more = 0;
+  // (all of it the same in every lane of a wave, which the compiler does not see through the loops: scalar registers)
+  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  auto place_column = [&](Segment &s, int column) {
+    if constexpr (WAYS == 1) column = column * ATT_WAVES + wave;
+    s.kv_head = uniform(column / a.row_groups), s.rows_at = uniform(column) - s.kv_head * a.row_groups;
+    if (s.kv_head >= a.kv_heads) s.kv_head = 0, s.rows_at = a.row_groups;      // (no column: no tile of it is there, and no row)
+  };
   auto segment = [&](int at, int b, int before) {
     Segment s;
+    at = uniform(at), b = uniform(b), before = uniform(before);
     for (;; ++b) {
       s.length = length_of(a, lengths[b]);
       s.tiles = (s.length + ATT_TILE - 1) / ATT_TILE;
@@ -120,16 +143,19 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       before += s.tiles;
     }
     s.b = b, s.before = before;
-    const int column = __builtin_amdgcn_readfirstlane((at - before * columns) / s.tiles), begin = before * columns + column * s.tiles;
-    s.rows_at = __builtin_amdgcn_readfirstlane(column % a.row_groups), s.kv_head = __builtin_amdgcn_readfirstlane(column / a.row_groups);
+    s.b = uniform(s.b), s.before = uniform(s.before), s.tiles = uniform(s.tiles), s.length = uniform(s.length);
+    before = s.before;
+    const int column = uniform((at - before * columns) / s.tiles), begin = before * columns + column * s.tiles;
+    place_column(s, column);
     s.first = at - begin, s.last = min(run_end - begin, s.tiles), s.end = begin + s.last;
     return s;
   };
   Segment seg;
-  if constexpr (SOLO) {
+  if (a.solo) {
     const int b = blockIdx.x / columns, column = blockIdx.x - b * columns;
     const int length = length_of(a, lengths[b]), tiles = (length + ATT_TILE - 1) / ATT_TILE;
-    seg = Segment{b, 0, tiles, length, column / a.row_groups, column % a.row_groups, 0, tiles, 0};
+    seg = Segment{b, 0, tiles, length, 0, 0, 0, tiles, 0};
+    place_column(seg, column);
   } else {
     // tiles of one column, request by request: every wave adds them up, a lane `per` of them
     const int per = (a.B + 63) / 64;
@@ -143,22 +169,24 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       if (lane >= o) sum += up;
     }
     const int total = __builtin_amdgcn_readlane(sum, 63);
-    if (blockIdx.x == 0 && wave == 0) {             // (for the join)
-      int at = sum - mine;
-      for (int i = 0; i < per; ++i)
-        if (lane * per + i < a.B) {
-          a.before[lane * per + i] = at;
-          at += tiles_of(a, a.lengths[lane * per + i]);
-        }
-      if (lane == 0) a.before[a.B] = total;
+    // zeros for requests without tokens
+    for (int b = run; b < a.B; b += gridDim.x)
+      if (lengths[b] <= 0 || a.most == 0) {
+        if (a.by_item)
+          for (int x = tid; x < columns; x += 256) a.cuts[b * columns + x] = Cut{0, 0, 0, 0};
+        for (int x = tid; x < a.kv_heads * a.group * a.dim / 8; x += 256)
+          reinterpret_cast<u32x4 *>(a.out + (int64_t)b * a.kv_heads * a.group * a.dim)[x] = u32x4{0, 0, 0, 0};
+      }
+    const Runs runs(total * columns, gridDim.x, WAYS);
+    run_begin = uniform(runs.begin(min(run, runs.runs))), run_end = uniform(runs.begin(min(run + 1, runs.runs)));
+    if (run_begin == run_end) {                     // (fewer tiles than workgroups)
+      if (tid == 0 && !a.by_item) a.cuts[run] = Cut{0, 0, 0, 0};
+      return;
     }
-    const Runs runs(total * columns, gridDim.x);
-    if ((int)blockIdx.x >= runs.runs) return;
-    run_begin = runs.begin(blockIdx.x), run_end = runs.begin(blockIdx.x + 1);
-    if (run_begin == run_end) return;               // (nothing at all)
     // the lane whose requests the run begins in
     const int owner = __builtin_ctzll(__ballot(run_begin < sum * columns));
     seg = segment(run_begin, owner * per, __builtin_amdgcn_readlane(sum - mine, owner));
+    tiles_each = uniform(runs.each), tiles_more = uniform(runs.more);
   }
 
   // what a lane reads of a group of 16 tokens, in bytes from its first token
@@ -200,7 +228,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
     for (int u = 0; u < 2; ++u) {
       const int t = tile * ATT_TILE + 16 * u, t16 = 2 * tile + u;
       const int in_page = (t16 - (int)((uint64_t)t16 * (uint64_t)a.page16_magic >> 38) * (a.page_size / 16)) * 16;
-      const bool there = tile < s.last && t < s.length && p.page[u] >= 0 && p.page[u] < a.pages;
+      const bool there = tile < s.last && t < s.length && s.rows_at < a.row_groups && p.page[u] >= 0 && p.page[u] < a.pages;
       w.count[u] = there ? min(s.length - t, 16) : 0;
       w.at[u] = ((there ? p.page[u] : 0) * a.page_stride + s.kv_head * a.head_stride) * BYTES + (int64_t)in_page * a.token_bytes;
     }
@@ -252,36 +280,42 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
     }
   };
 
-  Pages pages = look_up(seg, seg.first + wave);
-  Place here = place(seg, seg.first + wave, pages);
+  Pages pages = look_up(seg, seg.first + way);
+  Place here = place(seg, seg.first + way, pages);
   load_q(seg);
   __builtin_amdgcn_sched_barrier(0);                // (K ahead of V, as in the loop, whose waits count them)
   load_k(here);
   __builtin_amdgcn_sched_barrier(0);
   load_v(here);
   for (;;) {
+    const bool whole = seg.first == 0 && seg.last == seg.tiles;
+    if (!a.solo && tid == 0 && (a.by_item ? seg.first == 0 : seg.end == run_end)) {
+      const int begin = seg.end - seg.last, column = (begin - seg.before * columns) / seg.tiles;
+      const int parts = seg.first == 0 && !whole ? Runs(tiles_each, tiles_more).of(begin + seg.tiles - 1) - run + 1 : 0;
+      a.cuts[a.by_item ? seg.b * columns + column : run] = Cut{seg.b, column, parts, 2 * run + (run_begin < begin)};
+    }
     // what comes behind this segment: its first tile is on the way when this one's last is worked on
-    const bool more = !SOLO && seg.end < run_end;
+    const bool more = seg.end < run_end;
     Segment behind = seg;
     behind.last = 0;                                // (no tile of it is there)
     if (more) behind = segment(seg.end, seg.b, seg.before);
-    Pages pages_behind = look_up(behind, behind.first + wave);
-    pages = look_up(seg, seg.first + wave + ATT_WAVES);
+    Pages pages_behind = look_up(behind, behind.first + way);
+    pages = look_up(seg, seg.first + way + WAYS);
     f32x4 o[NH * E];
 #pragma unroll
     for (int i = 0; i < NH * E; ++i) o[i] = f32x4{0, 0, 0, 0};
     float m = -INFINITY, l = 0.0f;
-    if (seg.first + wave >= seg.last) {             // (nothing for this wave)
-      here = place(behind, behind.first + wave, pages_behind);
+    if (seg.first + way >= seg.last) {             // (nothing for this wave)
+      here = place(behind, behind.first + way, pages_behind);
       load_k(here);
       __builtin_amdgcn_sched_barrier(0);
       load_v(here);
     }
-    for (int tile = seg.first + wave; tile < seg.last; tile += ATT_WAVES) {
+    for (int tile = seg.first + way; tile < seg.last; tile += WAYS) {
       Place next;
-      if (tile + ATT_WAVES < seg.last) next = place(seg, tile + ATT_WAVES, pages);
-      else next = place(behind, behind.first + wave, pages_behind);
-      pages = look_up(seg, tile + 2 * ATT_WAVES);
+      if (tile + WAYS < seg.last) next = place(seg, tile + WAYS, pages);
+      else next = place(behind, behind.first + way, pages_behind);
+      pages = look_up(seg, tile + 2 * WAYS);
       f32x4 st[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -359,50 +393,71 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       load_v(next);
       here = next;
     }
-    // the four waves' put together.  The lanes of a column hold the sums of their own tokens.
+    // The lanes of a column hold the sums of their own tokens.
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (g == 0) m_all[wave][n] = m, l_all[wave][n] = l;
     const int rows = min(ATT_ROWS, a.group - seg.rows_at * ATT_ROWS);
-    const bool whole = seg.first == 0 && seg.last == seg.tiles;
     uint16_t *const out = a.out + ((int64_t)seg.b * a.kv_heads * a.group + seg.kv_head * a.group + seg.rows_at * ATT_ROWS) * a.dim;
     // where the run begins within a column: its first place in the workspace, else its second
-    const int64_t part = ((int64_t)blockIdx.x * 2 + (seg.end - (seg.last - seg.first) == run_begin ? 0 : 1)) * ATT_ROWS;
+    const int64_t part = ((int64_t)(run * 2 + (seg.end - (seg.last - seg.first) == run_begin ? 0 : 1)) * (ATT_WAVES / WAYS) +
+                          (WAYS == 1 ? wave : 0)) * ATT_ROWS;
+    // lane (n, g), o[h E + j][r] = O[head n][16 E h + E (4 g + r) + j]
+    if constexpr (WAYS == 1) {
+      const float inverse = l != 0.0f ? 1.0f / l : 0.0f;
+      if (n < rows && !whole && g == 0) a.part_ml[2 * (part + n)] = m, a.part_ml[2 * (part + n) + 1] = l;
 #pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      // lane (n, g), o[h E + j][r] = O[head n][16 E h + E (4 g + r) + j]
+      for (int h = 0; h < NH; ++h)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r) {
+          const int i = 16 * E * h + E * (4 * g + r);
+          if (n >= rows || i >= a.dim) continue;
 #pragma unroll
-        for (int j = 0; j < E; j += 4)
-          o_all[wave][n][(E * (4 * g + r) + j) / 4] = f32x4{o[h * E + j][r], o[h * E + j + 1][r], o[h * E + j + 2][r], o[h * E + j + 3][r]};
-      __syncthreads();
-      const int begin = 16 * E * h, quads = min(16 * E, a.dim - begin) / 4;
-      for (int x = tid; x < rows * quads; x += 256) {
-        const int r = x / quads, c = x - r * quads;
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < ATT_WAVES; ++w) top = fmaxf(top, m_all[w][r]);
-        const float base = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f;
-        f32x4 value = {0, 0, 0, 0};
-#pragma unroll
-        for (int w = 0; w < ATT_WAVES; ++w) {
-          const float f = __builtin_amdgcn_exp2f(m_all[w][r] - base);
-          sum += f * l_all[w][r];
-          value += f * o_all[w][r][c];
+          for (int j = 0; j < E; j += 4) {
+            f32x4 x = {o[h * E + j][r], o[h * E + j + 1][r], o[h * E + j + 2][r], o[h * E + j + 3][r]};
+            if (whole) {
+              x *= inverse;
+              *reinterpret_cast<bf16x4 *>(out + n * a.dim + i + j) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+            } else {
+              *reinterpret_cast<f32x4 *>(a.part + (part + n) * a.dim + i + j) = x;
+            }
+          }
         }
-        if (whole) {
-          bf16x4 y;
+    } else {
+      // the waves' put together
+      if (g == 0) m_all[wave][n] = m, l_all[wave][n] = l;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = (__bf16)(sum != 0.0f ? value[e] / sum : 0.0f);
-          *reinterpret_cast<bf16x4 *>(out + r * a.dim + begin + 4 * c) = y;
-        } else {
-          *reinterpret_cast<f32x4 *>(a.part + (part + r) * a.dim + begin + 4 * c) = value;
-          if (begin + c == 0) a.part_ml[2 * (part + r)] = top, a.part_ml[2 * (part + r) + 1] = sum;
+      for (int h = 0; h < NH; ++h) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < E; j += 4)
+            o_all[wave][n][(E * (4 * g + r) + j) / 4] = f32x4{o[h * E + j][r], o[h * E + j + 1][r], o[h * E + j + 2][r], o[h * E + j + 3][r]};
+        __syncthreads();
+        const int begin = 16 * E * h, quads = min(16 * E, a.dim - begin) / 4;
+        for (int x = tid; x < rows * quads; x += 256) {
+          const int r = x / quads, c = x - r * quads;
+          float top = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < WAYS; ++w) top = fmaxf(top, m_all[w][r]);
+          const float base = top == -INFINITY ? 0.0f : top;
+          float sum = 0.0f;
+          f32x4 value = {0, 0, 0, 0};
+#pragma unroll
+          for (int w = 0; w < WAYS; ++w) {
+            const float f = __builtin_amdgcn_exp2f(m_all[w][r] - base);
+            sum += f * l_all[w][r];
+            value += f * o_all[w][r][c];
+          }
+          if (whole) {
+            value *= sum != 0.0f ? 1.0f / sum : 0.0f;
+            *reinterpret_cast<bf16x4 *>(out + r * a.dim + begin + 4 * c) = bf16x4{(__bf16)value[0], (__bf16)value[1], (__bf16)value[2], (__bf16)value[3]};
+          } else {
+            *reinterpret_cast<f32x4 *>(a.part + (part + r) * a.dim + begin + 4 * c) = value;
+            if (begin + c == 0) a.part_ml[2 * (part + r)] = top, a.part_ml[2 * (part + r) + 1] = sum;
+          }
         }
+        if (h + 1 < NH || more) __syncthreads();
       }
-      if (h + 1 < NH || more) __syncthreads();
     }
     if (!more) break;
     seg = behind;
@@ -410,120 +465,119 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   }
 }
 
-// What is not whole within a run, put together in the order of the runs; zeros for a request without tokens.  A workgroup for each (request,
-// query head): its lanes take four values each of the parts of every few runs, which are put together in LDS.
-__global__ void __launch_bounds__(256) paged_attention_join_kernel(AttentionArgs a, int groups) {
-  __shared__ float factor[ATT_GROUPS], reduced[256 / 64];
-  __shared__ f32x4 values[256];
-  const int tid = threadIdx.x, heads = a.kv_heads * a.group, columns = a.kv_heads * a.row_groups;
-  const int b = blockIdx.x / heads, head = blockIdx.x - b * heads, kv_head = head / a.group, r = head % a.group % ATT_ROWS;
-  const int column = kv_head * a.row_groups + head % a.group / ATT_ROWS;
-  const int before = a.before[b], tiles = a.before[b + 1] - before;
-  uint16_t *const out = a.out + (int64_t)blockIdx.x * a.dim;
-  if (tiles == 0) {
-    if (tid < a.dim) out[tid] = 0;
-    return;
-  }
-  const Runs runs(a.before[a.B] * columns, groups);
-  const int begin = before * columns + column * tiles, run0 = runs.of(begin), count = runs.of(begin + tiles - 1) - run0 + 1;
-  if (count == 1) return;
-  // the first part is its run's second place unless the run begins with it
-  const int first = runs.begin(run0) == begin ? 2 * run0 : 2 * run0 + 1;
-  auto place = [&](int i) { return (int64_t)(i ? 2 * (run0 + i) : first) * ATT_ROWS + r; };
-  auto over_group = [&](float v, auto op) {         // of all threads, in a fixed order
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = op(v, __shfl_xor(v, o));
-    __syncthreads();
-    if ((tid & 63) == 0) reduced[tid >> 6] = v;
-    __syncthreads();
-    return op(op(reduced[0], reduced[1]), op(reduced[2], reduced[3]));
-  };
-  float m[ATT_GROUPS / 256], top = -INFINITY, sum = 0.0f;
-#pragma unroll
-  for (int i = 0; i < ATT_GROUPS / 256; ++i) {
-    m[i] = tid + 256 * i < count ? a.part_ml[2 * place(tid + 256 * i)] : -INFINITY;
-    top = fmaxf(top, m[i]);
-  }
-  top = over_group(top, [](float x, float y) { return fmaxf(x, y); });
-  const float base = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-  for (int i = 0; i < ATT_GROUPS / 256; ++i)
-    if (tid + 256 * i < count) {
-      const float f = __builtin_amdgcn_exp2f(m[i] - base);
-      factor[tid + 256 * i] = f;
-      sum += f * a.part_ml[2 * place(tid + 256 * i) + 1];
-    }
-  sum = over_group(sum, [](float x, float y) { return x + y; });
-  // lanes: values 4 c ... 4 c + 3 of every `apart`-th part
-  const int quads = a.dim / 4, apart = 256 / quads, c = tid % quads, from = tid / quads;
+// What is not whole within a run, put together in the order of the tokens.  A thread takes four values of a query head and every
+// so many-th of its parts, in one pass like the waves above; a workgroup's threads for the same values are put together in LDS.
+// many: values, by fours, that a workgroup takes.
+__global__ void __launch_bounds__(ATT_JOIN) paged_attention_join_kernel(AttentionArgs a, int together, int many) {
+  __shared__ f32x4 values[ATT_JOIN];
+  __shared__ float m_all[ATT_JOIN], l_all[ATT_JOIN];
+  const Cut cut = a.cuts[blockIdx.x];
+  if (cut.parts == 0) return;
+  const int tid = threadIdx.x, quads = a.dim / 4, rows = min(ATT_ROWS, a.group);
+  const int all = together * rows * quads, here = min(all, many), ways = blockDim.x / here, way = tid / here;
+  const int x = blockIdx.y * many + (tid - way * here), c = x % quads, r = x / quads % rows, w = x / quads / rows;
+  const int column = cut.columns * together + w, kv_head = column / a.row_groups, row = (column - kv_head * a.row_groups) * ATT_ROWS + r;
+  const bool real = x < all && way < ways && row < a.group && kv_head < a.kv_heads;
+  float m = -INFINITY, l = 0.0f;
   f32x4 v = {0, 0, 0, 0};
-  if (from < apart)
+  if (real) {
 #pragma unroll 4
-    for (int i = from; i < count; i += apart)
-      v += factor[i] * *reinterpret_cast<const f32x4 *>(a.part + place(i) * a.dim + 4 * c);
-  values[tid] = v;
-  __syncthreads();
-  if (tid < quads) {
-    for (int i = 1; i < apart; ++i) v += values[tid + i * quads];
-    bf16x4 y;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (__bf16)(sum != 0.0f ? v[e] / sum : 0.0f);
-    *reinterpret_cast<bf16x4 *>(out + 4 * tid) = y;
+    for (int i = way; i < cut.parts; i += ways) {
+      const int64_t at = ((int64_t)(i ? (cut.place / 2 + i) * 2 : cut.place) * together + w) * ATT_ROWS + r;
+      const float mi = a.part_ml[2 * at], li = a.part_ml[2 * at + 1];
+      const f32x4 vi = *reinterpret_cast<const f32x4 *>(a.part + at * a.dim + 4 * c);
+      const float top = fmaxf(m, mi), base = top == -INFINITY ? 0.0f : top;
+      const float f = __builtin_amdgcn_exp2f(m - base), fi = __builtin_amdgcn_exp2f(mi - base);
+      m = top;
+      l = l * f + li * fi;
+      v = v * f + vi * fi;
+    }
   }
+  m_all[tid] = m, l_all[tid] = l, values[tid] = v;
+  __syncthreads();
+  if (!real || way > 0) return;
+  float top = m;
+  for (int i = 1; i < ways; ++i) top = fmaxf(top, m_all[tid + i * here]);
+  const float base = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - base);
+  l *= f;
+  v *= f;
+  for (int i = 1; i < ways; ++i) {
+    const float fi = __builtin_amdgcn_exp2f(m_all[tid + i * here] - base);
+    l += l_all[tid + i * here] * fi;
+    v += values[tid + i * here] * fi;
+  }
+  v *= l != 0.0f ? 1.0f / l : 0.0f;
+  uint16_t *const out = a.out + ((int64_t)(cut.b * a.kv_heads + kv_head) * a.group + row) * a.dim;
+  *reinterpret_cast<bf16x4 *>(out + 4 * c) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
 }
 
 namespace {
 int row_groups_of(const torq_kv_cache_t &cache, int heads) { return (heads / cache.heads + ATT_ROWS - 1) / ATT_ROWS; }
-// Workgroups: a tile at least for each wave, by the longest that the tables hold
-int groups_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
-  const int64_t most = (int64_t)width * cache.page_size;
-  const int64_t tiles = B * cache.heads * row_groups_of(cache, heads) * ((most + ATT_TILE - 1) / ATT_TILE);
-  const int64_t groups = (tiles + ATT_WAVES - 1) / ATT_WAVES;
-  return (int)(groups < 1 ? 1 : groups < ATT_GROUPS ? groups : ATT_GROUPS);
-}
-// Every request within so few tokens that a workgroup each (four rounds of its waves) is done before runs would be made out
-bool solo_of(const torq_kv_cache_t &cache, int width) { return (int64_t)width * cache.page_size <= 16 * ATT_TILE; }
 // Past the cache: rows of whole lines, and more of them than the cache holds
 bool once_of(const torq_kv_cache_t &cache, int64_t B, int width) {
   const int bytes = cache.format == FMT_BF16 ? 2 : 1;
   const double pages = (double)std::min<int64_t>(cache.pages, B * (int64_t)width);
   return cache.head_dim * bytes % 128 == 0 && 2.0 * pages * cache.page_size * cache.heads * cache.head_dim * bytes > ONE_PASS_WEIGHT_BYTES;
 }
-size_t before_bytes(int64_t B) { return ((size_t)(B + 1) * sizeof(int) + 255) & ~(size_t)255; }
+struct Plan {
+  int ways, groups;
+  bool solo, by_item;
+  int64_t items;
+};
+Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
+  Plan p;
+  const int64_t columns = (int64_t)cache.heads * row_groups_of(cache, heads), tiles = ((int64_t)width * cache.page_size + ATT_TILE - 1) / ATT_TILE;
+  const bool own = columns % ATT_WAVES == 0 && heads / cache.heads <= 2 && B * columns >= ATT_WAYS_ITEMS;
+  p.ways = own || row_groups_of(cache, heads) > 1 ? 1 : ATT_WAVES;
+  // Every request within so few tokens that a workgroup each is done before runs would be made out
+  p.solo = tiles <= 16;
+  p.items = B * ((columns + ATT_WAVES / p.ways - 1) / (ATT_WAVES / p.ways));
+  const int64_t groups = (p.items * tiles + p.ways - 1) / p.ways;       // a tile at least for each wave, by the longest that the tables hold
+  p.groups = p.solo ? (int)p.items : (int)(groups < 1 ? 1 : groups < ATT_GROUPS ? groups : ATT_GROUPS);
+  p.by_item = p.items < p.groups;
+  return p;
+}
+size_t cuts_bytes(const Plan &p) { return (p.by_item ? (size_t)p.items : (size_t)p.groups) * sizeof(Cut); }
+size_t part_rows(const Plan &p) { return (size_t)p.groups * 2 * (ATT_WAVES / p.ways) * ATT_ROWS; }
 }  // namespace
 
 size_t paged_attention_workspace_bytes(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
-  if (solo_of(cache, width)) return 0;
-  return before_bytes(B) + (size_t)groups_of(cache, heads, B, width) * 2 * ATT_ROWS * (cache.head_dim + 2) * sizeof(float);
+  const Plan p = plan_of(cache, heads, B, width);
+  return p.solo ? 0 : cuts_bytes(p) + part_rows(p) * (cache.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, int64_t q_stride, int64_t q_head_stride, int heads,
                                   const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths,
                                   int64_t B, float scale, void *out, void *workspace, hipStream_t stream) {
-  const int row_groups = row_groups_of(cache, heads), groups = groups_of(cache, heads, B, width);
+  const Plan plan = plan_of(cache, heads, B, width);
+  const bool f8 = cache.format == FMT_MXFP8, once = once_of(cache, B, width);
   if (cache.pages == 0) width = 0;                  // no token has a page: nothing of the cache is touched
   const int page16 = cache.page_size / 16;
-  float *const part = (float *)((uintptr_t)workspace + before_bytes(B));
+  float *const part = (float *)((uintptr_t)workspace + cuts_bytes(plan));
   AttentionArgs a{(const char *)cache.k, (const char *)cache.v, cache.k_scales, cache.v_scales, cache.pages, cache.page_stride,
-                  cache.head_stride, (int)cache.token_stride * (cache.format == FMT_BF16 ? 2 : 1), (const uint16_t *)q, q_stride,
+                  cache.head_stride, (int)cache.token_stride * (f8 ? 1 : 2), (const uint16_t *)q, q_stride,
                   q_head_stride, block_tables, lengths, table_stride, ((int64_t)1 << 38) / page16 + 1,
-                  (int64_t)width * cache.page_size, (int)B, cache.page_size, cache.heads, heads / cache.heads, row_groups,
-                  cache.head_dim, scale * 1.44269504088896340736f, (uint16_t *)out, part, part + (size_t)groups * 2 * ATT_ROWS * cache.head_dim,
-                  (int *)workspace};
-  const bool f8 = cache.format == FMT_MXFP8, solo = solo_of(cache, width), once = once_of(cache, B, width);
-  const unsigned items = (unsigned)(B * cache.heads * row_groups);
-  auto go = [&](auto dp, auto of8) {
+                  (int64_t)width * cache.page_size, (int)B, cache.page_size, cache.heads, heads / cache.heads, row_groups_of(cache, heads),
+                  cache.head_dim, plan.solo, scale * 1.44269504088896340736f, (uint16_t *)out, part, part + part_rows(plan) * cache.head_dim,
+                  (Cut *)workspace, plan.by_item};
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(plan.groups), dim3(256), 0, stream, a); };
+  auto of_hint = [&](auto dp, auto of8, auto hint) {
     constexpr int DP = decltype(dp)::value;
-    constexpr bool F8 = decltype(of8)::value;
-    if (solo) hipLaunchKernelGGL((paged_attention_kernel<DP, F8, false, true>), dim3(items), dim3(256), 0, stream, a);
-    else if (once) hipLaunchKernelGGL((paged_attention_kernel<DP, F8, true, false>), dim3(groups), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((paged_attention_kernel<DP, F8, false, false>), dim3(groups), dim3(256), 0, stream, a);
+    constexpr bool F8 = decltype(of8)::value, ONCE = decltype(hint)::value;
+    plan.ways > 1 ? go(paged_attention_kernel<DP, F8, ONCE, ATT_WAVES>) : go(paged_attention_kernel<DP, F8, ONCE, 1>);
   };
-  auto of_format = [&](auto dp) { f8 ? go(dp, std::true_type{}) : go(dp, std::false_type{}); };
-  if (cache.head_dim <= 64) of_format(std::integral_constant<int, 64>{});
-  else if (cache.head_dim <= 128) of_format(std::integral_constant<int, 128>{});
-  else of_format(std::integral_constant<int, 256>{});
-  if (!solo) hipLaunchKernelGGL(paged_attention_join_kernel, dim3((unsigned)(B * heads)), dim3(256), 0, stream, a, groups);
+  auto of_format = [&](auto dp, auto of8) { once ? of_hint(dp, of8, std::true_type{}) : of_hint(dp, of8, std::false_type{}); };
+  auto of_dim = [&](auto dp) { f8 ? of_format(dp, std::true_type{}) : of_format(dp, std::false_type{}); };
+  if (cache.head_dim <= 64) of_dim(std::integral_constant<int, 64>{});
+  else if (cache.head_dim <= 128) of_dim(std::integral_constant<int, 128>{});
+  else of_dim(std::integral_constant<int, 256>{});
+  if (!plan.solo) {
+    // fewer (request, key head)s than runs: many parts each, over more threads; else two or three, one for most runs
+    const int together = ATT_WAVES / plan.ways, values = together * std::min(ATT_ROWS, a.group) * (a.dim / 4);
+    const int threads = plan.by_item ? ATT_JOIN : 256, many = plan.by_item ? 64 : 256;
+    hipLaunchKernelGGL(paged_attention_join_kernel, dim3(plan.by_item ? (unsigned)plan.items : (unsigned)plan.groups, (values + many - 1) / many),
+                       dim3(threads), 0, stream, a, together, many);
+  }
   return hipGetLastError();
 }
 

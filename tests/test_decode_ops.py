@@ -358,6 +358,23 @@ def test_paged_attention_of_many_ragged_requests(tq, fmt):
 
 
 @gpu
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,dim,fmt,layout", [
+    (8, 4, 64, "bf16", "tokens"), (4, 4, 80, "bf16", "tokens"), (16, 4, 128, "bf16", "heads"), (16, 4, 128, "mxfp8", "heads"), (12, 4, 96, "mxfp8", "tokens"),
+    (4, 4, 64, "mxfp8", "heads"), (8, 4, 256, "bf16", "heads"), (8, 4, 192, "mxfp8", "heads"), (40, 2, 64, "bf16", "heads"), (72, 4, 32, "mxfp8", "heads")])
+def test_paged_attention_of_a_large_batch(tq, heads, kv_heads, dim, fmt, layout, wide):
+    # so many (request, key head)s that a wave takes one for itself
+    g = np.random.default_rng(dim)
+    lengths = [int(n) for n in g.integers(0, 90, 200)]
+    lengths[3], lengths[77], lengths[199] = 400, 0, 300
+    cache, q, tables, lens, pages = attention_case(tq, 200, heads, kv_heads, dim, 16, lengths, fmt, layout, 7)
+    want = attention_reference(q, values_of(cache, "k"), values_of(cache, "v"), tables, lens, dim ** -0.5, pages)
+    if wide:
+        tables = torch.cat([tables, torch.full((200, 100), -1, dtype=torch.int32)], 1)
+    check_attention(tq.torq_paged_attention(q.to(DEV), cache, tables.to(DEV), lens.to(DEV), dim ** -0.5), *want)
+
+
+@gpu
 def test_paged_attention_with_one_weight_near_one(tq):
     # scores of hundreds: maxima that move from tile to tile, weights that underflow
     cache, q, tables, lens, pages = attention_case(tq, 3, 8, 2, 128, 16, [500, 64, 1], "bf16", "heads", 3, spread=6.0)
