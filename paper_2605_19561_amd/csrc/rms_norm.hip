@@ -21,6 +21,11 @@ __device__ __forceinline__ u32x4 load16(const u32x4 *p) {
   if constexpr (ONCE) return __builtin_nontemporal_load(p);
   else return *p;
 }
+template <bool ONCE>
+__device__ __forceinline__ void store16(u32x4 *p, u32x4 v) {
+  if constexpr (ONCE) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
 __device__ __forceinline__ u32x4 pack8_bf16(const float (&f)[8]) {
   bf16x8 v;
 #pragma unroll
@@ -32,6 +37,8 @@ __device__ __forceinline__ u32x4 pack8_bf16(const float (&f)[8]) {
 // leave less of the cache to them, so the line is lower).  us without / with the hint, from HBM and with x just written (with the
 // writing): [2048, 5120] to MXFP8, 42 MB 13.4 / 16.1; [4096, 8192] 134 MB 42.5 / 43.3, 72.3 / 62.0; [6144, 8192] 73.2 / 62.1, 107.8 /
 // 103.2; [8192, 8192] 95.5 / 79.4, 144.9 / 136.2, to MXFP8 85.5 / 74.3, 135.2 / 127.8; [16384, 8192] written 286.7 / 283.4
+// residual_out goes past the cache with them: out is what comes next, residual_out a layer later.  [8192, 8192] called in turn with one
+// set of outputs 94.4 -> 80.3, to MXFP8 84.5 -> 74.6, [16384, 8192] with outputs of their own 187 -> 156.
 constexpr double ONE_PASS_NORM_BYTES = 120.0 * 1024 * 1024;
 
 // TPR: lanes of a row, CH: pieces of 8 values that each of them holds.
@@ -63,7 +70,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) add_rms_norm_kernel(con
         unpack8(rs[c], r);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[c][e] += r[e];
-        residual_out[at + c * TPR] = pack8_bf16(s[c]);
+        store16<ONCE>(residual_out + at + c * TPR, pack8_bf16(s[c]));
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) total += s[c][e] * s[c][e];
