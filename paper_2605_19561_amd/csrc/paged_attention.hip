@@ -513,8 +513,9 @@ __global__ void __launch_bounds__(ATT_JOIN) paged_attention_join_kernel(Attentio
 
 namespace {
 int row_groups_of(const torq_kv_cache_t &cache, int heads) { return (heads / cache.heads + ATT_ROWS - 1) / ATT_ROWS; }
-// Past the cache: rows of whole lines, and more of them than the cache holds
-bool once_of(const torq_kv_cache_t &cache, int64_t B, int width) {
+// Past the cache: rows of whole lines that one workgroup reads, and more of them than the cache holds
+bool once_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
+  if (row_groups_of(cache, heads) > 1) return false;
   const int bytes = cache.format == FMT_BF16 ? 2 : 1;
   const double pages = (double)std::min<int64_t>(cache.pages, B * (int64_t)width);
   return cache.head_dim * bytes % 128 == 0 && 2.0 * pages * cache.page_size * cache.heads * cache.head_dim * bytes > ONE_PASS_WEIGHT_BYTES;
@@ -550,7 +551,7 @@ hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, i
                                   const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths,
                                   int64_t B, float scale, void *out, void *workspace, hipStream_t stream) {
   const Plan plan = plan_of(cache, heads, B, width);
-  const bool f8 = cache.format == FMT_MXFP8, once = once_of(cache, B, width);
+  const bool f8 = cache.format == FMT_MXFP8, once = once_of(cache, heads, B, width);
   if (cache.pages == 0) width = 0;                  // no token has a page: nothing of the cache is touched
   const int page16 = cache.page_size / 16;
   float *const part = (float *)((uintptr_t)workspace + cuts_bytes(plan));
