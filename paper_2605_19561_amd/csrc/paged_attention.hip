@@ -32,7 +32,6 @@ namespace torq {
 constexpr int ATT_TILE = 32;          // tokens of a wave's step
 constexpr int ATT_WAVES = 4;
 constexpr int ATT_ROWS = 16;          // query heads of a workgroup
-constexpr int ATT_GROUPS = 512;       // workgroups, two for each CU
 constexpr int ATT_JOIN = 512;         // threads of a workgroup that joins, at most
 constexpr int ATT_WAYS_ITEMS = 768;  // columns from which each wave has one of its own
 constexpr int ATT_FAR = 0x7FFFFF00;   // an offset past every buffer
@@ -532,9 +531,11 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   p.ways = own || row_groups_of(cache, heads) > 1 ? 1 : ATT_WAVES;
   // Every request within so few tokens that a workgroup each is done before runs would be made out
   p.solo = tiles <= 16;
+  // workgroups: three, two or one for each CU by the registers that a wave takes
+  const int64_t full = cache.head_dim <= 64 ? 768 : cache.head_dim <= 128 ? 512 : 256;
   p.items = B * ((columns + ATT_WAVES / p.ways - 1) / (ATT_WAVES / p.ways));
   const int64_t groups = (p.items * tiles + p.ways - 1) / p.ways;       // a tile at least for each wave, by the longest that the tables hold
-  p.groups = p.solo ? (int)p.items : (int)(groups < 1 ? 1 : groups < ATT_GROUPS ? groups : ATT_GROUPS);
+  p.groups = p.solo ? (int)p.items : (int)(groups < 1 ? 1 : groups < full ? groups : full);
   p.by_item = p.items < p.groups;
   return p;
 }
