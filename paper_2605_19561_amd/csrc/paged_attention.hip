@@ -36,10 +36,10 @@ constexpr int ATT_JOIN = 512;         // threads of a workgroup that joins, at m
 constexpr int ATT_WAYS_ITEMS = 768;  // columns from which each wave has one of its own
 constexpr int ATT_FAR = 0x7FFFFF00;   // an offset past every buffer
 
-// What begins in a run and does not end there: a request, which of the columns that a workgroup works on at a time, in how many runs
-// (0: in none), and the place of the first part; the others are first in their runs.
-struct Cut {
-  int b, columns, parts, place;
+// What begins in a run and does not end there: a request, which of the columns that a workgroup works on at a time, the place of its first
+// part (that of nothing: -1; the others are first in their runs), its last tile, and the runs' lengths.
+struct alignas(16) Cut {
+  int b, column, place, last_tile, each, more;
 };
 
 struct AttentionArgs {
@@ -99,9 +99,8 @@ __device__ __forceinline__ auto buffer_load(__amdgpu_buffer_rsrc_t r, int at) {
   else return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, LOAD_POLICY<ONCE>);
 }
 
-// Tokens of a request, and its tiles.
+// Tokens of a request.
 __device__ __forceinline__ int length_of(const AttentionArgs &a, int n) { return n < 0 ? 0 : n < a.most ? n : (int)a.most; }
-__device__ __forceinline__ int tiles_of(const AttentionArgs &a, int n) { return (length_of(a, n) + ATT_TILE - 1) / ATT_TILE; }
 
 // DP: head_dim rounded up to what the operands hold.  WAYS: 4, the waves take turns at the tiles of a column; 1, each has a column
 // of its own and all of its tiles in the run.
@@ -119,48 +118,57 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   const int columns = (a.kv_heads * a.row_groups + ATT_WAVES / WAYS - 1) / (ATT_WAVES / WAYS), way = WAYS > 1 ? wave : 0;
   const uniform_ints lengths = (uniform_ints)(uintptr_t)a.lengths;
 
-  // one (request, key head, rows), as far as it lies in the run: its tiles first ... last - 1 of `tiles`
+  // one (request, column), as far as it lies in the run: its tiles first ... last - 1 of `tiles`; end: the tile of the run behind it
   struct Segment {
-    int b, before, tiles, length, kv_head, rows_at, first, last, end;      // end: the tile of the run behind it
+    int b, column, tiles, length, kv_head, rows_at, first, last, end;
   };
   const int run = (int)blockIdx.x;
   int run_begin = 0, run_end = 0, tiles_each = 1, tiles_more = 0;
   // (all of it the same in every lane of a wave, which the compiler does not see through the loops: scalar registers)
   auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
   auto place_column = [&](Segment &s, int column) {
-    if constexpr (WAYS == 1) column = column * ATT_WAVES + wave;
-    s.kv_head = uniform(column / a.row_groups), s.rows_at = uniform(column) - s.kv_head * a.row_groups;
+    s.column = uniform(column);
+    column = uniform(WAYS == 1 ? column * ATT_WAVES + wave : column);
+    s.kv_head = a.row_groups == 1 ? column : uniform(column / a.row_groups), s.rows_at = column - s.kv_head * a.row_groups;
     if (s.kv_head >= a.kv_heads) s.kv_head = 0, s.rows_at = a.row_groups;      // (no column: no tile of it is there, and no row)
   };
-  auto segment = [&](int at, int b, int before) {
-    Segment s;
-    at = uniform(at), b = uniform(b), before = uniform(before);
-    for (;; ++b) {
-      s.length = length_of(a, lengths[b]);
-      s.tiles = (s.length + ATT_TILE - 1) / ATT_TILE;
-      if (at < (before + s.tiles) * columns) break;
-      before += s.tiles;
+  auto take_request = [&](Segment &s, int b, int length) {
+    s.b = uniform(b), s.length = uniform(length), s.tiles = (s.length + ATT_TILE - 1) / ATT_TILE;
+  };
+  // the one behind s, which the run goes on with
+  auto behind_of = [&](Segment s) {
+    int column = s.column + 1;
+    if (column == columns) {
+      do take_request(s, s.b + 1, length_of(a, lengths[s.b + 1]));
+      while (s.tiles == 0);
+      column = 0;
     }
-    s.b = b, s.before = before;
-    s.b = uniform(s.b), s.before = uniform(s.before), s.tiles = uniform(s.tiles), s.length = uniform(s.length);
-    before = s.before;
-    const int column = uniform((at - before * columns) / s.tiles), begin = before * columns + column * s.tiles;
     place_column(s, column);
-    s.first = at - begin, s.last = min(run_end - begin, s.tiles), s.end = begin + s.last;
+    s.first = 0, s.last = min(run_end - s.end, s.tiles), s.end += s.last;
     return s;
+  };
+  // requests without tokens: zeros, and nothing to join
+  auto zeros = [&] {
+    for (int b = run; b < a.B; b += gridDim.x)
+      if (length_of(a, lengths[b]) == 0) {
+        if (a.by_item)
+          for (int x = tid; x < columns; x += 256) a.cuts[b * columns + x] = Cut{0, 0, -1, 0, 1, 0};
+        for (int x = tid; x < a.kv_heads * a.group * a.dim / 8; x += 256)
+          reinterpret_cast<u32x4 *>(a.out + (int64_t)b * a.kv_heads * a.group * a.dim)[x] = u32x4{0, 0, 0, 0};
+      }
   };
   Segment seg;
   if (a.solo) {
     const int b = blockIdx.x / columns, column = blockIdx.x - b * columns;
     const int length = length_of(a, lengths[b]), tiles = (length + ATT_TILE - 1) / ATT_TILE;
-    seg = Segment{b, 0, tiles, length, 0, 0, 0, tiles, 0};
+    seg = Segment{b, 0, tiles, length, 0, 0, 0, tiles, 0};      // (end: that of no run)
     place_column(seg, column);
   } else {
     // tiles of one column, request by request: every wave adds them up, a lane `per` of them
     const int per = (a.B + 63) / 64;
-    int mine = 0;
+    int mine = 0, length = 0;
     for (int i = 0; i < per; ++i)
-      if (lane * per + i < a.B) mine += tiles_of(a, a.lengths[lane * per + i]);
+      if (lane * per + i < a.B) length = length_of(a, a.lengths[lane * per + i]), mine += (length + ATT_TILE - 1) / ATT_TILE;
     int sum = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -168,23 +176,25 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       if (lane >= o) sum += up;
     }
     const int total = __builtin_amdgcn_readlane(sum, 63);
-    // zeros for requests without tokens
-    for (int b = run; b < a.B; b += gridDim.x)
-      if (lengths[b] <= 0 || a.most == 0) {
-        if (a.by_item)
-          for (int x = tid; x < columns; x += 256) a.cuts[b * columns + x] = Cut{0, 0, 0, 0};
-        for (int x = tid; x < a.kv_heads * a.group * a.dim / 8; x += 256)
-          reinterpret_cast<u32x4 *>(a.out + (int64_t)b * a.kv_heads * a.group * a.dim)[x] = u32x4{0, 0, 0, 0};
-      }
     const Runs runs(total * columns, gridDim.x, WAYS);
     run_begin = uniform(runs.begin(min(run, runs.runs))), run_end = uniform(runs.begin(min(run + 1, runs.runs)));
     if (run_begin == run_end) {                     // (fewer tiles than workgroups)
-      if (tid == 0 && !a.by_item) a.cuts[run] = Cut{0, 0, 0, 0};
+      if (tid == 0 && !a.by_item) a.cuts[run] = Cut{0, 0, -1, 0, 1, 0};
+      zeros();
       return;
     }
-    // the lane whose requests the run begins in
+    // the lane whose requests the run begins in, and the request
     const int owner = __builtin_ctzll(__ballot(run_begin < sum * columns));
-    seg = segment(run_begin, owner * per, __builtin_amdgcn_readlane(sum - mine, owner));
+    int before = __builtin_amdgcn_readlane(sum - mine, owner), b = owner * per;
+    take_request(seg, b, per == 1 ? __builtin_amdgcn_readlane(length, owner) : length_of(a, lengths[b]));
+    while (run_begin >= (before + seg.tiles) * columns) {
+      before += seg.tiles;
+      take_request(seg, seg.b + 1, length_of(a, lengths[seg.b + 1]));
+    }
+    const int into = run_begin - before * columns, column = uniform(into / seg.tiles);
+    place_column(seg, column);
+    seg.first = into - column * seg.tiles, seg.last = min(run_end - run_begin + seg.first, seg.tiles);
+    seg.end = run_begin + seg.last - seg.first;
     tiles_each = uniform(runs.each), tiles_more = uniform(runs.more);
   }
 
@@ -286,18 +296,19 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   load_k(here);
   __builtin_amdgcn_sched_barrier(0);
   load_v(here);
+  if (!a.solo) zeros();
   for (;;) {
     const bool whole = seg.first == 0 && seg.last == seg.tiles;
     if (!a.solo && tid == 0 && (a.by_item ? seg.first == 0 : seg.end == run_end)) {
-      const int begin = seg.end - seg.last, column = (begin - seg.before * columns) / seg.tiles;
-      const int parts = seg.first == 0 && !whole ? Runs(tiles_each, tiles_more).of(begin + seg.tiles - 1) - run + 1 : 0;
-      a.cuts[a.by_item ? seg.b * columns + column : run] = Cut{seg.b, column, parts, 2 * run + (run_begin < begin)};
+      const int begin = seg.end - seg.last;
+      a.cuts[a.by_item ? seg.b * columns + seg.column : run] = Cut{
+          seg.b, seg.column, seg.first == 0 && !whole ? 2 * run + (run_begin < begin) : -1, begin + seg.tiles - 1, tiles_each, tiles_more};
     }
     // what comes behind this segment: its first tile is on the way when this one's last is worked on
     const bool more = seg.end < run_end;
     Segment behind = seg;
     behind.last = 0;                                // (no tile of it is there)
-    if (more) behind = segment(seg.end, seg.b, seg.before);
+    if (more) behind = behind_of(seg);
     Pages pages_behind = look_up(behind, behind.first + way);
     pages = look_up(seg, seg.first + way + WAYS);
     f32x4 o[NH * E];
@@ -310,6 +321,9 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       __builtin_amdgcn_sched_barrier(0);
       load_v(here);
     }
+    // Q is there from here on: a wait for it inside the loop would be one for all loads, in every round
+#pragma unroll
+    for (int t = 0; t < KS; ++t) asm volatile("" : "+v"(q[t]));
     for (int tile = seg.first + way; tile < seg.last; tile += WAYS) {
       Place next;
       if (tile + WAYS < seg.last) next = place(seg, tile + WAYS, pages);
@@ -471,17 +485,18 @@ __global__ void __launch_bounds__(ATT_JOIN) paged_attention_join_kernel(Attentio
   __shared__ f32x4 values[ATT_JOIN];
   __shared__ float m_all[ATT_JOIN], l_all[ATT_JOIN];
   const Cut cut = a.cuts[blockIdx.x];
-  if (cut.parts == 0) return;
+  if (cut.place < 0) return;
+  const int parts = Runs(cut.each, cut.more).of(cut.last_tile) - cut.place / 2 + 1;
   const int tid = threadIdx.x, quads = a.dim / 4, rows = min(ATT_ROWS, a.group);
   const int all = together * rows * quads, here = min(all, many), ways = blockDim.x / here, way = tid / here;
   const int x = blockIdx.y * many + (tid - way * here), c = x % quads, r = x / quads % rows, w = x / quads / rows;
-  const int column = cut.columns * together + w, kv_head = column / a.row_groups, row = (column - kv_head * a.row_groups) * ATT_ROWS + r;
+  const int column = cut.column * together + w, kv_head = column / a.row_groups, row = (column - kv_head * a.row_groups) * ATT_ROWS + r;
   const bool real = x < all && way < ways && row < a.group && kv_head < a.kv_heads;
   float m = -INFINITY, l = 0.0f;
   f32x4 v = {0, 0, 0, 0};
   if (real) {
 #pragma unroll 4
-    for (int i = way; i < cut.parts; i += ways) {
+    for (int i = way; i < parts; i += ways) {
       const int64_t at = ((int64_t)(i ? (cut.place / 2 + i) * 2 : cut.place) * together + w) * ATT_ROWS + r;
       const float mi = a.part_ml[2 * at], li = a.part_ml[2 * at + 1];
       const f32x4 vi = *reinterpret_cast<const f32x4 *>(a.part + at * a.dim + 4 * c);
