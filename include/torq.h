@@ -313,8 +313,8 @@ int torq_cache_append(const torq_kv_cache_t *cache, const void *key_bf16, int64_
  *   out[b][h] = sum_t p_t v_t,  p = softmax over t < lengths[b] of scale * q[b][h] . k_t,
  * k_t, v_t: position t of request b under key head h / (heads / cache->heads).  A request without tokens: zeros.
  *   q_bf16        [B][heads][head_dim], strides in elements, multiples of 8, not negative; heads a multiple of cache->heads
- *   block_tables  as torq_block_tables leaves them, width * page_size at most 2^30, and B * width * page_size *
- *                 cache->heads * ceil(heads / cache->heads / 16) below 2^35.  A position past `width` pages counts as past the length; tokens of
+ *   block_tables  as torq_block_tables leaves them, width * page_size at most 2^30, and B * cache->heads *
+ *                 ceil(heads / cache->heads / 16) * (width * page_size / 32 + 8) below 2^31.  A position past `width` pages counts as past the length; tokens of
  *                 a page outside [0, pages) are left out.  What lies in a page behind the length is not used, NaN or not.
  *   out_bf16      [B][heads][head_dim], contiguous
  *   workspace     16-byte aligned, torq_paged_attention_workspace_bytes() of the same sizes; contents do not matter

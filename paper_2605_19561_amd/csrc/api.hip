@@ -864,7 +864,7 @@ inline bool bad_stride(int64_t stride) { return stride < 0 || stride % 8; }
 bool attention_sizes(const torq_kv_cache_t *c, int heads, int64_t B, int width) {
   if (heads <= 0 || heads % c->heads || heads > (1 << 20) || B < 0 || width < 0 || B > 0x7FFFFFFF / heads) return false;
   const int64_t most = (int64_t)width * c->page_size, columns = B * c->heads * ((heads / c->heads + 15) / 16);
-  return most <= (int64_t)1 << 30 && columns <= 0x7FFFFFFF / (most / 32 + 1);
+  return most <= (int64_t)1 << 30 && columns <= 0x7FFFFFFF / (most / 32 + 8);
 }
 
 }  // namespace

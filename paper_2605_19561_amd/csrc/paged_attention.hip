@@ -3,11 +3,14 @@
 // The query heads of a key head are the columns of one matrix product, up to 16 at a time, so K and V are read once for all of
 // them: HBM-bound, 2 (bf16) or 1 1/32 (MXFP8) bytes for 2 heads / kv_heads flops.
 //
-// Work: the tokens of every (request, key head) in tiles of 32, all of them in one row of tiles, cut into equal runs, one for each
-// workgroup: lengths may be as ragged as they like, and the host need not know them (every workgroup adds them up itself).  A run goes through one or
-// several (request, key head)s.  The four waves of a workgroup take turns at the tiles, each with a softmax of its own in one pass (running
-// maximum m, sum l, unnormalised O), put together in LDS at the end of a (request, key head).  What lies whole within a run is written as output, the
-// others' O, m and l go to the workspace, two at most for a run, and a second kernel joins them in the order of the tokens.
+// Work: the tokens of every (request, key head) in tiles of 32, all of them in one row of tiles (with room for what each one costs
+// besides), cut into equal runs, one for each workgroup: lengths may be as ragged as they like, and the host need not know them, since every
+// workgroup adds them up itself.  A run goes through one or several (request, key head)s.  The four waves of a workgroup take turns at
+// the tiles of one, each with a softmax of its own in one pass (running maximum m, sum l, unnormalised O), put together in LDS at its end; or
+// (few query heads for a key head and many of those, or more than 16 query heads, whose waves then find the same lines in the cache)
+// each has one for itself and they need not wait for one another.  What lies whole within a run is written as output; of the others
+// O, m and l go to the workspace, two at most for a run (and wave), and a second kernel joins them in the order of the tokens.  Tables for
+// at most 512 tokens: one launch, a workgroup for each (request, key head).
 //
 // A tile goes through the matrix cores transposed, and nothing of it passes between lanes but the column maxima:
 //   S^T [token][head] = K [token][i] Q^T [i][head]           v_mfma_f32_16x16x32_bf16, two groups of 16 tokens
@@ -34,6 +37,10 @@ constexpr int ATT_WAVES = 4;
 constexpr int ATT_ROWS = 16;          // query heads of a workgroup
 constexpr int ATT_JOIN = 512;         // threads of a workgroup that joins, at most
 constexpr int ATT_WAYS_ITEMS = 768;  // columns from which each wave has one of its own
+// What a (request, key head) costs besides its tiles (its place, its query, putting it together), in tiles of the row of them that is cut
+// into runs, by the waves that take turns.  64 requests of 1 to 600 tokens, 64 / 8 heads, with 0, 4, 8, 16: 35.4, 24.1, 23.9, 23.7 us;
+// 16 of 1000 to 8192 58.6, 58.7, 59.1, 60.4; 77 x 20 heads, a wave each, with 0, 1, 2, 5: 89.6, 89.8, 92.8, 95.0.
+constexpr int att_setup(int ways) { return ways > 1 ? 4 : 1; }
 constexpr int ATT_FAR = 0x7FFFFF00;   // an offset past every buffer
 
 // What begins in a run and does not end there: a request, which of the columns that a workgroup works on at a time, the place of its first
@@ -118,7 +125,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   const int columns = (a.kv_heads * a.row_groups + ATT_WAVES / WAYS - 1) / (ATT_WAVES / WAYS), way = WAYS > 1 ? wave : 0;
   const uniform_ints lengths = (uniform_ints)(uintptr_t)a.lengths;
 
-  // one (request, column), as far as it lies in the run: its tiles first ... last - 1 of `tiles`; end: the tile of the run behind it
+  // one (request, column), as far as it lies in the run: its tiles first ... last - 1 of `tiles`; end: the place behind them
   struct Segment {
     int b, column, tiles, length, kv_head, rows_at, first, last, end;
   };
@@ -135,6 +142,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   auto take_request = [&](Segment &s, int b, int length) {
     s.b = uniform(b), s.length = uniform(length), s.tiles = (s.length + ATT_TILE - 1) / ATT_TILE;
   };
+  auto places_of = [](int tiles) { return tiles ? tiles + att_setup(WAYS) : 0; };
   // the one behind s, which the run goes on with
   auto behind_of = [&](Segment s) {
     int column = s.column + 1;
@@ -144,6 +152,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       column = 0;
     }
     place_column(s, column);
+    s.end += att_setup(WAYS);
     s.first = 0, s.last = min(run_end - s.end, s.tiles), s.end += s.last;
     return s;
   };
@@ -168,7 +177,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
     const int per = (a.B + 63) / 64;
     int mine = 0, length = 0;
     for (int i = 0; i < per; ++i)
-      if (lane * per + i < a.B) length = length_of(a, a.lengths[lane * per + i]), mine += (length + ATT_TILE - 1) / ATT_TILE;
+      if (lane * per + i < a.B) length = length_of(a, a.lengths[lane * per + i]), mine += places_of((length + ATT_TILE - 1) / ATT_TILE);
     int sum = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -187,14 +196,20 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
     const int owner = __builtin_ctzll(__ballot(run_begin < sum * columns));
     int before = __builtin_amdgcn_readlane(sum - mine, owner), b = owner * per;
     take_request(seg, b, per == 1 ? __builtin_amdgcn_readlane(length, owner) : length_of(a, lengths[b]));
-    while (run_begin >= (before + seg.tiles) * columns) {
-      before += seg.tiles;
+    while (run_begin >= (before + places_of(seg.tiles)) * columns) {
+      before += places_of(seg.tiles);
       take_request(seg, seg.b + 1, length_of(a, lengths[seg.b + 1]));
     }
-    const int into = run_begin - before * columns, column = uniform(into / seg.tiles);
+    const int into = run_begin - before * columns, column = uniform(into / places_of(seg.tiles));
     place_column(seg, column);
-    seg.first = into - column * seg.tiles, seg.last = min(run_end - run_begin + seg.first, seg.tiles);
-    seg.end = run_begin + seg.last - seg.first;
+    // tile t of a column has the place att_setup + t from its beginning
+    const int tile0 = run_begin - into + column * places_of(seg.tiles) + att_setup(WAYS);
+    seg.first = max(run_begin - tile0, 0), seg.last = min(run_end - tile0, seg.tiles), seg.end = tile0 + seg.last;
+    if (seg.last <= 0) {                            // (the run ends ahead of the first tile)
+      if (tid == 0 && !a.by_item) a.cuts[run] = Cut{0, 0, -1, 0, 1, 0};
+      zeros();
+      return;
+    }
     tiles_each = uniform(runs.each), tiles_more = uniform(runs.more);
   }
 
@@ -297,18 +312,17 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   __builtin_amdgcn_sched_barrier(0);
   load_v(here);
   if (!a.solo) zeros();
-  for (;;) {
+  for (int second = 0;; second = 1) {               // second: the run's second segment, or a later one
     const bool whole = seg.first == 0 && seg.last == seg.tiles;
-    if (!a.solo && tid == 0 && (a.by_item ? seg.first == 0 : seg.end == run_end)) {
-      const int begin = seg.end - seg.last;
-      a.cuts[a.by_item ? seg.b * columns + seg.column : run] = Cut{
-          seg.b, seg.column, seg.first == 0 && !whole ? 2 * run + (run_begin < begin) : -1, begin + seg.tiles - 1, tiles_each, tiles_more};
-    }
     // what comes behind this segment: its first tile is on the way when this one's last is worked on
-    const bool more = seg.end < run_end;
     Segment behind = seg;
     behind.last = 0;                                // (no tile of it is there)
-    if (more) behind = behind_of(seg);
+    if (seg.end < run_end) behind = behind_of(seg);
+    const bool more = behind.last > 0;
+    if (!a.solo && tid == 0 && (a.by_item ? seg.first == 0 : !more)) {
+      a.cuts[a.by_item ? seg.b * columns + seg.column : run] = Cut{
+          seg.b, seg.column, seg.first == 0 && !whole ? 2 * run + second : -1, seg.end - seg.last + seg.tiles - 1, tiles_each, tiles_more};
+    }
     Pages pages_behind = look_up(behind, behind.first + way);
     pages = look_up(seg, seg.first + way + WAYS);
     f32x4 o[NH * E];
@@ -411,8 +425,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
     l += __shfl_xor(l, 32);
     const int rows = min(ATT_ROWS, a.group - seg.rows_at * ATT_ROWS);
     uint16_t *const out = a.out + ((int64_t)seg.b * a.kv_heads * a.group + seg.kv_head * a.group + seg.rows_at * ATT_ROWS) * a.dim;
-    // where the run begins within a column: its first place in the workspace, else its second
-    const int64_t part = ((int64_t)(run * 2 + (seg.end - (seg.last - seg.first) == run_begin ? 0 : 1)) * (ATT_WAVES / WAYS) +
+    const int64_t part = ((int64_t)(run * 2 + second) * (ATT_WAVES / WAYS) +
                           (WAYS == 1 ? wave : 0)) * ATT_ROWS;
     // lane (n, g), o[h E + j][r] = O[head n][16 E h + E (4 g + r) + j]
     if constexpr (WAYS == 1) {
@@ -549,7 +562,7 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   // workgroups: three, two or one for each CU by the registers that a wave takes
   const int64_t full = cache.head_dim <= 64 ? 768 : cache.head_dim <= 128 ? 512 : 256;
   p.items = B * ((columns + ATT_WAVES / p.ways - 1) / (ATT_WAVES / p.ways));
-  const int64_t groups = (p.items * tiles + p.ways - 1) / p.ways;       // a tile at least for each wave, by the longest that the tables hold
+  const int64_t groups = (p.items * (tiles + att_setup(p.ways)) + p.ways - 1) / p.ways;      // by the longest that the tables hold
   p.groups = p.solo ? (int)p.items : (int)(groups < 1 ? 1 : groups < full ? groups : full);
   p.by_item = p.items < p.groups;
   return p;
