@@ -52,8 +52,8 @@ struct alignas(16) Cut {
 struct AttentionArgs {
   const char *k, *v;
   const uint8_t *k_scales, *v_scales;
-  int64_t pages, page_stride, head_stride;
-  int token_bytes;                    // from a token to the next
+  int64_t page_bytes, head_bytes;     // from one to the next
+  int pages, token_bytes;
   const uint16_t *q;
   int64_t q_stride, q_head_stride;
   const int *tables, *lengths;
@@ -228,17 +228,18 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       q[t] = as_bf16(v);
     }
   };
-  // the pages of a tile's two groups of 16 tokens; how many of a group are tokens; where they lie, in bytes
+  // the pages of a tile's two groups of 16 tokens, and where in them the groups begin; how many of a group are tokens; where they lie, in bytes
   struct Pages {
-    int page[2];
+    int page[2], in_page[2];
   };
   auto look_up = [&](const Segment &s, int tile) {
     Pages p;
     const uniform_ints table = (uniform_ints)(uintptr_t)(a.tables + s.b * a.table_stride);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int t16 = min(2 * tile + u, (s.length - 1) / 16);
-      p.page[u] = t16 >= 0 && s.length > 0 ? table[(int)((uint64_t)t16 * (uint64_t)a.page16_magic >> 38)] : -1;
+      const int t16 = max(min(2 * tile + u, (s.length - 1) / 16), 0), entry = (int)((uint64_t)(uint32_t)t16 * (uint64_t)a.page16_magic >> 38);
+      p.page[u] = s.length > 0 ? table[entry] : -1;
+      p.in_page[u] = 16 * (t16 - entry * (a.page_size / 16));
     }
     return p;
   };
@@ -250,11 +251,11 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
     Place w;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int t = tile * ATT_TILE + 16 * u, t16 = 2 * tile + u;
-      const int in_page = (t16 - (int)((uint64_t)t16 * (uint64_t)a.page16_magic >> 38) * (a.page_size / 16)) * 16;
-      const bool there = tile < s.last && t < s.length && s.rows_at < a.row_groups && p.page[u] >= 0 && p.page[u] < a.pages;
-      w.count[u] = there ? min(s.length - t, 16) : 0;
-      w.at[u] = ((there ? p.page[u] : 0) * a.page_stride + s.kv_head * a.head_stride) * BYTES + (int64_t)in_page * a.token_bytes;
+      const int t = tile * ATT_TILE + 16 * u;
+      // (a page that is none: as a number without a sign past all others)
+      const int left = tile < s.last && (uint32_t)p.page[u] < (uint32_t)a.pages && s.rows_at < a.row_groups ? s.length - t : 0;
+      w.count[u] = max(min(left, 16), 0);
+      w.at[u] = (left > 0 ? p.page[u] : 0) * a.page_bytes + (s.kv_head * a.head_bytes + (int64_t)(p.in_page[u] * a.token_bytes));
     }
     return w;
   };
@@ -266,7 +267,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   };
   u32x4 k[2][KL];
   uint32_t v[2][NH][4][E * BYTES / 4];
-  uint32_t k_scales[2][KL], v_scales[2][NH][4];
+  uint8_t k_scales[2][KL], v_scales[2][NH][4];
   auto load_k = [&](const Place &p) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
 #pragma unroll
         for (int s = 0; s < KL; ++s) {
           if constexpr (F8) {
-            const float scale = __uint_as_float(k_scales[u][s] << 23);
+            const float scale = __uint_as_float((uint32_t)k_scales[u][s] << 23);
             uint32_t w[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) widen4(k[u][s][e], scale, w[2 * e], w[2 * e + 1]);
@@ -399,7 +400,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           if constexpr (F8) {
-            const float scale = __uint_as_float(v_scales[e / 4][h][e % 4] << 23);
+            const float scale = __uint_as_float((uint32_t)v_scales[e / 4][h][e % 4] << 23);
 #pragma unroll
             for (int c = 0; c < E / 4; ++c) widen4(v[e / 4][h][e % 4][c], scale, w[e][2 * c], w[e][2 * c + 1]);
           } else {
@@ -582,10 +583,10 @@ hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, i
   const Plan plan = plan_of(cache, heads, B, width);
   const bool f8 = cache.format == FMT_MXFP8, once = once_of(cache, heads, B, width);
   if (cache.pages == 0) width = 0;                  // no token has a page: nothing of the cache is touched
-  const int page16 = cache.page_size / 16;
+  const int page16 = cache.page_size / 16, bytes = f8 ? 1 : 2;
   float *const part = (float *)((uintptr_t)workspace + cuts_bytes(plan));
-  AttentionArgs a{(const char *)cache.k, (const char *)cache.v, cache.k_scales, cache.v_scales, cache.pages, cache.page_stride,
-                  cache.head_stride, (int)cache.token_stride * (f8 ? 1 : 2), (const uint16_t *)q, q_stride,
+  AttentionArgs a{(const char *)cache.k, (const char *)cache.v, cache.k_scales, cache.v_scales, cache.page_stride * bytes,
+                  cache.head_stride * bytes, (int)cache.pages, (int)cache.token_stride * bytes, (const uint16_t *)q, q_stride,
                   q_head_stride, block_tables, lengths, table_stride, ((int64_t)1 << 38) / page16 + 1,
                   (int64_t)width * cache.page_size, (int)B, cache.page_size, cache.heads, heads / cache.heads, row_groups_of(cache, heads),
                   cache.head_dim, plan.solo, scale * 1.44269504088896340736f, (uint16_t *)out, part, part + part_rows(plan) * cache.head_dim,
