@@ -597,7 +597,12 @@ hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, i
     constexpr bool F8 = decltype(of8)::value, ONCE = decltype(hint)::value;
     plan.ways > 1 ? go(paged_attention_kernel<DP, F8, ONCE, ATT_WAVES>) : go(paged_attention_kernel<DP, F8, ONCE, 1>);
   };
-  auto of_format = [&](auto dp, auto of8) { once ? of_hint(dp, of8, std::true_type{}) : of_hint(dp, of8, std::false_type{}); };
+  auto of_format = [&](auto dp, auto of8) {
+    // (rows of up to 64 bytes never go past the cache)
+    if constexpr (!(decltype(of8)::value && decltype(dp)::value == 64))
+      if (once) return of_hint(dp, of8, std::true_type{});
+    of_hint(dp, of8, std::false_type{});
+  };
   auto of_dim = [&](auto dp) { f8 ? of_format(dp, std::true_type{}) : of_format(dp, std::false_type{}); };
   if (cache.head_dim <= 64) of_dim(std::integral_constant<int, 64>{});
   else if (cache.head_dim <= 128) of_dim(std::integral_constant<int, 128>{});

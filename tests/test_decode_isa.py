@@ -7,7 +7,8 @@ import pytest
 
 from paper_2605_19561_amd import build
 
-KERNELS = [(dp, f8, once, ways) for dp in (64, 128, 256) for f8 in (0, 1) for once in (0, 1) for ways in (1, 4)]
+# (rows of up to 64 bytes never go past the cache)
+KERNELS = [(dp, f8, once, ways) for dp in (64, 128, 256) for f8 in (0, 1) for once in (0, 1) for ways in (1, 4) if not (dp == 64 and f8 and once)]
 
 
 @pytest.fixture(scope="module")

@@ -375,6 +375,50 @@ def test_paged_attention_of_a_large_batch(tq, heads, kv_heads, dim, fmt, layout,
 
 
 @gpu
+@pytest.mark.parametrize("long", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,dim,fmt", [(8, 8, 64, "bf16"), (16, 2, 64, "bf16"), (8, 8, 128, "bf16"), (16, 2, 128, "bf16"), (8, 8, 128, "mxfp8"),
+                                                    (16, 2, 128, "mxfp8"), (4, 4, 256, "bf16"), (16, 2, 256, "bf16"), (4, 4, 256, "mxfp8"), (16, 2, 256, "mxfp8")])
+def test_paged_attention_past_the_cache(tq, heads, kv_heads, dim, fmt, long):
+    # tables that could name more than 96 MiB of whole lines: read with the non-temporal hint, however little there is
+    B = 200 if heads == kv_heads else 3
+    g = np.random.default_rng(dim)
+    lengths = [int(n) for n in g.integers(0, 120, B)]
+    lengths[0], lengths[2] = 0, 450
+    cache, q, tables, lens, pages = attention_case(tq, B, heads, kv_heads, dim, 16, lengths, fmt, "heads", 8)
+    want = attention_reference(q, values_of(cache, "k"), values_of(cache, "v"), tables, lens, dim ** -0.5, pages)
+    # the same pages at the front of a large pool
+    size = (1 if fmt == "mxfp8" else 2) * kv_heads * 16 * dim
+    pool = 60 * 2 ** 20 // size
+    parts = []
+    for n in ("k", "v") + (("k_scales", "v_scales") if fmt == "mxfp8" else ()):
+        t = getattr(cache, n)
+        big = torch.empty((pool, *t.shape[1:]), dtype=torch.uint8 if fmt == "mxfp8" else BF, device=DEV)
+        big[:pages] = t.view(torch.uint8) if fmt == "mxfp8" else t
+        parts.append(big.view(t.dtype))
+    if long or B < 200:                              # (else 32 pages a request, one launch; B requests of them are enough)
+        tables = torch.cat([tables, torch.full((B, 40000), -1, dtype=torch.int32)], 1)
+    big = tq.KVCache(*parts)
+    check_attention(tq.torq_paged_attention(q.to(DEV), big, tables.to(DEV), lens.to(DEV), dim ** -0.5), *want)
+
+
+@gpu
+@pytest.mark.parametrize("native", [True, False])
+def test_decode_calls_without_requests_or_tokens(tq, native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(binding, "_host", binding._Interpreted)
+    cache = make_cache(tq, 2, 2, 16, 64, "bf16", "heads")
+    before = u8(cache.k).copy()
+    none = torch.empty((0, 2, 64), dtype=BF, device=DEV)
+    tq.torq_cache_append(cache, none, none, torch.empty(0, dtype=torch.int64, device=DEV))
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=DEV)
+    assert np.array_equal(u8(cache.k), before)
+    assert tq.torq_paged_attention(none, cache, i32(0, 3), i32(0), 1.0).shape == (0, 2, 64)
+    slots, cursor = tq.torq_block_tables(i32(0), i32(0), i32(0), i32(1), i32(0, 0), 16, 3)
+    assert slots.tolist() == [-1] * 3 and cursor.tolist() == [0]
+    assert tq.torq_add_rms_norm(none[:, 0].contiguous(), none[:, 0].contiguous(), torch.ones(64, dtype=BF, device=DEV), 1e-5, tq.TORQ_FMT_MXFP8)[1].shape == (0, 2)
+
+
+@gpu
 def test_paged_attention_with_one_weight_near_one(tq):
     # scores of hundreds: maxima that move from tile to tile, weights that underflow
     cache, q, tables, lens, pages = attention_case(tq, 3, 8, 2, 128, 16, [500, 64, 1], "bf16", "heads", 3, spread=6.0)
