@@ -106,6 +106,16 @@ __device__ __forceinline__ auto buffer_load(__amdgpu_buffer_rsrc_t r, int at) {
   else return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, LOAD_POLICY<ONCE>);
 }
 
+// Over the four lanes l, l ^ 16, l ^ 32, l ^ 48 of a column: the rows of 16 lanes (then the halves of the wave) of a register with itself
+// exchanged, so that each lane has its own and the other's
+template <class F>
+__device__ __forceinline__ float over_column(float v, F &&op) {
+  const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = op(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
+  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+}
+
 // Tokens of a request.
 __device__ __forceinline__ int length_of(const AttentionArgs &a, int n) { return n < 0 ? 0 : n < a.most ? n : (int)a.most; }
 
@@ -369,8 +379,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
         p[e] = 4 * g + e % 4 < here.count[e / 4] ? st[e / 4][e % 4] * a.scale_log2 : -INFINITY;
         m_new = fmaxf(m_new, p[e]);
       }
-      m_new = fmaxf(m_new, __shfl_xor(m_new, 16));
-      m_new = fmaxf(m_new, __shfl_xor(m_new, 32));
+      m_new = over_column(m_new, [](float x, float y) { return fmaxf(x, y); });
       // (nothing but masked tokens so far: everything below is 0)
       const float base = m_new == -INFINITY ? 0.0f : m_new;
       const float alpha = __builtin_amdgcn_exp2f(m - base);
@@ -422,8 +431,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       here = next;
     }
     // The lanes of a column hold the sums of their own tokens.
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    l = over_column(l, [](float x, float y) { return x + y; });
     const int rows = min(ATT_ROWS, a.group - seg.rows_at * ATT_ROWS);
     uint16_t *const out = a.out + ((int64_t)seg.b * a.kv_heads * a.group + seg.kv_head * a.group + seg.rows_at * ATT_ROWS) * a.dim;
     const int64_t part = ((int64_t)(run * 2 + second) * (ATT_WAVES / WAYS) +
