@@ -113,7 +113,7 @@ struct Unlocked {
 };
 
 Tensor given_or_new(const Tensor *given, const Tensor &like, at::IntArrayRef sizes, at::ScalarType type) {
-  return given ? *given : like.new_empty(sizes, like.options().dtype(type));
+  return given ? *given : at::empty(sizes, like.options().dtype(type));
 }
 Tensor scratch(const Tensor *given, const Tensor &like, int64_t bytes, const std::optional<c10::Stream> &user) {
   if (given) return *given;
