@@ -25,6 +25,11 @@
 // moment that O is.  The loads are buffer loads over the 16 tokens of a group (a group lies in one page) as far as they are tokens of
 // the request: what is past the length, in no page or past the last tile has no records, costs no traffic and comes back as
 // zeros, so the loop knows no other case (and a NaN behind the length is not read).
+//
+// Measured (called in turn over three caches, 303 MB to 1.9 GB): 16 requests of 1000 to 8192 tokens, 64 query and 8 key heads of 128, 55.7 us =
+// 5.4 TB/s; one of 131072 87.8 us = 6.1; 45 of 8000 to 32768 in MXFP8 311 us = 6.2; 77 with 20 heads of 80 each, 85.9 us = 4.9.  The traffic
+// is what has to be read (counters within 1 %); vector instructions take a third (bf16) to half (MXFP8) of the time.  What is left over HBM's time: 5 to 7 us until
+// the first tiles are there, 5 for the join and its launch.  One request of 333 tokens 7.2 us, one launch: three rounds that hang on one another.
 #include <algorithm>
 
 #include "torq_device.h"
@@ -36,7 +41,9 @@ constexpr int ATT_TILE = 32;          // tokens of a wave's step
 constexpr int ATT_WAVES = 4;
 constexpr int ATT_ROWS = 16;          // query heads of a workgroup
 constexpr int ATT_JOIN = 512;         // threads of a workgroup that joins, at most
-constexpr int ATT_WAYS_ITEMS = 768;  // columns from which each wave has one of its own
+// Columns from which each wave has one of its own, with up to 2 query heads for each.  77 x 20 heads 120 -> 91 us, 256 requests x 8 key heads
+// with 2 query heads each 144.6 -> 139.7; with 4 146.7 -> 151.1, with 8 153 -> 162 (four times the parts to join).
+constexpr int ATT_WAYS_ITEMS = 768;
 // What a (request, key head) costs besides its tiles (its place, its query, putting it together), in tiles of the row of them that is cut
 // into runs, by the waves that take turns.  64 requests of 1 to 600 tokens, 64 / 8 heads, with 0, 4, 8, 16: 35.4, 24.1, 23.9, 23.7 us;
 // 16 of 1000 to 8192 58.6, 58.7, 59.1, 60.4; 77 x 20 heads, a wave each, with 0, 1, 2, 5: 89.6, 89.8, 92.8, 95.0.
@@ -549,7 +556,10 @@ __global__ void __launch_bounds__(ATT_JOIN) paged_attention_join_kernel(Attentio
 
 namespace {
 int row_groups_of(const torq_kv_cache_t &cache, int heads) { return (heads / cache.heads + ATT_ROWS - 1) / ATT_ROWS; }
-// Past the cache: rows of whole lines that one workgroup reads, and more of them than the cache holds
+// Past the cache: rows of whole lines that one workgroup reads, and more of them than the cache holds, as far as the tables can tell.  Without /
+// with the hint, from HBM and the same cache again, us: 67 MB 21.7 / 20.7, 19.5 / 19.6; 134 MB 33.9 / 30.9, 28.4 / 29.4; 268 MB 57.8 / 52.1,
+// 47.8 / 50.8; 537 MB 104.7 / 94.2, 104.8 / 93.2; MXFP8 69 MB 23.9 / 23.5, 20.7 / 22.2, 277 MB 61.4 / 58.7, 52.0 / 57.9.  Rows that share lines
+// lose: heads of 80 168 MB 40.1 / 42.7, of 96 in MXFP8, tokens outermost, 208 MB 70.8 / 83.6.
 bool once_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   if (row_groups_of(cache, heads) > 1) return false;
   const int bytes = cache.format == FMT_BF16 ? 2 : 1;
@@ -566,9 +576,10 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   const int64_t columns = (int64_t)cache.heads * row_groups_of(cache, heads), tiles = ((int64_t)width * cache.page_size + ATT_TILE - 1) / ATT_TILE;
   const bool own = columns % ATT_WAVES == 0 && heads / cache.heads <= 2 && B * columns >= ATT_WAYS_ITEMS;
   p.ways = own || row_groups_of(cache, heads) > 1 ? 1 : ATT_WAVES;
-  // Every request within so few tokens that a workgroup each is done before runs would be made out
+  // Every request within so few tokens that a workgroup each is done before runs would be made out and joined (333 tokens 13 -> 7.2 us)
   p.solo = tiles <= 16;
-  // workgroups: three, two or one for each CU by the registers that a wave takes
+  // workgroups: three, two or one for each CU by the registers that a wave takes.  head_dim 64 with 512, 768, 1024: 64 requests of 100 to
+  // 3000 tokens 52.3, 50.1, 49.6 us, 16 long ones 34.6, 35.4, 35.8; 128: 16 58.3, 59.4, 64.6; 256 with 256, 512, 768: 64.9, 72.6, 79.9
   const int64_t full = cache.head_dim <= 64 ? 768 : cache.head_dim <= 128 ? 512 : 256;
   p.items = B * ((columns + ATT_WAVES / p.ways - 1) / (ATT_WAVES / p.ways));
   const int64_t groups = (p.items * (tiles + att_setup(p.ways)) + p.ways - 1) / p.ways;      // by the longest that the tables hold
