@@ -574,10 +574,13 @@ struct Plan {
 Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   Plan p;
   const int64_t columns = (int64_t)cache.heads * row_groups_of(cache, heads), tiles = ((int64_t)width * cache.page_size + ATT_TILE - 1) / ATT_TILE;
-  const bool own = columns % ATT_WAVES == 0 && heads / cache.heads <= 2 && B * columns >= ATT_WAYS_ITEMS;
-  p.ways = own || row_groups_of(cache, heads) > 1 ? 1 : ATT_WAVES;
   // Every request within so few tokens that a workgroup each is done before runs would be made out and joined (333 tokens 13 -> 7.2 us)
   p.solo = tiles <= 16;
+  bool own;                                         // each wave has a column of its own
+  if (p.solo) own = tiles <= ATT_WAVES && B * columns >= 512;         // 820 columns of 1 to 3 tokens, head_dim 256, 26 -> 8 us
+  else if (row_groups_of(cache, heads) > 1) own = B * columns >= 64;  // 24 query heads for each of 8 key heads, 1, 4, 16 requests: 12.5 -> 15.7, 33.8 -> 28.9, 102 -> 80 us
+  else own = columns % ATT_WAVES == 0 && heads / cache.heads <= 2 && B * columns >= ATT_WAYS_ITEMS;
+  p.ways = own ? 1 : ATT_WAVES;
   // workgroups: three, two or one for each CU by the registers that a wave takes.  head_dim 64 with 512, 768, 1024: 64 requests of 100 to
   // 3000 tokens 52.3, 50.1, 49.6 us, 16 long ones 34.6, 35.4, 35.8; 128: 16 58.3, 59.4, 64.6; 256 with 256, 512, 768: 64.9, 72.6, 79.9
   const int64_t full = cache.head_dim <= 64 ? 768 : cache.head_dim <= 128 ? 512 : 256;

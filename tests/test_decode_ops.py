@@ -402,6 +402,20 @@ def test_paged_attention_past_the_cache(tq, heads, kv_heads, dim, fmt, long):
 
 
 @gpu
+@pytest.mark.parametrize("heads,kv_heads,dim,fmt,page", [(20, 20, 80, "bf16", 16), (40, 8, 128, "bf16", 32), (16, 8, 64, "mxfp8", 16), (32, 4, 256, "mxfp8", 64), (51, 3, 96, "bf16", 16)])
+def test_paged_attention_of_many_tiny_requests(tq, heads, kv_heads, dim, fmt, page):
+    # tables for at most 128 tokens
+    g = np.random.default_rng(dim)
+    lengths = [int(n) for n in g.integers(0, 64 - page + 1, 190)]
+    lengths[5], lengths[6] = 64, 0
+    cache, q, tables, lens, pages = attention_case(tq, 190, heads, kv_heads, dim, page, lengths, fmt, "tokens", 9)
+    assert tables.shape[1] * page <= 192
+    tables = tables[:, : 128 // page].contiguous()
+    want = attention_reference(q, values_of(cache, "k"), values_of(cache, "v"), tables, lens, dim ** -0.5, pages)
+    check_attention(tq.torq_paged_attention(q.to(DEV), cache, tables.to(DEV), lens.to(DEV), dim ** -0.5), *want)
+
+
+@gpu
 @pytest.mark.parametrize("native", [True, False])
 def test_decode_calls_without_requests_or_tokens(tq, native, monkeypatch):
     if not native:
