@@ -70,7 +70,7 @@ struct AttentionArgs {
   int solo;                           // a workgroup for each (request, columns that it works on), which is its run
   float scale_log2;                   // scale * log2(e): the softmax is taken to base 2
   uint16_t *out;
-  float *part, *part_ml;              // [run][2][16][dim] and [run][2][16][2]: O, and m and l, of a (request, key head) not whole in a run
+  float *part, *part_ml;              // [run][2][columns at a time][16][dim] and [2]: O, and m and l, of what is not whole in a run
   Cut *cuts;                          // [run], or [request][columns that a workgroup works on at a time]
   int by_item;
 };
@@ -98,7 +98,6 @@ __device__ __forceinline__ void widen4(uint32_t v, float scale, uint32_t &a, uin
   b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, scale, true));
 }
 typedef const __attribute__((address_space(4))) int *uniform_ints;      // read by scalar loads
-typedef __attribute__((__vector_size__(2 * sizeof(unsigned)))) unsigned u32x2;
 
 // `bytes` bytes from p as a raw buffer; all three the same in every lane
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t records(const void *base, int64_t at, int bytes) {
@@ -190,17 +189,23 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
     seg = Segment{b, 0, tiles, length, 0, 0, 0, tiles, 0};      // (end: that of no run)
     place_column(seg, column);
   } else {
-    // tiles of one column, request by request: every wave adds them up, a lane `per` of them
+    // places of one column, request by request: every wave adds them up, a lane those of `per` requests (eight loads at a time)
     const int per = (a.B + 63) / 64;
+    auto length_at = [&](int b) { return b < a.B ? length_of(a, a.lengths[b]) : 0; };
     int mine = 0, length = 0;
-    for (int i = 0; i < per; ++i)
-      if (lane * per + i < a.B) length = length_of(a, a.lengths[lane * per + i]), mine += places_of((length + ATT_TILE - 1) / ATT_TILE);
-    int sum = mine;
+    if (per == 1) {
+      length = length_at(lane);
+      mine = places_of((length + ATT_TILE - 1) / ATT_TILE);
+    } else {
+      for (int i0 = 0; i0 < per; i0 += 8) {
+        int read[8];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int up = __shfl_up(sum, o);
-      if (lane >= o) sum += up;
+        for (int i = 0; i < 8; ++i) read[i] = i0 + i < per ? length_at(lane * per + i0 + i) : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mine += places_of((read[i] + ATT_TILE - 1) / ATT_TILE);
+      }
     }
+    int sum = wave_sum(mine);
     const int total = __builtin_amdgcn_readlane(sum, 63);
     const Runs runs(total * columns, gridDim.x, WAYS);
     run_begin = uniform(runs.begin(min(run, runs.runs))), run_end = uniform(runs.begin(min(run + 1, runs.runs)));
@@ -209,14 +214,23 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       zeros();
       return;
     }
-    // the lane whose requests the run begins in, and the request
-    const int owner = __builtin_ctzll(__ballot(run_begin < sum * columns));
-    int before = __builtin_amdgcn_readlane(sum - mine, owner), b = owner * per;
-    take_request(seg, b, per == 1 ? __builtin_amdgcn_readlane(length, owner) : length_of(a, lengths[b]));
-    while (run_begin >= (before + places_of(seg.tiles)) * columns) {
-      before += places_of(seg.tiles);
-      take_request(seg, seg.b + 1, length_of(a, lengths[seg.b + 1]));
+    // the lane whose requests the run begins in; then the request, 64 of them at a time
+    int owner = __builtin_ctzll(__ballot(run_begin < sum * columns)), before = __builtin_amdgcn_readlane(sum - mine, owner), b = owner;
+    if (per > 1) {
+      for (int b0 = owner * per;; b0 += 64) {
+        length = length_at(b0 + lane);
+        mine = places_of((length + ATT_TILE - 1) / ATT_TILE);
+        sum = before + wave_sum(mine);
+        const uint64_t behind_it = __ballot(run_begin < sum * columns);
+        if (behind_it) {
+          owner = __builtin_ctzll(behind_it), b = b0 + owner;
+          before = __builtin_amdgcn_readlane(sum - mine, owner);
+          break;
+        }
+        before = __builtin_amdgcn_readlane(sum, 63);
+      }
     }
+    take_request(seg, b, __builtin_amdgcn_readlane(length, owner));
     const int into = run_begin - before * columns, column = uniform(into / places_of(seg.tiles));
     place_column(seg, column);
     // tile t of a column has the place att_setup + t from its beginning

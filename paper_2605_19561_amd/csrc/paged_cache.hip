@@ -14,28 +14,6 @@ namespace torq {
 constexpr int TAB_CHUNK = 1024;
 constexpr int TAB_FEW = 2;            // entries of a request that its lane writes
 
-// inclusive sum over the lanes of a wave, by DPP: shifts within rows of 16, then the rows' last lanes passed on
-template <class T>
-__device__ __forceinline__ T wave_sum(T x) {
-  if constexpr (sizeof(T) == 4) {
-    int v = x;
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
-    return v;
-  } else {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const T up = __shfl_up(x, o);
-      if ((threadIdx.x & 63) >= o) x += up;
-    }
-    return x;
-  }
-}
-
 // T: what holds the sums of a chunk.
 template <class T>
 __global__ void __launch_bounds__(256) block_tables_kernel(const int *__restrict__ held, const int *__restrict__ lengths, int64_t B,

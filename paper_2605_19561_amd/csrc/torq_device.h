@@ -296,6 +296,28 @@ __device__ __forceinline__ float quad_amax_nan(float v) {
   return __uint_as_float(a);
 }
 
+// Inclusive sum over the lanes of a wave, 32 bits by DPP: shifts within rows of 16, then the rows' last lanes passed on
+template <class T>
+__device__ __forceinline__ T wave_sum(T x) {
+  if constexpr (sizeof(T) == 4) {
+    int v = x;
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+    return v;
+  } else {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const T up = __shfl_up(x, o);
+      if ((threadIdx.x & 63) >= o) x += up;
+    }
+    return x;
+  }
+}
+
 // bf16 <-> fp32 bit moves
 __device__ __forceinline__ float bf16_bits_to_f32(uint32_t h) { return __uint_as_float(h << 16); }
 

@@ -416,6 +416,18 @@ def test_paged_attention_of_many_tiny_requests(tq, heads, kv_heads, dim, fmt, pa
 
 
 @gpu
+@pytest.mark.parametrize("B,heads,kv_heads", [(64, 4, 2), (65, 4, 2), (513, 4, 2), (5000, 2, 1), (5000, 4, 4)])
+def test_paged_attention_of_very_many_requests(tq, B, heads, kv_heads):
+    # more requests than a wave has lanes, most of them empty or short, a few long, wide tables
+    g = np.random.default_rng(B)
+    lengths = [int(n) for n in g.integers(0, 40, B) * (g.random(B) < 0.3)]
+    lengths[B // 2], lengths[B - 1], lengths[63] = 700, 333, 90
+    cache, q, tables, lens, pages = attention_case(tq, B, heads, kv_heads, 32, 16, lengths, "bf16", "heads", 10)
+    want = attention_reference(q, values_of(cache, "k"), values_of(cache, "v"), tables, lens, 0.2, pages)
+    check_attention(tq.torq_paged_attention(q.to(DEV), cache, tables.to(DEV), lens.to(DEV), 0.2), *want)
+
+
+@gpu
 @pytest.mark.parametrize("native", [True, False])
 def test_decode_calls_without_requests_or_tokens(tq, native, monkeypatch):
     if not native:
