@@ -10,7 +10,7 @@
 // (few query heads for a key head and many of those, or more than 16 query heads, whose waves then find the same lines in the cache)
 // each has one for itself and they need not wait for one another.  What lies whole within a run is written as output; of the others
 // O, m and l go to the workspace, two at most for a run (and wave), and a second kernel joins them in the order of the tokens.  Tables for
-// at most 512 tokens: one launch, a workgroup for each (request, key head).
+// at most 512 tokens (1024 if there are many): one launch, a workgroup for each (request, key head).
 //
 // A tile goes through the matrix cores transposed, and nothing of it passes between lanes but the column maxima:
 //   S^T [token][head] = K [token][i] Q^T [i][head]           v_mfma_f32_16x16x32_bf16, two groups of 16 tokens
@@ -588,8 +588,11 @@ struct Plan {
 Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   Plan p;
   const int64_t columns = (int64_t)cache.heads * row_groups_of(cache, heads), tiles = ((int64_t)width * cache.page_size + ATT_TILE - 1) / ATT_TILE;
-  // Every request within so few tokens that a workgroup each is done before runs would be made out and joined (333 tokens 13 -> 7.2 us)
-  p.solo = tiles <= 16;
+  // Every request within so few tokens that a workgroup each is done before runs would be made out and joined.  333 tokens, 8 key heads 13 ->
+  // 7.2 us; up to 1000 tokens, 8 key heads, 1, 4, 16, 64, 256 requests in runs / a workgroup each: 10.1 / 12.8, 13.8 / 14.7, 20.4 / 15.5,
+  // 49.8 / 44.2, 175 / 165 us, ragged (1 to 1000) 4, 16, 64 of them 10.9 / 13.2, 16.3 / 14.6, 32.5 / 32.9; up to 2000, ragged, 64 of
+  // them 52.5 / 61.5
+  p.solo = tiles <= 16 || (tiles <= 32 && B * columns >= 128);
   bool own;                                         // each wave has a column of its own
   if (p.solo) own = tiles <= ATT_WAVES && B * columns >= 512;         // 820 columns of 1 to 3 tokens, head_dim 256, 26 -> 8 us
   else if (row_groups_of(cache, heads) > 1) own = B * columns >= 64;  // 24 query heads for each of 8 key heads, 1, 4, 16 requests: 12.5 -> 15.7, 33.8 -> 28.9, 102 -> 80 us
