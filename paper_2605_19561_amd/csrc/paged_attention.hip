@@ -594,7 +594,7 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   // them 52.5 / 61.5
   p.solo = tiles <= 16 || (tiles <= 32 && B * columns >= 128);
   bool own;                                         // each wave has a column of its own
-  if (p.solo) own = tiles <= ATT_WAVES && B * columns >= 512;         // 820 columns of 1 to 3 tokens, head_dim 256, 26 -> 8 us
+  if (p.solo) own = (tiles <= 4 && B * columns >= 512) || (tiles <= 8 && B * columns >= 2048);      // 820 columns of 1 to 3 tokens, head_dim 256, 26 -> 8 us
   else if (row_groups_of(cache, heads) > 1) own = B * columns >= 64;  // 24 query heads for each of 8 key heads, 1, 4, 16 requests: 12.5 -> 15.7, 33.8 -> 28.9, 102 -> 80 us
   else own = columns % ATT_WAVES == 0 && heads / cache.heads <= 2 && B * columns >= ATT_WAYS_ITEMS;
   p.ways = own ? 1 : ATT_WAVES;

@@ -2,7 +2,7 @@
 // HBM-bound, 8 bytes a value with a residual and bf16 out, 7 1/32 to MXFP8.  Measured: [8192, 8192] 79.4 us (6.8 TB/s), [2048, 5120]
 // to MXFP8 13.4 us (5.5 TB/s), one row of 4096 3.1 us in a graph.
 //
-// 16, 64, 256 or 1024 lanes take a row; its s stay in registers between the sum of squares and the product, so x and residual are read once.
+// 16 to 1024 lanes take a row; its s stay in registers between the sum of squares and the product, so x and residual are read once.
 // A lane holds 8 consecutive values (16-byte loads and stores), four lanes a block of MXFP8.
 #include "torq_device.h"
 #include "torq_internal.h"
@@ -126,6 +126,7 @@ hipError_t launch_add_rms_norm(const void *x, const void *residual, const void *
   // lanes for every row, against this: [65536, 128] 30.6 -> 7.3 us, [500000, 64] to MXFP8 387 -> 47, [1, 28672] 10.3 -> 4.7,
   // [2300, 25600] to MXFP8 53 -> 38.
   if (n8 <= 16) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+  if (n8 <= 32) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
   if (n8 <= 64) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
   if (n8 <= 128) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
   if (n8 <= 256) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});

@@ -624,6 +624,23 @@ def test_add_rms_norm(tq, either_way, M, d, fmt, with_residual):
 
 
 @gpu
+@pytest.mark.parametrize("M,d", [(1000, 32), (999, 128), (777, 160), (501, 256), (333, 288), (130, 1024), (70, 1056)])
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp8"])
+def test_add_rms_norm_of_many_short_rows(tq, M, d, fmt):
+    # rows that share a wave or a workgroup, the last of them not full
+    g = rng(M, d)
+    x, w = torch.randn((M, d), generator=g).to(BF), (1 + 0.1 * torch.randn(d, generator=g)).to(BF)
+    _, y = norm_reference(x, None, w, 1e-6)
+    form = tq.TORQ_FMT_BF16 if fmt == "bf16" else tq.TORQ_FMT_MXFP8
+    out, scales, _ = tq.torq_add_rms_norm(x.to(DEV), None, w.to(DEV), 1e-6, form)
+    if fmt == "bf16":
+        assert ((out.double().cpu() - y).abs() <= (2.0 ** -8 + 2.0 ** -16) * y.abs() + 1e-38).all()
+        return
+    step = (2.0 ** (scales.view(torch.uint8).cpu().double() - 127)).repeat_interleave(32, -1)
+    assert ((out.double().cpu() * step - y).abs() <= (2.0 ** -4 + 2.0 ** -15) * y.abs() + step * 2.0 ** -10).all()
+
+
+@gpu
 def test_add_rms_norm_in_place_and_at_the_edges(tq):
     g = rng(8)
     x, r, w = torch.randn((5, 256), generator=g).to(BF), torch.randn((5, 256), generator=g).to(BF), torch.ones(256, dtype=BF)
