@@ -1,13 +1,13 @@
 // torq_paged_attention: one new token of each request over its pages, out = softmax(scale q K^T) V for each head.
 //
-// The query heads of a key head are the columns of one matrix product, up to 16 at a time, so K and V are read once for all of
-// them: HBM-bound, 2 (bf16) or 1 1/32 (MXFP8) bytes for 2 heads / kv_heads flops.
+// The query heads of a key head are the columns of one matrix product, up to 16, or of two side by side, up to 32, so K and V are
+// read once for all of them: HBM-bound, 2 (bf16) or 1 1/32 (MXFP8) bytes for 2 heads / kv_heads flops.
 //
 // Work: the tokens of every (request, key head) in tiles of 32, all of them in one row of tiles (with room for what each one costs
 // besides), cut into equal runs, one for each workgroup: lengths may be as ragged as they like, and the host need not know them, since every
 // workgroup adds them up itself.  A run goes through one or several (request, key head)s.  The four waves of a workgroup take turns at
 // the tiles of one, each with a softmax of its own in one pass (running maximum m, sum l, unnormalised O), put together in LDS at its end; or
-// (few query heads for a key head and many of those, or more than 16 query heads, whose waves then find the same lines in the cache)
+// (few query heads for a key head and many of those, or more query heads than fit a column, whose waves then find the same lines in the cache)
 // each has one for itself and they need not wait for one another.  What lies whole within a run is written as output; of the others
 // O, m and l go to the workspace, two at most for a run (and wave), and a second kernel joins them in the order of the tokens.  Tables for
 // at most 512 tokens (1024 if there are many): one launch, a workgroup for each (request, key head).
@@ -39,7 +39,7 @@ namespace torq {
 
 constexpr int ATT_TILE = 32;          // tokens of a wave's step
 constexpr int ATT_WAVES = 4;
-constexpr int ATT_ROWS = 16;          // query heads of a workgroup
+constexpr int ATT_ROWS = 16;          // query heads of a product's columns
 constexpr int ATT_JOIN = 512;         // threads of a workgroup that joins, at most
 // Columns from which each wave has one of its own, with up to 2 query heads for each.  77 x 20 heads 120 -> 91 us, 256 requests x 8 key heads
 // with 2 query heads each 144.6 -> 139.7; with 4 146.7 -> 151.1, with 8 153 -> 162 (four times the parts to join).
@@ -66,11 +66,11 @@ struct AttentionArgs {
   const int *tables, *lengths;
   int64_t table_stride, page16_magic; // t / page_size = (t / 16) * page16_magic >> 38
   int64_t most;                       // width * page_size
-  int B, page_size, kv_heads, group, row_groups, dim;
+  int B, page_size, kv_heads, group, rows, row_groups, dim;            // rows: query heads of a column at most
   int solo;                           // a workgroup for each (request, columns that it works on), which is its run
   float scale_log2;                   // scale * log2(e): the softmax is taken to base 2
   uint16_t *out;
-  float *part, *part_ml;              // [run][2][columns at a time][16][dim] and [2]: O, and m and l, of what is not whole in a run
+  float *part, *part_ml;              // [run][2][columns at a time][rows][dim] and [2]: O, and m and l, of what is not whole in a run
   Cut *cuts;                          // [run], or [request][columns that a workgroup works on at a time]
   int by_item;
 };
@@ -126,16 +126,16 @@ __device__ __forceinline__ float over_column(float v, F &&op) {
 __device__ __forceinline__ int length_of(const AttentionArgs &a, int n) { return n < 0 ? 0 : n < a.most ? n : (int)a.most; }
 
 // DP: head_dim rounded up to what the operands hold.  WAYS: 4, the waves take turns at the tiles of a column; 1, each has a column
-// of its own and all of its tiles in the run.
-template <int DP, bool F8, bool ONCE, int WAYS>
+// of its own and all of its tiles in the run.  RT: products side by side, for up to 16 query heads each.
+template <int DP, bool F8, bool ONCE, int WAYS, int RT>
 __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   constexpr int KS = DP / 32;                       // k-steps of S
   constexpr int E = DP < 128 ? DP / 16 : 8;         // consecutive values of V in a lane
   constexpr int NH = DP / (16 * E);                 // such pieces of a row
-  constexpr int BYTES = F8 ? 1 : 2;
+  constexpr int BYTES = F8 ? 1 : 2, ROWS = ATT_ROWS * RT;
   constexpr int KL = DP * BYTES / 64;               // 16-byte loads of a lane for a group of 16 rows of K
   __shared__ f32x4 o_all[WAYS][ATT_ROWS][WAYS > 1 ? 4 * E + 1 : 1];       // a piece of O at a time
-  __shared__ float m_all[WAYS][ATT_ROWS], l_all[WAYS][ATT_ROWS];
+  __shared__ float m_all[WAYS][ROWS], l_all[WAYS][ROWS];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
   // (key head, rows) of a request, as many at a time as the workgroup works on
   const int columns = (a.kv_heads * a.row_groups + ATT_WAVES / WAYS - 1) / (ATT_WAVES / WAYS), way = WAYS > 1 ? wave : 0;
@@ -247,16 +247,19 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   // what a lane reads of a group of 16 tokens, in bytes from its first token
   const int k_at = n * a.token_bytes + 16 * g, v_at = 4 * g * a.token_bytes + E * n * BYTES;
   // Q^T as the B operand: column n, the i of this lane's K values
-  bf16x8 q[KS];
+  bf16x8 q[RT][KS];
   auto load_q = [&](const Segment &s) {
-    const int row = s.rows_at * ATT_ROWS + n;       // query head of this lane's column within the group
 #pragma unroll
-    for (int t = 0; t < KS; ++t) {
-      const int i = F8 ? 64 * (t / 2) + 16 * g + 8 * (t % 2) : 32 * t + 8 * g;
-      u32x4 v = {0, 0, 0, 0};
-      if (row < a.group && i < a.dim)
-        v = *reinterpret_cast<const u32x4 *>(a.q + s.b * a.q_stride + (int64_t)(s.kv_head * a.group + row) * a.q_head_stride + i);
-      q[t] = as_bf16(v);
+    for (int rt = 0; rt < RT; ++rt) {
+      const int row = s.rows_at * ROWS + rt * ATT_ROWS + n;       // query head of this lane's column within the group
+#pragma unroll
+      for (int t = 0; t < KS; ++t) {
+        const int i = F8 ? 64 * (t / 2) + 16 * g + 8 * (t % 2) : 32 * t + 8 * g;
+        u32x4 v = {0, 0, 0, 0};
+        if (row < a.group && i < a.dim)
+          v = *reinterpret_cast<const u32x4 *>(a.q + s.b * a.q_stride + (int64_t)(s.kv_head * a.group + row) * a.q_head_stride + i);
+        q[rt][t] = as_bf16(v);
+      }
     }
   };
   // the pages of a tile's two groups of 16 tokens, and where in them the groups begin; how many of a group are tokens; where they lie, in bytes
@@ -357,10 +360,14 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
     }
     Pages pages_behind = look_up(behind, behind.first + way);
     pages = look_up(seg, seg.first + way + WAYS);
-    f32x4 o[NH * E];
+    f32x4 o[RT][NH * E];
+    float m[RT], l[RT];
 #pragma unroll
-    for (int i = 0; i < NH * E; ++i) o[i] = f32x4{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.0f;
+    for (int rt = 0; rt < RT; ++rt) {
+      m[rt] = -INFINITY, l[rt] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NH * E; ++i) o[rt][i] = f32x4{0, 0, 0, 0};
+    }
     if (seg.first + way >= seg.last) {             // (nothing for this wave)
       here = place(behind, behind.first + way, pages_behind);
       load_k(here);
@@ -369,16 +376,19 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
     }
     // Q is there from here on: a wait for it inside the loop would be one for all loads, in every round
 #pragma unroll
-    for (int t = 0; t < KS; ++t) asm volatile("" : "+v"(q[t]));
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int t = 0; t < KS; ++t) asm volatile("" : "+v"(q[rt][t]));
     for (int tile = seg.first + way; tile < seg.last; tile += WAYS) {
       Place next;
       if (tile + WAYS < seg.last) next = place(seg, tile + WAYS, pages);
       else next = place(behind, behind.first + way, pages_behind);
       pages = look_up(seg, tile + 2 * WAYS);
-      f32x4 st[2];
+      f32x4 st[RT][2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        st[u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) st[rt][u] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < KL; ++s) {
           if constexpr (F8) {
@@ -386,44 +396,52 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
             uint32_t w[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) widen4(k[u][s][e], scale, w[2 * e], w[2 * e + 1]);
-            st[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(u32x4{w[0], w[1], w[2], w[3]}), q[2 * s], st[u], 0, 0, 0);
-            st[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(u32x4{w[4], w[5], w[6], w[7]}), q[2 * s + 1], st[u], 0, 0, 0);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+              st[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(u32x4{w[0], w[1], w[2], w[3]}), q[rt][2 * s], st[rt][u], 0, 0, 0);
+              st[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(u32x4{w[4], w[5], w[6], w[7]}), q[rt][2 * s + 1], st[rt][u], 0, 0, 0);
+            }
           } else {
-            st[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(k[u][s]), q[s], st[u], 0, 0, 0);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+              st[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(k[u][s]), q[rt][s], st[rt][u], 0, 0, 0);
           }
         }
       }
       load_k(next);
-      float m_new = m, p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = 4 * g + e % 4 < here.count[e / 4] ? st[e / 4][e % 4] * a.scale_log2 : -INFINITY;
-        m_new = fmaxf(m_new, p[e]);
-      }
-      m_new = over_column(m_new, [](float x, float y) { return fmaxf(x, y); });
-      // (nothing but masked tokens so far: everything below is 0)
-      const float base = m_new == -INFINITY ? 0.0f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m - base);
-      m = m_new;
-      l *= alpha;
       // p as two bf16 parts, the first cut off and the second rounded: p to 2^-16, so the output's own rounding is the only one to
       // bf16 that shows.  Both are positive: an infinite v stays infinite (masked tokens have a v of 0 below).
-      u32x4 pt, pt_rest;
+      u32x4 pt[RT], pt_rest[RT];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(p[e] - base);
-        l += p[e];
+      for (int rt = 0; rt < RT; ++rt) {
+        float m_new = m[rt], p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = 4 * g + e % 4 < here.count[e / 4] ? st[rt][e / 4][e % 4] * a.scale_log2 : -INFINITY;
+          m_new = fmaxf(m_new, p[e]);
+        }
+        m_new = over_column(m_new, [](float x, float y) { return fmaxf(x, y); });
+        // (nothing but masked tokens so far: everything below is 0)
+        const float base = m_new == -INFINITY ? 0.0f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m[rt] - base);
+        m[rt] = m_new;
+        l[rt] *= alpha;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(p[e] - base);
+          l[rt] += p[e];
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t lo = __float_as_uint(p[2 * c]), hi = __float_as_uint(p[2 * c + 1]);
+          pt[rt][c] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
+          const bf16x2 rest = {(__bf16)fmaxf(p[2 * c] - __uint_as_float(lo & 0xFFFF0000u), 0x1p-126f),
+                               (__bf16)fmaxf(p[2 * c + 1] - __uint_as_float(hi & 0xFFFF0000u), 0x1p-126f)};
+          pt_rest[rt][c] = __builtin_bit_cast(uint32_t, rest);
+        }
+#pragma unroll
+        for (int i = 0; i < NH * E; ++i) o[rt][i] *= alpha;
       }
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const uint32_t lo = __float_as_uint(p[2 * c]), hi = __float_as_uint(p[2 * c + 1]);
-        pt[c] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
-        const bf16x2 rest = {(__bf16)fmaxf(p[2 * c] - __uint_as_float(lo & 0xFFFF0000u), 0x1p-126f),
-                             (__bf16)fmaxf(p[2 * c + 1] - __uint_as_float(hi & 0xFFFF0000u), 0x1p-126f)};
-        pt_rest[c] = __builtin_bit_cast(uint32_t, rest);
-      }
-#pragma unroll
-      for (int i = 0; i < NH * E; ++i) o[i] *= alpha;
 #pragma unroll
       for (int h = 0; h < NH; ++h) {
         uint32_t w[8][E / 2];                       // 8 tokens, E values each
@@ -444,75 +462,81 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
 #pragma unroll
           for (int c = 0; c < 4; ++c)
             vt[c] = __builtin_amdgcn_perm(w[2 * c + 1][j / 2], w[2 * c][j / 2], j % 2 ? 0x07060302 : 0x05040100);
-          o[h * E + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(vt), as_bf16(pt), o[h * E + j], 0, 0, 0);
-          o[h * E + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(vt), as_bf16(pt_rest), o[h * E + j], 0, 0, 0);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            o[rt][h * E + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(vt), as_bf16(pt[rt]), o[rt][h * E + j], 0, 0, 0);
+            o[rt][h * E + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(vt), as_bf16(pt_rest[rt]), o[rt][h * E + j], 0, 0, 0);
+          }
         }
       }
       load_v(next);
       here = next;
     }
-    // The lanes of a column hold the sums of their own tokens.
-    l = over_column(l, [](float x, float y) { return x + y; });
-    const int rows = min(ATT_ROWS, a.group - seg.rows_at * ATT_ROWS);
-    uint16_t *const out = a.out + ((int64_t)seg.b * a.kv_heads * a.group + seg.kv_head * a.group + seg.rows_at * ATT_ROWS) * a.dim;
-    const int64_t part = ((int64_t)(run * 2 + second) * (ATT_WAVES / WAYS) +
-                          (WAYS == 1 ? wave : 0)) * ATT_ROWS;
-    // lane (n, g), o[h E + j][r] = O[head n][16 E h + E (4 g + r) + j]
-    if constexpr (WAYS == 1) {
-      const float inverse = l != 0.0f ? 1.0f / l : 0.0f;
-      if (n < rows && !whole && g == 0) a.part_ml[2 * (part + n)] = m, a.part_ml[2 * (part + n) + 1] = l;
+    const int rows = min(ROWS, a.group - seg.rows_at * ROWS);
+    uint16_t *const out = a.out + ((int64_t)seg.b * a.kv_heads * a.group + seg.kv_head * a.group + seg.rows_at * ROWS) * a.dim;
+    const int64_t part = ((int64_t)(run * 2 + second) * (ATT_WAVES / WAYS) + (WAYS == 1 ? wave : 0)) * ROWS;
 #pragma unroll
-      for (int h = 0; h < NH; ++h)
+    for (int rt = 0; rt < RT; ++rt) {
+      // The lanes of a column hold the sums of their own tokens.
+      l[rt] = over_column(l[rt], [](float x, float y) { return x + y; });
+      const int at = rt * ATT_ROWS;                 // the first row; lane (n, g), o[h E + j][r] = O[row at + n][16 E h + E (4 g + r) + j]
+      if constexpr (WAYS == 1) {
+        const float inverse = l[rt] != 0.0f ? 1.0f / l[rt] : 0.0f;
+        if (at + n < rows && !whole && g == 0) a.part_ml[2 * (part + at + n)] = m[rt], a.part_ml[2 * (part + at + n) + 1] = l[rt];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int i = 16 * E * h + E * (4 * g + r);
-          if (n >= rows || i >= a.dim) continue;
+        for (int h = 0; h < NH; ++h)
 #pragma unroll
-          for (int j = 0; j < E; j += 4) {
-            f32x4 x = {o[h * E + j][r], o[h * E + j + 1][r], o[h * E + j + 2][r], o[h * E + j + 3][r]};
-            if (whole) {
-              x *= inverse;
-              *reinterpret_cast<bf16x4 *>(out + n * a.dim + i + j) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
-            } else {
-              *reinterpret_cast<f32x4 *>(a.part + (part + n) * a.dim + i + j) = x;
+          for (int r = 0; r < 4; ++r) {
+            const int i = 16 * E * h + E * (4 * g + r);
+            if (at + n >= rows || i >= a.dim) continue;
+#pragma unroll
+            for (int j = 0; j < E; j += 4) {
+              f32x4 x = {o[rt][h * E + j][r], o[rt][h * E + j + 1][r], o[rt][h * E + j + 2][r], o[rt][h * E + j + 3][r]};
+              if (whole) {
+                x *= inverse;
+                *reinterpret_cast<bf16x4 *>(out + (at + n) * a.dim + i + j) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+              } else {
+                *reinterpret_cast<f32x4 *>(a.part + (part + at + n) * a.dim + i + j) = x;
+              }
             }
           }
-        }
-    } else {
-      // the waves' put together
-      if (g == 0) m_all[wave][n] = m, l_all[wave][n] = l;
+      } else {
+        // the waves' put together
+        if (g == 0) m_all[wave][at + n] = m[rt], l_all[wave][at + n] = l[rt];
 #pragma unroll
-      for (int h = 0; h < NH; ++h) {
+        for (int h = 0; h < NH; ++h) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+          for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int j = 0; j < E; j += 4)
-            o_all[wave][n][(E * (4 * g + r) + j) / 4] = f32x4{o[h * E + j][r], o[h * E + j + 1][r], o[h * E + j + 2][r], o[h * E + j + 3][r]};
-        __syncthreads();
-        const int begin = 16 * E * h, quads = min(16 * E, a.dim - begin) / 4;
-        for (int x = tid; x < rows * quads; x += 256) {
-          const int r = x / quads, c = x - r * quads;
-          float top = -INFINITY;
+            for (int j = 0; j < E; j += 4)
+              o_all[wave][n][(E * (4 * g + r) + j) / 4] =
+                  f32x4{o[rt][h * E + j][r], o[rt][h * E + j + 1][r], o[rt][h * E + j + 2][r], o[rt][h * E + j + 3][r]};
+          __syncthreads();
+          const int begin = 16 * E * h, quads = min(16 * E, a.dim - begin) / 4;
+          for (int x = tid; x < min(rows - at, ATT_ROWS) * quads; x += 256) {
+            const int r = x / quads, c = x - r * quads, row = at + r;
+            float top = -INFINITY;
 #pragma unroll
-          for (int w = 0; w < WAYS; ++w) top = fmaxf(top, m_all[w][r]);
-          const float base = top == -INFINITY ? 0.0f : top;
-          float sum = 0.0f;
-          f32x4 value = {0, 0, 0, 0};
+            for (int w = 0; w < WAYS; ++w) top = fmaxf(top, m_all[w][row]);
+            const float base = top == -INFINITY ? 0.0f : top;
+            float sum = 0.0f;
+            f32x4 value = {0, 0, 0, 0};
 #pragma unroll
-          for (int w = 0; w < WAYS; ++w) {
-            const float f = __builtin_amdgcn_exp2f(m_all[w][r] - base);
-            sum += f * l_all[w][r];
-            value += f * o_all[w][r][c];
+            for (int w = 0; w < WAYS; ++w) {
+              const float f = __builtin_amdgcn_exp2f(m_all[w][row] - base);
+              sum += f * l_all[w][row];
+              value += f * o_all[w][r][c];
+            }
+            if (whole) {
+              value *= sum != 0.0f ? 1.0f / sum : 0.0f;
+              *reinterpret_cast<bf16x4 *>(out + row * a.dim + begin + 4 * c) = bf16x4{(__bf16)value[0], (__bf16)value[1], (__bf16)value[2], (__bf16)value[3]};
+            } else {
+              *reinterpret_cast<f32x4 *>(a.part + (part + row) * a.dim + begin + 4 * c) = value;
+              if (begin + c == 0) a.part_ml[2 * (part + row)] = top, a.part_ml[2 * (part + row) + 1] = sum;
+            }
           }
-          if (whole) {
-            value *= sum != 0.0f ? 1.0f / sum : 0.0f;
-            *reinterpret_cast<bf16x4 *>(out + r * a.dim + begin + 4 * c) = bf16x4{(__bf16)value[0], (__bf16)value[1], (__bf16)value[2], (__bf16)value[3]};
-          } else {
-            *reinterpret_cast<f32x4 *>(a.part + (part + r) * a.dim + begin + 4 * c) = value;
-            if (begin + c == 0) a.part_ml[2 * (part + r)] = top, a.part_ml[2 * (part + r) + 1] = sum;
-          }
+          if (rt + 1 < RT || h + 1 < NH || more) __syncthreads();
         }
-        if (h + 1 < NH || more) __syncthreads();
       }
     }
     if (!more) break;
@@ -530,17 +554,17 @@ __global__ void __launch_bounds__(ATT_JOIN) paged_attention_join_kernel(Attentio
   const Cut cut = a.cuts[blockIdx.x];
   if (cut.place < 0) return;
   const int parts = Runs(cut.each, cut.more).of(cut.last_tile) - cut.place / 2 + 1;
-  const int tid = threadIdx.x, quads = a.dim / 4, rows = min(ATT_ROWS, a.group);
+  const int tid = threadIdx.x, quads = a.dim / 4, rows = min(a.rows, a.group);
   const int all = together * rows * quads, here = min(all, many), ways = blockDim.x / here, way = tid / here;
   const int x = blockIdx.y * many + (tid - way * here), c = x % quads, r = x / quads % rows, w = x / quads / rows;
-  const int column = cut.column * together + w, kv_head = column / a.row_groups, row = (column - kv_head * a.row_groups) * ATT_ROWS + r;
+  const int column = cut.column * together + w, kv_head = column / a.row_groups, row = (column - kv_head * a.row_groups) * a.rows + r;
   const bool real = x < all && way < ways && row < a.group && kv_head < a.kv_heads;
   float m = -INFINITY, l = 0.0f;
   f32x4 v = {0, 0, 0, 0};
   if (real) {
 #pragma unroll 4
     for (int i = way; i < parts; i += ways) {
-      const int64_t at = ((int64_t)(i ? (cut.place / 2 + i) * 2 : cut.place) * together + w) * ATT_ROWS + r;
+      const int64_t at = ((int64_t)(i ? (cut.place / 2 + i) * 2 : cut.place) * together + w) * a.rows + r;
       const float mi = a.part_ml[2 * at], li = a.part_ml[2 * at + 1];
       const f32x4 vi = *reinterpret_cast<const f32x4 *>(a.part + at * a.dim + 4 * c);
       const float top = fmaxf(m, mi), base = top == -INFINITY ? 0.0f : top;
@@ -569,25 +593,36 @@ __global__ void __launch_bounds__(ATT_JOIN) paged_attention_join_kernel(Attentio
 }
 
 namespace {
-int row_groups_of(const torq_kv_cache_t &cache, int heads) { return (heads / cache.heads + ATT_ROWS - 1) / ATT_ROWS; }
+// Query heads of a column: 32 where there are more than 16, the registers hold two products side by side, and there are columns
+// enough without the second 16.  24 heads for each of 8 key heads of 128, 1, 4, 16 requests of 1000 to 8192 tokens with 16 / 32:
+// 12.3 / 13.1, 28.9 / 26.4, 79.8 / 65.6 us (32 heads 83.1 / 68.6, heads of 64 49.1 / 39.2, MXFP8 up to 32768 199 / 139); for one
+// key head, 1 request of 60000, 64 of up to 8192: 23.2 / 26.3, 53.0 / 39.1; one of 333 tokens 7.9 / 10.0.
+int rows_of(const torq_kv_cache_t &cache, int heads, int64_t B) {
+  return heads / cache.heads > ATT_ROWS && cache.head_dim <= 128 && B * cache.heads >= 32 ? 2 * ATT_ROWS : ATT_ROWS;
+}
+int row_groups_of(const torq_kv_cache_t &cache, int heads, int64_t B) {
+  const int rows = rows_of(cache, heads, B);
+  return (heads / cache.heads + rows - 1) / rows;
+}
 // Past the cache: rows of whole lines that one workgroup reads, and more of them than the cache holds, as far as the tables can tell.  Without /
 // with the hint, from HBM and the same cache again, us: 67 MB 21.7 / 20.7, 19.5 / 19.6; 134 MB 33.9 / 30.9, 28.4 / 29.4; 268 MB 57.8 / 52.1,
 // 47.8 / 50.8; 537 MB 104.7 / 94.2, 104.8 / 93.2; MXFP8 69 MB 23.9 / 23.5, 20.7 / 22.2, 277 MB 61.4 / 58.7, 52.0 / 57.9.  Rows that share lines
 // lose: heads of 80 168 MB 40.1 / 42.7, of 96 in MXFP8, tokens outermost, 208 MB 70.8 / 83.6.
 bool once_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
-  if (row_groups_of(cache, heads) > 1) return false;
+  if (row_groups_of(cache, heads, B) > 1) return false;
   const int bytes = cache.format == FMT_BF16 ? 2 : 1;
   const double pages = (double)std::min<int64_t>(cache.pages, B * (int64_t)width);
   return cache.head_dim * bytes % 128 == 0 && 2.0 * pages * cache.page_size * cache.heads * cache.head_dim * bytes > ONE_PASS_WEIGHT_BYTES;
 }
 struct Plan {
-  int ways, groups;
+  int ways, groups, rows;
   bool solo, by_item;
   int64_t items;
 };
 Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   Plan p;
-  const int64_t columns = (int64_t)cache.heads * row_groups_of(cache, heads), tiles = ((int64_t)width * cache.page_size + ATT_TILE - 1) / ATT_TILE;
+  p.rows = rows_of(cache, heads, B);
+  const int64_t columns = (int64_t)cache.heads * row_groups_of(cache, heads, B), tiles = ((int64_t)width * cache.page_size + ATT_TILE - 1) / ATT_TILE;
   // Every request within so few tokens that a workgroup each is done before runs would be made out and joined.  333 tokens, 8 key heads 13 ->
   // 7.2 us; up to 1000 tokens, 8 key heads, 1, 4, 16, 64, 256 requests in runs / a workgroup each: 10.1 / 12.8, 13.8 / 14.7, 20.4 / 15.5,
   // 49.8 / 44.2, 175 / 165 us, ragged (1 to 1000) 4, 16, 64 of them 10.9 / 13.2, 16.3 / 14.6, 32.5 / 32.9; up to 2000, ragged, 64 of
@@ -595,7 +630,7 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   p.solo = tiles <= 16 || (tiles <= 32 && B * columns >= 128);
   bool own;                                         // each wave has a column of its own
   if (p.solo) own = (tiles <= 4 && B * columns >= 512) || (tiles <= 8 && B * columns >= 2048);      // 820 columns of 1 to 3 tokens, head_dim 256, 26 -> 8 us
-  else if (row_groups_of(cache, heads) > 1) own = B * columns >= 64;  // 24 query heads for each of 8 key heads, 1, 4, 16 requests: 12.5 -> 15.7, 33.8 -> 28.9, 102 -> 80 us
+  else if (row_groups_of(cache, heads, B) > 1) own = B * columns >= 64;  // two columns of 16, 8 key heads, 1, 4, 16 requests: 12.5 -> 15.7, 33.8 -> 28.9, 102 -> 80 us
   else own = columns % ATT_WAVES == 0 && heads / cache.heads <= 2 && B * columns >= ATT_WAYS_ITEMS;
   p.ways = own ? 1 : ATT_WAVES;
   // workgroups: three, two or one for each CU by the registers that a wave takes.  head_dim 64 with 512, 768, 1024: 64 requests of 100 to
@@ -608,7 +643,7 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   return p;
 }
 size_t cuts_bytes(const Plan &p) { return (p.by_item ? (size_t)p.items : (size_t)p.groups) * sizeof(Cut); }
-size_t part_rows(const Plan &p) { return (size_t)p.groups * 2 * (ATT_WAVES / p.ways) * ATT_ROWS; }
+size_t part_rows(const Plan &p) { return (size_t)p.groups * 2 * (ATT_WAVES / p.ways) * p.rows; }
 }  // namespace
 
 size_t paged_attention_workspace_bytes(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
@@ -627,14 +662,20 @@ hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, i
   AttentionArgs a{(const char *)cache.k, (const char *)cache.v, cache.k_scales, cache.v_scales, cache.page_stride * bytes,
                   cache.head_stride * bytes, (int)cache.pages, (int)cache.token_stride * bytes, (const uint16_t *)q, q_stride,
                   q_head_stride, block_tables, lengths, table_stride, ((int64_t)1 << 38) / page16 + 1,
-                  (int64_t)width * cache.page_size, (int)B, cache.page_size, cache.heads, heads / cache.heads, row_groups_of(cache, heads),
+                  (int64_t)width * cache.page_size, (int)B, cache.page_size, cache.heads, heads / cache.heads, plan.rows, row_groups_of(cache, heads, B),
                   cache.head_dim, plan.solo, scale * 1.44269504088896340736f, (uint16_t *)out, part, part + part_rows(plan) * cache.head_dim,
                   (Cut *)workspace, plan.by_item};
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(plan.groups), dim3(256), 0, stream, a); };
   auto of_hint = [&](auto dp, auto of8, auto hint) {
     constexpr int DP = decltype(dp)::value;
     constexpr bool F8 = decltype(of8)::value, ONCE = decltype(hint)::value;
-    plan.ways > 1 ? go(paged_attention_kernel<DP, F8, ONCE, ATT_WAVES>) : go(paged_attention_kernel<DP, F8, ONCE, 1>);
+    if constexpr (DP <= 128)
+      if (plan.rows > ATT_ROWS) {
+        // (a column for each wave: short tables, or lines that are read more than once)
+        if (plan.ways == 1) return go(paged_attention_kernel<DP, F8, false, 1, 2>);
+        return go(paged_attention_kernel<DP, F8, ONCE, ATT_WAVES, 2>);
+      }
+    plan.ways > 1 ? go(paged_attention_kernel<DP, F8, ONCE, ATT_WAVES, 1>) : go(paged_attention_kernel<DP, F8, ONCE, 1, 1>);
   };
   auto of_format = [&](auto dp, auto of8) {
     // (rows of up to 64 bytes never go past the cache)
@@ -648,7 +689,7 @@ hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, i
   else of_dim(std::integral_constant<int, 256>{});
   if (!plan.solo) {
     // fewer (request, key head)s than runs: many parts each, over more threads; else two or three, one for most runs
-    const int together = ATT_WAVES / plan.ways, values = together * std::min(ATT_ROWS, a.group) * (a.dim / 4);
+    const int together = ATT_WAVES / plan.ways, values = together * std::min(a.rows, a.group) * (a.dim / 4);
     const int threads = plan.by_item ? ATT_JOIN : 256, many = plan.by_item ? 64 : 256;
     hipLaunchKernelGGL(paged_attention_join_kernel, dim3(plan.by_item ? (unsigned)plan.items : (unsigned)plan.groups, (values + many - 1) / many),
                        dim3(threads), 0, stream, a, together, many);

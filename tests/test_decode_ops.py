@@ -309,6 +309,10 @@ ATTENTION = [
     (7, 1, 64, 16, [65, 130], "bf16", "heads"), (7, 1, 64, 16, [65, 130], "mxfp8", "pairs"),
     (12, 1, 96, 16, [77, 200], "mxfp8", "heads"), (12, 1, 96, 16, [77, 200], "bf16", "heads"),
     (17, 1, 112, 32, [90, 1], "bf16", "heads"), (48, 2, 128, 16, [300, 20], "mxfp8", "heads"), (71, 1, 64, 16, [300, 20], "bf16", "heads"),
+    # more than 16 query heads for a key head, few and many of those
+    (24, 1, 128, 16, [1, 0, 2, 33, 700] * 8, "bf16", "heads"), (68, 4, 96, 32, [31, 257, 0, 64, 129, 1] * 3, "mxfp8", "tokens"),
+    (64, 2, 64, 16, [5, 520, 0, 77] * 5, "bf16", "pairs"), (33, 1, 80, 16, [90, 1, 200, 16] * 9, "bf16", "heads"),
+    (80, 2, 128, 16, [300, 45, 0, 1] * 12, "mxfp8", "heads"), (40, 2, 40, 16, [3, 0, 40, 33] * 70, "bf16", "heads"),
     (8, 4, 192, 16, [100, 33], "bf16", "heads"), (8, 4, 192, 16, [100, 33], "mxfp8", "tokens"),
     (16, 1, 256, 16, [400, 31], "bf16", "tokens"), (16, 1, 256, 16, [400, 31], "mxfp8", "heads"),
     (4, 2, 16, 16, [40], "bf16", "heads"), (4, 2, 24, 16, [40], "bf16", "heads"), (4, 4, 40, 16, [40, 3], "bf16", "heads"),
