@@ -41,8 +41,9 @@ constexpr int ATT_TILE = 32;          // tokens of a wave's step
 constexpr int ATT_WAVES = 4;
 constexpr int ATT_ROWS = 16;          // query heads of a product's columns
 constexpr int ATT_JOIN = 512;         // threads of a workgroup that joins, at most
-// Columns from which each wave has one of its own, with up to 2 query heads for each.  77 x 20 heads 120 -> 91 us, 256 requests x 8 key heads
-// with 2 query heads each 144.6 -> 139.7; with 4 146.7 -> 151.1, with 8 153 -> 162 (four times the parts to join).
+// Columns from which each wave has one of its own, with up to 2 query heads for each or head_dim over 128.  77 x 20 heads 120 -> 91 us, 256 requests x 8 key heads
+// with 2 query heads each 144.6 -> 139.7; with 4 146.7 -> 151.1, with 8 153 -> 162 (four times the parts to join).  head_dim 256, 4 query heads each, 128 x 8
+// of 1000 to 1500 tokens 217 -> 213, MXFP8 of 1000 to 2500 174 -> 164.
 constexpr int ATT_WAYS_ITEMS = 768;
 // What a (request, key head) costs besides its tiles (its place, its query, putting it together), in tiles of the row of them that is cut
 // into runs, by the waves that take turns.  64 requests of 1 to 600 tokens, 64 / 8 heads, with 0, 4, 8, 16: 35.4, 24.1, 23.9, 23.7 us;
@@ -629,9 +630,13 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   // them 52.5 / 61.5
   p.solo = tiles <= 16 || (tiles <= 32 && B * columns >= 128);
   bool own;                                         // each wave has a column of its own
-  if (p.solo) own = (tiles <= 4 && B * columns >= 512) || (tiles <= 8 && B * columns >= 2048);      // 820 columns of 1 to 3 tokens, head_dim 256, 26 -> 8 us
+  // Short tables: 820 columns of 1 to 3 tokens, head_dim 256, 26 -> 8 us.  Over 128 a CU has one workgroup, so the waves' getting ready and putting
+  // together are not hidden by others'; 512 and 1024 columns of 60 to 120 tokens 19.4 -> 16.8, 37.4 -> 23.7; 512 of 130 to 250 28.4 -> 36.3,
+  // 1000 of 53 to 252 51 -> 40; 768 and 1024 of 300 to 500 66 -> 70, 86.9 -> 78.4; MXFP8 of 100 to 400 52.9 -> 38.3 us
+  const bool alone = cache.head_dim > 128;
+  if (p.solo) own = (tiles <= 4 && B * columns >= 512) || (tiles <= 8 && B * columns >= (alone ? 512 : 2048)) || (alone && B * columns > 768);
   else if (row_groups_of(cache, heads, B) > 1) own = B * columns >= 64;  // two columns of 16, 8 key heads, 1, 4, 16 requests: 12.5 -> 15.7, 33.8 -> 28.9, 102 -> 80 us
-  else own = columns % ATT_WAVES == 0 && heads / cache.heads <= 2 && B * columns >= ATT_WAYS_ITEMS;
+  else own = columns % ATT_WAVES == 0 && (alone || heads / cache.heads <= 2) && B * columns >= ATT_WAYS_ITEMS;
   p.ways = own ? 1 : ATT_WAVES;
   // workgroups: three, two or one for each CU by the registers that a wave takes.  head_dim 64 with 512, 768, 1024: 64 requests of 100 to
   // 3000 tokens 52.3, 50.1, 49.6 us, 16 long ones 34.6, 35.4, 35.8; 128: 16 58.3, 59.4, 64.6; 256 with 256, 512, 768: 64.9, 72.6, 79.9
