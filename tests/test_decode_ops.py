@@ -692,6 +692,14 @@ def test_caches_that_are_refused(changed):
     assert L.torq_paged_attention_workspace_bytes(bad, 8, 2, 4) == 0
 
 
+def test_attention_workspace_stays_within_its_documented_bound():
+    need = binding.lib().torq_paged_attention_workspace_bytes
+    sizes = [need(C.byref(cache_struct(heads=kv, head_dim=dim)), kv * group, B, width)
+             for kv in (1, 3, 8, 20, 64) for dim in (8, 64, 72, 128, 136, 256) for group in (1, 2, 3, 16, 17, 32, 33, 71)
+             for B in (0, 1, 5, 31, 32, 77, 300) for width in (0, 1, 32, 33, 64, 65, 999, 2000)]
+    assert 0 < max(sizes) <= 66 << 20 and all(n % 16 == 0 for n in sizes)
+
+
 def test_decode_calls_reject_bad_arguments_without_launching():
     L, p, odd, odd2 = binding.lib(), C.c_void_p(0x1000), C.c_void_p(0x1004), C.c_void_p(0x1002)
     E, A, OK = binding.TORQ_EINVAL, binding.TORQ_EALIGN, binding.TORQ_OK
