@@ -724,7 +724,8 @@ class KVCache:
     """A paged cache of keys and values: k and v [pages, heads, page_size, head_dim], bf16 or float8_e4m3fn, the latter with scales
     [pages, heads, page_size, head_dim / 32] float8_e8m0fnu (or the same bytes as uint8).  k and v may be views, with a page's
     tokens ahead of its heads or the two in one tensor, but lie alike; the scales lie like the elements.  The tensors are the
-    caller's: the cache keeps them alive, and what they hold may change at any time."""
+    caller's: the cache keeps them alive, and what they hold may change at any time.  The calls below take caches on the GPU of their
+    other tensors only."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales=None, v_scales=None):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.dtype not in (torch.bfloat16, _E4M3):
@@ -748,7 +749,8 @@ class KVCache:
         self.format = TORQ_FMT_MXFP8 if mx else TORQ_FMT_BF16
         self._struct = _KVCacheStruct(k.data_ptr(), v.data_ptr(), *((t.data_ptr() for t in scales) if mx else (None, None)),
                                       pages, *strides[:3], self.format, self.heads, self.head_dim, self.page_size)
-        self.kv_handle = C.c_void_p(C.addressof(self._struct))
+        # what the calls go by; on the host there is nothing that a kernel could be given
+        self.kv_handle, self.kv_device = (C.c_void_p(C.addressof(self._struct)), k.get_device()) if k.is_cuda else (None, -1)
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_size: int, head_dim: int, fmt: int = TORQ_FMT_BF16, device="cuda"):
@@ -759,6 +761,13 @@ class KVCache:
             raise ValueError("a cache is TORQ_FMT_BF16, or TORQ_FMT_MXFP8 with a head_dim that is a multiple of 32")
         return cls(*(torch.empty((pages, heads, page_size, n), dtype=t, device=device)
                      for t, n in ((_E4M3, head_dim), (_E8M0, head_dim // 32)) for _ in "kv"))
+
+
+def _kv(cache: KVCache, with_it: torch.Tensor, what):
+    """The handle of a cache that lies on the GPU, on the same one as the tensor that it is used with."""
+    if cache.kv_handle is None or cache.k.device != with_it.device:
+        raise ValueError(f"cache: its keys and values are on {cache.k.device}, {what} is on {with_it.device}; expected one GPU for both")
+    return cache.kv_handle
 
 
 def torq_block_tables(held, lengths, free_pages, cursor, block_tables, page_size: int, tokens: int, slots=None, cursor_out=None,
@@ -789,16 +798,17 @@ def torq_cache_append(cache: KVCache, key, value, slots, stream=None):
     """key and value [tokens, heads, head_dim] bf16 (views of a projection's output will do) to the cache's slots [tokens] int64."""
     if (_host or _native()).cache_append(cache, key, value, slots, stream):
         return
+    handle = _kv(cache, key, "key")
     T = slots.numel()
     if key.shape != (T, cache.heads, cache.head_dim) or value.shape != key.shape or slots.dim() != 1:
         raise ValueError("key and value must be [tokens, heads, head_dim], slots [tokens]")
     at = lambda t: [st if n > 1 else 0 for n, st in zip(t.shape[:2], t.stride())]
-    _check(lib().torq_cache_append(cache.kv_handle, _rows(key, torch.bfloat16, 3, "key"), *at(key), _rows(value, torch.bfloat16, 3, "value"),
+    _check(lib().torq_cache_append(handle, _rows(key, torch.bfloat16, 3, "key"), *at(key), _rows(value, torch.bfloat16, 3, "value"),
                                    *at(value), _dev(slots, torch.int64, "slots"), T, _stream(stream)), "torq_cache_append")
 
 
 def torq_paged_attention_workspace_bytes(cache: KVCache, heads: int, B: int, width: int) -> int:
-    return int(lib().torq_paged_attention_workspace_bytes(cache.kv_handle, heads, B, width))
+    return int(lib().torq_paged_attention_workspace_bytes(C.addressof(cache._struct), heads, B, width))
 
 
 def torq_paged_attention(q, cache: KVCache, block_tables, lengths, scale: float, out=None, workspace=None, stream=None):
@@ -807,6 +817,7 @@ def torq_paged_attention(q, cache: KVCache, block_tables, lengths, scale: float,
     y = (_host or _native()).paged_attention(q, cache, block_tables, lengths, scale, out, workspace, stream)
     if y is not None:
         return y
+    handle = _kv(cache, q, "q")
     B, heads, dim = q.shape
     width = block_tables.shape[-1]
     if dim != cache.head_dim or block_tables.shape != (B, width) or lengths.shape != (B,):
@@ -818,7 +829,7 @@ def torq_paged_attention(q, cache: KVCache, block_tables, lengths, scale: float,
     if out.shape != q.shape:
         raise ValueError("out must be [B, heads, head_dim]")
     at = [st if n > 1 else 0 for n, st in zip(q.shape[:2], q.stride())]
-    _check(lib().torq_paged_attention(cache.kv_handle, _rows(q, torch.bfloat16, 3, "q"), *at, heads,
+    _check(lib().torq_paged_attention(handle, _rows(q, torch.bfloat16, 3, "q"), *at, heads,
                                       _rows(block_tables, torch.int32, 2, "block_tables"), block_tables.stride(0) if B > 1 else width,
                                       width, _dev(lengths, torch.int32, "lengths"), B, float(scale), _dev(out, torch.bfloat16, "out"),
                                       _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)),

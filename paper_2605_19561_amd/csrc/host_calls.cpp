@@ -42,7 +42,7 @@ decltype(&torq_paged_attention) f_attention;
 decltype(&torq_paged_attention_workspace_bytes) f_attention_bytes;
 decltype(&torq_add_rms_norm) f_norm;
 PyObject *py_stream, *py_check;
-PyObject *s_handle, *s_kv_handle, *s_value, *s_d;
+PyObject *s_handle, *s_kv_handle, *s_kv_device, *s_value, *s_d;
 
 struct NotPlain {};
 
@@ -264,9 +264,11 @@ double number(PyObject *o) {
   if (!PyFloat_CheckExact(o)) throw NotPlain{};
   return PyFloat_AS_DOUBLE(o);
 }
-const torq_kv_cache_t *cache_of(PyObject *cache) {
+// a cache on the GPU of the tensor that it is used with (one on the host has no handle)
+const torq_kv_cache_t *cache_of(PyObject *cache, const Tensor &with_it) {
   const torq_kv_cache_t *c = static_cast<const torq_kv_cache_t *>(handle_of(cache, s_kv_handle));
-  if (!c) throw NotPlain{};
+  Ref device(PyObject_GetAttr(cache, s_kv_device));
+  if (!c || integer(device.p) != with_it.get_device()) throw NotPlain{};
   return c;
 }
 PyObject *packed(std::initializer_list<PyObject *> items) {
@@ -318,8 +320,8 @@ PyObject *block_tables(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return plain_or_none([&]() -> PyObject * {
     if (n != 5) throw NotPlain{};
-    const torq_kv_cache_t *const cache = cache_of(a[0]);
     const Tensor &key = tensor(a[1]), &value = tensor(a[2]), &slots = tensor(a[3]);
+    const torq_kv_cache_t *const cache = cache_of(a[0], key);
     const void *const kp = rows(key, at::kBFloat16, 3), *const vp = rows(value, at::kBFloat16, 3);
     const int64_t *const sp = static_cast<const int64_t *>(address(slots, at::kLong)), T = slots.numel();
     shape(slots, {T});
@@ -341,7 +343,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return plain_or_none([&]() -> PyObject * {
     if (n != 8) throw NotPlain{};
     const Tensor &q = tensor(a[0]), &tables = tensor(a[2]), &lengths = tensor(a[3]);
-    const torq_kv_cache_t *const cache = cache_of(a[1]);
+    const torq_kv_cache_t *const cache = cache_of(a[1], q);
     const float scale = (float)number(a[4]);
     const Tensor *out_in = optional(a[5]), *ws_in = optional(a[6]);
     const void *const qp = rows(q, at::kBFloat16, 3);
@@ -459,9 +461,10 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, null
 PyMODINIT_FUNC PyInit__host() {
   s_handle = PyUnicode_InternFromString("handle");
   s_kv_handle = PyUnicode_InternFromString("kv_handle");
+  s_kv_device = PyUnicode_InternFromString("kv_device");
   s_value = PyUnicode_InternFromString("value");
   s_d = PyUnicode_InternFromString("d");
-  if (!s_handle || !s_kv_handle || !s_value || !s_d) return nullptr;
+  if (!s_handle || !s_kv_handle || !s_kv_device || !s_value || !s_d) return nullptr;
   PyObject *m = PyModule_Create(&module);
   // (binding.py binds no module built against another torch)
   if (m && PyModule_AddStringConstant(m, "torch_version", TORQ_TORCH_VERSION) != 0) Py_CLEAR(m);

@@ -1,0 +1,74 @@
+"""Where the calls of the attention side of a decoder block end: caches that no kernel may be given, places that may not be shared, sizes of a
+launch, counts past 32 bits, and values at the ends of their types."""
+import types
+
+import pytest
+import torch
+
+from paper_2605_19561_amd import binding
+
+DEV = "cuda:0"
+BF, F8, E8 = torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(params=["native", "interpreted"])
+def either_way(request, monkeypatch):
+    """The binding's C++ module, and its own Python in the place of that."""
+    if request.param == "interpreted":
+        monkeypatch.setattr(binding, "_host", binding._Interpreted)
+    return request.param
+
+
+def calls_with(cache, device):
+    """The two calls that take a cache, all their other arguments in order."""
+    x = torch.zeros((3, 2, 64), dtype=BF, device=device)
+    i = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)
+    return {"append": lambda: binding.torq_cache_append(cache, x, x, torch.full((3,), -1, dtype=torch.int64, device=device)),
+            "attention": lambda: binding.torq_paged_attention(x, cache, i(3, 2), i(3), 1.0, out=torch.zeros_like(x),
+                                                              workspace=torch.zeros(1 << 20, dtype=torch.uint8, device=device))}
+
+
+def host_cache():
+    return binding.KVCache(*(torch.zeros((4, 2, 16, 64), dtype=BF) for _ in "kv"))
+
+
+def cache_elsewhere(cache):
+    """The same one as if it lay on another GPU."""
+    there = torch.device("cuda", 1)
+    return types.SimpleNamespace(kv_handle=cache.kv_handle, kv_device=1, k=types.SimpleNamespace(device=there), _struct=cache._struct,
+                                 format=cache.format, heads=cache.heads, head_dim=cache.head_dim, page_size=cache.page_size)
+
+
+@pytest.mark.parametrize("call", ["append", "attention"])
+@pytest.mark.parametrize("elsewhere", [False, True])
+def test_no_kernel_is_given_a_cache_of_the_host_or_of_another_device(monkeypatch, call, elsewhere):
+    # every other argument passes as if it were on the device, and the library is one that takes note of its calls
+    launched = []
+    note = lambda *args: launched.append(args) or 0
+    cache = cache_elsewhere(host_cache()) if elsewhere else host_cache()
+    if elsewhere:
+        cache.kv_handle = 0x1000
+    monkeypatch.setattr(binding, "_host", binding._Interpreted)
+    monkeypatch.setattr(binding, "_dev", lambda t, dtype, what: t.data_ptr())
+    monkeypatch.setattr(binding, "_rows", lambda t, dtype, dims, what: t.data_ptr())
+    monkeypatch.setattr(binding, "_stream", lambda stream=None: 0)
+    monkeypatch.setattr(binding, "lib", lambda: types.SimpleNamespace(torq_cache_append=note, torq_paged_attention=note))
+    with pytest.raises(ValueError, match="cache"):
+        calls_with(cache, "cpu")[call]()
+    assert not launched
+
+
+@gpu
+@pytest.mark.parametrize("call", ["append", "attention"])
+def test_device_tensors_with_a_cache_of_the_host_or_of_another_device(either_way, call):
+    with pytest.raises(ValueError, match="cache"):
+        calls_with(host_cache(), DEV)[call]()
+    here = binding.KVCache(*(torch.zeros((4, 2, 16, 64), dtype=BF, device=DEV) for _ in "kv"))
+    calls_with(here, DEV)[call]()
+    with pytest.raises(ValueError, match="cache"):
+        calls_with(cache_elsewhere(here), DEV)[call]()
+
+
+def test_workspace_sizes_need_no_cache_on_the_gpu():
+    assert binding.torq_paged_attention_workspace_bytes(host_cache(), 8, 3, 4000) > 0
