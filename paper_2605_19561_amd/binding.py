@@ -724,8 +724,13 @@ class KVCache:
     """A paged cache of keys and values: k and v [pages, heads, page_size, head_dim], bf16 or float8_e4m3fn, the latter with scales
     [pages, heads, page_size, head_dim / 32] float8_e8m0fnu (or the same bytes as uint8).  k and v may be views, with a page's
     tokens ahead of its heads or the two in one tensor, but lie alike; the scales lie like the elements.  The tensors are the
-    caller's: the cache keeps them alive, and what they hold may change at any time.  The calls below take caches on the GPU of their
-    other tensors only."""
+    caller's: the cache keeps them alive, and what they hold may change at any time, but not where they lie: the calls go by the addresses
+    of the construction, and other tensors take a KVCache of their own.  The calls below take caches on the GPU of their other tensors
+    only."""
+
+    k, v, k_scales, v_scales = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
+    format, heads, head_dim, page_size = (property(lambda self, name=name: getattr(self._struct, name))
+                                          for name in ("format", "heads", "head_dim", "page_size"))
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales=None, v_scales=None):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.dtype not in (torch.bfloat16, _E4M3):
@@ -744,11 +749,10 @@ class KVCache:
                 raise ValueError("scales must be [pages, heads, page_size, head_dim / 32], float8_e8m0fnu or uint8")
             if not alike(t, 32) or (t.shape[3] > 1 and t.stride(3) != 1):
                 raise ValueError("scales must lie like the elements, a 32nd of the strides")
-        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
-        pages, self.heads, self.page_size, self.head_dim = k.shape
-        self.format = TORQ_FMT_MXFP8 if mx else TORQ_FMT_BF16
+        self._tensors = k, v, k_scales, v_scales
+        pages, heads, page_size, head_dim = k.shape
         self._struct = _KVCacheStruct(k.data_ptr(), v.data_ptr(), *((t.data_ptr() for t in scales) if mx else (None, None)),
-                                      pages, *strides[:3], self.format, self.heads, self.head_dim, self.page_size)
+                                      pages, *strides[:3], TORQ_FMT_MXFP8 if mx else TORQ_FMT_BF16, heads, head_dim, page_size)
         # what the calls go by; on the host there is nothing that a kernel could be given
         self.kv_handle, self.kv_device = (C.c_void_p(C.addressof(self._struct)), k.get_device()) if k.is_cuda else (None, -1)
 

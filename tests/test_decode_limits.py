@@ -72,3 +72,15 @@ def test_device_tensors_with_a_cache_of_the_host_or_of_another_device(either_way
 
 def test_workspace_sizes_need_no_cache_on_the_gpu():
     assert binding.torq_paged_attention_workspace_bytes(host_cache(), 8, 3, 4000) > 0
+
+
+def test_a_cache_cannot_be_given_other_tensors():
+    # the calls go by the addresses that it was made with: with another k in its place they would use the old one, freed
+    cache = host_cache()
+    k, other = cache.k, torch.zeros((4, 2, 16, 64), dtype=BF)
+    for name, value in (("k", other), ("v", other), ("k_scales", None), ("v_scales", None), ("heads", 1), ("head_dim", 32), ("page_size", 32),
+                        ("format", binding.TORQ_FMT_MXFP8)):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, value)
+    assert cache.k is k and cache.k_scales is None and (cache.heads, cache.head_dim, cache.page_size) == (2, 64, 16)
+    assert cache._struct.k == k.data_ptr()
