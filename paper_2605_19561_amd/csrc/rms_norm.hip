@@ -110,7 +110,7 @@ hipError_t launch_add_rms_norm(const void *x, const void *residual, const void *
     constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value, WG = TPR > 256 ? TPR : 256, ROWS = WG / TPR;
     auto kernel = format == FMT_BF16 ? (once ? add_rms_norm_kernel<TPR, CH, FMT_BF16, true> : add_rms_norm_kernel<TPR, CH, FMT_BF16, false>)
                                      : (once ? add_rms_norm_kernel<TPR, CH, FMT_MXFP8, true> : add_rms_norm_kernel<TPR, CH, FMT_MXFP8, false>);
-    constexpr int64_t MOST = (int64_t)1 << 30;      // rows of one launch (the grid's limit is 2^31 - 1)
+    constexpr int64_t MOST = most_workgroups(WG) * ROWS;       // rows of one launch
     for (int64_t m = 0; m < M; m += MOST) {
       const int64_t rows = M - m < MOST ? M - m : MOST;
       const size_t at = (size_t)m * d * 2;

@@ -63,6 +63,9 @@ constexpr double ONE_PASS_LINEAR_INPUT_BYTES = 96.0 * 1024 * 1024;
 // 44.6 / 39.7, 36.8 / 38.9.  (From HBM layers of 4 to 70 MB would gain 3 - 10 % too; smaller models have theirs in the cache.)
 constexpr double ONE_PASS_WEIGHT_BYTES = 96.0 * 1024 * 1024;
 
+// The runtime takes no launch whose workgroups times threads reach 2^32 along a dimension of the grid: the most workgroups of `threads`.
+constexpr int64_t most_workgroups(int64_t threads) { return 0xFFFFFFFF / threads; }
+
 // Raises a kernel's dynamic LDS limit to `bytes`, once for each device it is launched on (the limit belongs to
 // the function on one device, and the call is slow).  `raised`: the caller's, one per kernel, a bit a device;
 // a failed call leaves the bit clear, so the next launch tries again.

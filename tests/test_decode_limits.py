@@ -1,11 +1,17 @@
 """Where the calls of the attention side of a decoder block end: caches that no kernel may be given, places that may not be shared, sizes of a
 launch, counts past 32 bits, and values at the ends of their types."""
+import json
+import os
+import subprocess
+import sys
+import textwrap
 import types
 
 import pytest
 import torch
 
-from paper_2605_19561_amd import binding
+from paper_2605_19561_amd import binding, build
+from test_launch_host import STUB
 
 DEV = "cuda:0"
 BF, F8, E8 = torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu
@@ -84,3 +90,83 @@ def test_a_cache_cannot_be_given_other_tensors():
             setattr(cache, name, value)
     assert cache.k is k and cache.k_scales is None and (cache.heads, cache.head_dim, cache.page_size) == (2, 64, 16)
     assert cache._struct.k == k.data_ptr()
+
+
+# ---- sizes of a launch -------------------------------------------------------------------------
+# The runtime refuses launches whose workgroups times threads reach 2^32 along a dimension.  A stand-in for it takes note of what is asked
+# of it; addresses are made up, and nothing goes to them.
+
+@pytest.fixture(scope="module")
+def stand_in(tmp_path_factory):
+    tmp = tmp_path_factory.mktemp("stub")
+    taken = "hipError_t hipLaunchKernel(const void *f, dim3 g, dim3, void **, size_t lds, hipStream_t) {"
+    noted = "hipError_t hipLaunchKernel(const void *f, dim3 g, dim3 b, void **args, size_t lds, hipStream_t) {\n" \
+            '  fprintf(events, "{\\"threads\\": %u, \\"fourth\\": %lld}\\n", b.x, *(long long *)args[fourth]);'
+    assert taken in STUB
+    source = STUB.replace(taken, noted).replace('extern "C" {', 'static int fourth = 0;\nextern "C" {\nvoid stub_argument(int n) { fourth = n; }', 1)
+    src, so = str(tmp / "stub.cpp"), str(tmp / "libstub.so")
+    open(src, "w").write(source)
+    subprocess.run(["g++", "-shared", "-fPIC", "-O1", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", src, "-o", so], check=True)
+    return so
+
+
+@pytest.fixture
+def launches(stand_in, tmp_path):
+    """Runs code with L, the library, and P, an address; returns (workgroups along x and y, threads, the argument that was asked for)."""
+    def run(body, argument=0):
+        if not os.path.exists(build.LIB):
+            build.build()
+        events = str(tmp_path / "events")
+        code = f"""
+import ctypes as C
+stub = C.CDLL({stand_in!r}, mode=C.RTLD_GLOBAL)
+stub.stub_open({events.encode()!r}); stub.stub_argument({argument})
+from paper_2605_19561_amd import binding
+L, P, OK = binding.lib(), C.c_void_p(1 << 20), binding.TORQ_OK
+""" + textwrap.dedent(body) + "\nstub.stub_close()\n"
+        subprocess.run([sys.executable, "-c", code], check=True, timeout=120, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+        lines = [json.loads(line) for line in open(events)]
+        return [(g["grid"], b["threads"], b["fourth"]) for b, g in zip(lines[::2], lines[1::2])]
+    return run
+
+
+@pytest.mark.parametrize("d", [32, 256, 1024, 2048, 8192, 32768])
+def test_norm_launches_stay_within_the_runtimes_limit(launches, d):
+    # (the kernel's fourth argument is its number of rows)
+    sizes = [1, 1000, 1 << 22, 1 << 24, (1 << 28) + 37, 1 << 31]
+    got = launches(f"""
+        for M in {sizes}:
+            assert L.torq_add_rms_norm(P, None, P, M, {d}, 1e-5, 8, None, P, None, None) == OK
+        """, argument=3)
+    assert all(grid[0] * threads < 1 << 32 for grid, threads, _ in got)
+    for M in sizes:
+        rows = 0
+        while rows < M:
+            rows += got.pop(0)[2]
+        assert rows == M
+    assert not got
+
+
+@gpu
+@pytest.mark.parametrize("fmt", [binding.TORQ_FMT_BF16, binding.TORQ_FMT_MXFP8])
+def test_norm_of_more_rows_than_one_launch_takes(fmt):
+    M, d, step = (1 << 28) + 37, 32, 1 << 25          # 16 rows a workgroup, 2^24 workgroups and some
+    weight = (1 + 0.25 * torch.randn(d, device=DEV)).to(BF)
+    x = torch.empty((M, d), dtype=BF, device=DEV)
+    for i in range(0, M, step):
+        x[i:i + step].normal_()
+    # the same rows by calls that a launch takes whole
+    want = []
+    for i in range(0, M, step):
+        want.append(binding.torq_add_rms_norm(x[i:i + step], None, weight, 1e-5, fmt)[:2])
+    out, scales, _ = binding.torq_add_rms_norm(x, None, weight, 1e-5, fmt, out=x if fmt == binding.TORQ_FMT_BF16 else None)
+    for n, (o, s) in enumerate(want):
+        rows = slice(n * step, (n + 1) * step)
+        assert torch.equal(out[rows].view(torch.uint8), o.view(torch.uint8)), n
+        assert s is None or torch.equal(scales[rows].view(torch.uint8), s.view(torch.uint8)), n
+    # and the last of them against the formula
+    if fmt == binding.TORQ_FMT_MXFP8:
+        tail = x[-100:].double()
+        y = tail / (tail.pow(2).mean(-1, keepdim=True) + 1e-5).sqrt() * weight.double()
+        unit = 2.0 ** (scales[-100:].view(torch.uint8).double() - 127)
+        assert ((out[-100:].double() * unit - y).abs() <= (2.0 ** -4 + 2.0 ** -15) * y.abs() + unit * 2.0 ** -10).all()
