@@ -628,7 +628,8 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   // 7.2 us; up to 1000 tokens, 8 key heads, 1, 4, 16, 64, 256 requests in runs / a workgroup each: 10.1 / 12.8, 13.8 / 14.7, 20.4 / 15.5,
   // 49.8 / 44.2, 175 / 165 us, ragged (1 to 1000) 4, 16, 64 of them 10.9 / 13.2, 16.3 / 14.6, 32.5 / 32.9; up to 2000, ragged, 64 of
   // them 52.5 / 61.5
-  p.solo = tiles <= 16 || (tiles <= 32 && B * columns >= 128);
+  // (and within a launch, which runs always are)
+  p.solo = (tiles <= 16 || (tiles <= 32 && B * columns >= 128)) && B * columns <= most_workgroups(256);
   bool own;                                         // each wave has a column of its own
   // Short tables: 820 columns of 1 to 3 tokens, head_dim 256, 26 -> 8 us.  Over 128 a CU has one workgroup, so the waves' getting ready and putting
   // together are not hidden by others'; 512 and 1024 columns of 60 to 120 tokens 19.4 -> 16.8, 37.4 -> 23.7; 512 of 130 to 250 28.4 -> 36.3,

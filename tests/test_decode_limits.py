@@ -170,3 +170,32 @@ def test_norm_of_more_rows_than_one_launch_takes(fmt):
         y = tail / (tail.pow(2).mean(-1, keepdim=True) + 1e-5).sqrt() * weight.double()
         unit = 2.0 ** (scales[-100:].view(torch.uint8).double() - 127)
         assert ((out[-100:].double() * unit - y).abs() <= (2.0 ** -4 + 2.0 ** -15) * y.abs() + unit * 2.0 ** -10).all()
+
+
+@pytest.mark.parametrize("kv_heads,heads,dim", [(1, 1, 8), (1, 24, 64), (1, 40, 256), (4, 8, 128)])
+def test_attention_launches_stay_within_the_runtimes_limit(launches, kv_heads, heads, dim):
+    # with tables of a page, of 16 tiles and of 32, as many requests as the call takes and about as many as a launch
+    got = launches(f"""
+        asked = 0
+        for width in (1, 32, 64):
+            columns = {kv_heads} * -(-({heads} // {kv_heads}) // 16)
+            most = min(0x7FFFFFFF // {heads}, 0x7FFFFFFF // (width // 2 + 8) // columns)
+            for B in (most, (1 << 24) // columns, (1 << 24) // columns - 1, (1 << 22) + 3):
+                cache = binding._KVCacheStruct(P, P, None, None, 10, {kv_heads} * 16 * {dim}, 16 * {dim}, {dim}, 8, {kv_heads}, {dim}, 16)
+                need = L.torq_paged_attention_workspace_bytes(C.byref(cache), {heads}, min(B, most), width)
+                status = L.torq_paged_attention(C.byref(cache), P, 128, 128, {heads}, P, width, width, P, min(B, most), 1.0, P, P, need, None)
+                assert status == OK
+        """)
+    assert len(got) >= 12 and all(grid[0] * threads < 1 << 32 for grid, threads, _ in got)
+
+
+@gpu
+def test_attention_of_more_requests_than_one_launch_takes_workgroups():
+    # a request's only token, or none: its output is that token's value
+    B, pages = (1 << 24) + 5, 3
+    cache = binding.KVCache(*(torch.randn((pages, 1, 16, 8), device=DEV).to(BF) for _ in "kv"))
+    tables = torch.randint(0, pages, (B, 1), dtype=torch.int32, device=DEV)
+    lengths = torch.randint(0, 2, (B,), dtype=torch.int32, device=DEV)
+    q = torch.randn((B, 1, 8), dtype=BF, device=DEV)
+    got = binding.torq_paged_attention(q, cache, tables, lengths, 1.0)
+    assert torch.equal(got[:, 0], cache.v[:, 0, 0][tables[:, 0].long()] * lengths[:, None])
