@@ -635,8 +635,20 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   // together are not hidden by others'; 512 and 1024 columns of 60 to 120 tokens 19.4 -> 16.8, 37.4 -> 23.7; 512 of 130 to 250 28.4 -> 36.3,
   // 1000 of 53 to 252 51 -> 40; 768 and 1024 of 300 to 500 66 -> 70, 86.9 -> 78.4; MXFP8 of 100 to 400 52.9 -> 38.3 us
   const bool alone = cache.head_dim > 128;
-  if (p.solo) own = (tiles <= 4 && B * columns >= 512) || (tiles <= 8 && B * columns >= (alone ? 512 : 2048)) || (alone && B * columns > 768);
-  else if (row_groups_of(cache, heads, B) > 1) own = B * columns >= 64;  // two columns of 16, 8 key heads, 1, 4, 16 requests: 12.5 -> 15.7, 33.8 -> 28.9, 102 -> 80 us
+  // A workgroup's waves have columns of one request, so that some have none where those are no multiple of four.  All four / one each, us: 4096
+  // columns of 60 to 256 tokens, head_dim 128, one key head 65 / 102 (MXFP8 53 / 106), two 65 / 72 (53 / 64), five 65 / 89 (53 / 61), three 64 / 67
+  // (53 / 52, up to 160 tokens 45 / 40); head_dim 256, one 188 / 225, two 188 / 163 (MXFP8 155 / 111), three 185 / 148 (153 / 93), five 186 / 189 (153 /
+  // 112); 1024 of 300 to 1000 tokens, head_dim 256, one 139 / 188 (96 / 176), two 143 / 149 (96 / 115), three 138 / 169 (94 / 125)
+  const int64_t idle = -columns & (ATT_WAVES - 1);
+  auto busy = [&](int eighths) { return 8 * columns >= eighths * (columns + idle); };
+  const bool mx = cache.format == FMT_MXFP8;
+  if (p.solo)
+    own = (tiles <= 8 && (alone ? columns > 1 && B * columns >= 512 : busy(6) && B * columns >= (tiles <= 4 ? 512 : 2048))) ||
+          (alone && busy(7) && B * columns > 768);
+  // Two columns of 16, 8 key heads, 1, 4, 16 requests: 12.5 -> 15.7, 33.8 -> 28.9, 102 -> 80 us.  In MXFP8, where it is the vector instructions that
+  // idle waves leave to others: 64 and 128 requests of 1000 to 4000, 24 query heads of 256 for one key head 39 -> 49, 66 -> 93, 40 of 128 31 -> 39,
+  // 44 -> 62, for three 59 -> 70, 87 -> 121; of 256 for three 88 -> 105, but from 128 requests on 184 -> 174
+  else if (row_groups_of(cache, heads, B) > 1) own = !mx || busy(7) ? B * columns >= 64 : alone && columns > 2 && B * columns >= ATT_WAYS_ITEMS;
   else own = columns % ATT_WAVES == 0 && (alone || heads / cache.heads <= 2) && B * columns >= ATT_WAYS_ITEMS;
   p.ways = own ? 1 : ATT_WAVES;
   // workgroups: three, two or one for each CU by the registers that a wave takes.  head_dim 64 with 512, 768, 1024: 64 requests of 100 to

@@ -112,7 +112,8 @@ def stand_in(tmp_path_factory):
 
 @pytest.fixture
 def launches(stand_in, tmp_path):
-    """Runs code with L, the library, and P, an address; returns (workgroups along x and y, threads, the argument that was asked for)."""
+    """Runs code with L, the library, and P, an address; returns (workgroups along x and y, threads, the argument that was asked for, the
+    kernel)."""
     def run(body, argument=0):
         if not os.path.exists(build.LIB):
             build.build()
@@ -126,7 +127,7 @@ L, P, OK = binding.lib(), C.c_void_p(1 << 20), binding.TORQ_OK
 """ + textwrap.dedent(body) + "\nstub.stub_close()\n"
         subprocess.run([sys.executable, "-c", code], check=True, timeout=120, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
         lines = [json.loads(line) for line in open(events)]
-        return [(g["grid"], b["threads"], b["fourth"]) for b, g in zip(lines[::2], lines[1::2])]
+        return [(g["grid"], b["threads"], b["fourth"], g["launch"]) for b, g in zip(lines[::2], lines[1::2])]
     return run
 
 
@@ -138,7 +139,7 @@ def test_norm_launches_stay_within_the_runtimes_limit(launches, d):
         for M in {sizes}:
             assert L.torq_add_rms_norm(P, None, P, M, {d}, 1e-5, 8, None, P, None, None) == OK
         """, argument=3)
-    assert all(grid[0] * threads < 1 << 32 for grid, threads, _ in got)
+    assert all(grid[0] * threads < 1 << 32 for grid, threads, *_ in got)
     for M in sizes:
         rows = 0
         while rows < M:
@@ -186,7 +187,7 @@ def test_attention_launches_stay_within_the_runtimes_limit(launches, kv_heads, h
                 status = L.torq_paged_attention(C.byref(cache), P, 128, 128, {heads}, P, width, width, P, min(B, most), 1.0, P, P, need, None)
                 assert status == OK
         """)
-    assert len(got) >= 12 and all(grid[0] * threads < 1 << 32 for grid, threads, _ in got)
+    assert len(got) >= 12 and all(grid[0] * threads < 1 << 32 for grid, threads, *_ in got)
 
 
 @gpu
@@ -199,3 +200,33 @@ def test_attention_of_more_requests_than_one_launch_takes_workgroups():
     q = torch.randn((B, 1, 8), dtype=BF, device=DEV)
     got = binding.torq_paged_attention(q, cache, tables, lengths, 1.0)
     assert torch.equal(got[:, 0], cache.v[:, 0, 0][tables[:, 0].long()] * lengths[:, None])
+
+
+def attention_kernels(launches, cases):
+    """The kernel of each call: cases of (kv_heads, heads, head_dim, requests, tokens that the tables hold, format)."""
+    return [kernel for _, _, _, kernel in launches(f"""
+        for kv, heads, dim, B, tokens, fmt in {cases}:
+            cache = binding._KVCacheStruct(P, P, P, P, 10, kv * 16 * dim, 16 * dim, dim, fmt, kv, dim, 16)
+            need = L.torq_paged_attention_workspace_bytes(C.byref(cache), heads, B, tokens // 16)
+            assert L.torq_paged_attention(C.byref(cache), P, dim, dim, heads, P, tokens // 16, tokens // 16, P, B, 1.0, P, P, need, None) == OK
+        """)]
+
+
+@pytest.mark.parametrize("fmt", [binding.TORQ_FMT_BF16, binding.TORQ_FMT_MXFP8])
+def test_waves_with_columns_of_their_own_have_one(launches, fmt):
+    # tables for up to 512 tokens: a launch a call.  Where a request has one column the waves take turns at it as they do for a single request,
+    # and so they do where it has five for eight waves, but for the shortest of head_dim 256; where its columns are enough each has one
+    for dim in (64, 128, 256):
+        single, *few = attention_kernels(launches, [(1, 8, dim, 1, 512, fmt)] + [(1, 8, dim, 4096, tokens, fmt) for tokens in (128, 256, 512)]
+                                         + [(kv, 8 * kv, dim, 4096, 256 if dim < 256 else 512, fmt) for kv in (2, 5)])
+        assert few == [single] * len(few), dim
+        enough = attention_kernels(launches, [(kv, 8 * kv, dim, 4096, tokens, fmt) for kv in (3, 4, 7, 8, 15, 18) + ((2, 5) if dim == 256 else ())
+                                              for tokens in (64, 128, 256)])
+        assert len(set(enough)) == 1 and enough[0] != single, dim
+
+
+def test_idle_waves_do_not_take_columns_of_mxfp8(launches):
+    # 24 query heads of 256 are two columns: for one key head half of the waves would have none
+    for kv, B, alone in ((1, 128, False), (1, 512, False), (2, 128, True), (3, 32, False), (3, 128, True), (8, 16, True)):
+        single, _, many, _ = attention_kernels(launches, [(1, 8, 256, 1, 4000, 9), (kv, 24 * kv, 256, B, 4000, 9)])
+        assert (many != single) == alone, (kv, B)
