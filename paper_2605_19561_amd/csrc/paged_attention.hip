@@ -632,8 +632,9 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   p.solo = (tiles <= 16 || (tiles <= 32 && B * columns >= 128)) && B * columns <= most_workgroups(256);
   bool own;                                         // each wave has a column of its own
   // Short tables: 820 columns of 1 to 3 tokens, head_dim 256, 26 -> 8 us.  Over 128 a CU has one workgroup, so the waves' getting ready and putting
-  // together are not hidden by others'; 512 and 1024 columns of 60 to 120 tokens 19.4 -> 16.8, 37.4 -> 23.7; 512 of 130 to 250 28.4 -> 36.3,
-  // 1000 of 53 to 252 51 -> 40; 768 and 1024 of 300 to 500 66 -> 70, 86.9 -> 78.4; MXFP8 of 100 to 400 52.9 -> 38.3 us
+  // together are not hidden by others'; but a column a wave for 512 leaves half of the CUs without.  512 of 100 to 128 tokens 20.8 -> 17.5, 120 to
+  // 192 23.8 -> 21.9, 130 to 208 24.5 -> 25.2, 130 to 256 27.5 -> 34.7 (MXFP8 18.2 -> 14.7, 20.9 -> 17.8, -, 21.6 -> 21.1), over two key heads, so 256
+  // workgroups, 24.7 -> 20.4, 29.0 -> 25.6; 640 of 130 to 256 37.5 -> 35.9; 1024 of 300 to 500 87 -> 79, MXFP8 63.5 -> 48.1
   const bool alone = cache.head_dim > 128;
   // A workgroup's waves have columns of one request, so that some have none where those are no multiple of four.  All four / one each, us: 4096
   // columns of 60 to 256 tokens, head_dim 128, one key head 65 / 102 (MXFP8 53 / 106), two 65 / 72 (53 / 64), five 65 / 89 (53 / 61), three 64 / 67
@@ -643,8 +644,8 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   auto busy = [&](int eighths) { return 8 * columns >= eighths * (columns + idle); };
   const bool mx = cache.format == FMT_MXFP8;
   if (p.solo)
-    own = (tiles <= 8 && (alone ? columns > 1 && B * columns >= 512 : busy(6) && B * columns >= (tiles <= 4 ? 512 : 2048))) ||
-          (alone && busy(7) && B * columns > 768);
+    own = alone ? (tiles <= (mx || B * (columns + idle) > 512 ? 8 : 6) && columns > 1 && B * columns >= 512) || (busy(7) && B * columns > 768)
+                : tiles <= 8 && busy(6) && B * columns >= (tiles <= 4 ? 512 : 2048);
   // Two columns of 16, 8 key heads, 1, 4, 16 requests: 12.5 -> 15.7, 33.8 -> 28.9, 102 -> 80 us.  In MXFP8, where it is the vector instructions that
   // idle waves leave to others: 64 and 128 requests of 1000 to 4000, 24 query heads of 256 for one key head 39 -> 49, 66 -> 93, 40 of 128 31 -> 39,
   // 44 -> 62, for three 59 -> 70, 87 -> 121; of 256 for three 88 -> 105, but from 128 requests on 184 -> 174

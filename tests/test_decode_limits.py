@@ -230,3 +230,11 @@ def test_idle_waves_do_not_take_columns_of_mxfp8(launches):
     for kv, B, alone in ((1, 128, False), (1, 512, False), (2, 128, True), (3, 32, False), (3, 128, True), (8, 16, True)):
         single, _, many, _ = attention_kernels(launches, [(1, 8, 256, 1, 4000, 9), (kv, 24 * kv, 256, B, 4000, 9)])
         assert (many != single) == alone, (kv, B)
+
+
+def test_512_columns_of_seven_and_eight_tiles_are_no_waves_own(launches):
+    # head_dim 256, bf16: four columns a workgroup would leave half of the CUs without; whether a table has a page to spare says nothing
+    for requests, kv, tokens, fmt, alone in ((64, 8, 192, 8, True), (64, 8, 208, 8, False), (64, 8, 256, 8, False), (64, 8, 272, 8, False),
+                                             (80, 8, 256, 8, True), (256, 2, 256, 8, True), (64, 8, 256, 9, True)):
+        single, *_, kernel = attention_kernels(launches, [(1, 8, 256, 1, 512, fmt), (kv, 4 * kv, 256, requests, tokens, fmt)])
+        assert (kernel != single) == alone, (requests, kv, tokens, fmt)
