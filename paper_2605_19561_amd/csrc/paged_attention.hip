@@ -410,8 +410,9 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
         }
       }
       load_k(next);
-      // p as two bf16 parts, the first cut off and the second rounded: p to 2^-16, so the output's own rounding is the only one to
-      // bf16 that shows.  Both are positive: an infinite v stays infinite (masked tokens have a v of 0 below).
+      // p as two bf16 parts, the first the next below p (its bits less one, cut off) and the second what is left, rounded: p to 2^-16, so the
+      // output's own rounding is the only one to bf16 that shows.  Both are positive where p is, so that an infinite v stays infinite, and
+      // both zero where p is: masked tokens, and weights that are nothing in 32 bits, however large their v.
       u32x4 pt[RT], pt_rest[RT];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
@@ -434,10 +435,9 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
         }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const uint32_t lo = __float_as_uint(p[2 * c]), hi = __float_as_uint(p[2 * c + 1]);
+          const uint32_t lo = __builtin_elementwise_sub_sat(__float_as_uint(p[2 * c]), 1u), hi = __builtin_elementwise_sub_sat(__float_as_uint(p[2 * c + 1]), 1u);
           pt[rt][c] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
-          const bf16x2 rest = {(__bf16)fmaxf(p[2 * c] - __uint_as_float(lo & 0xFFFF0000u), 0x1p-126f),
-                               (__bf16)fmaxf(p[2 * c + 1] - __uint_as_float(hi & 0xFFFF0000u), 0x1p-126f)};
+          const bf16x2 rest = {(__bf16)(p[2 * c] - __uint_as_float(lo & 0xFFFF0000u)), (__bf16)(p[2 * c + 1] - __uint_as_float(hi & 0xFFFF0000u))};
           pt_rest[rt][c] = __builtin_bit_cast(uint32_t, rest);
         }
 #pragma unroll

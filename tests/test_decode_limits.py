@@ -238,3 +238,38 @@ def test_512_columns_of_seven_and_eight_tiles_are_no_waves_own(launches):
                                              (80, 8, 256, 8, True), (256, 2, 256, 8, True), (64, 8, 256, 9, True)):
         single, *_, kernel = attention_kernels(launches, [(1, 8, 256, 1, 512, fmt), (kv, 4 * kv, 256, requests, tokens, fmt)])
         assert (kernel != single) == alone, (requests, kv, tokens, fmt)
+
+
+# ---- values at the ends of their types ---------------------------------------------------------
+
+def two_tokens(score, value, dim=64):
+    """The output of a token of score 0 and value 1 beside one of that score and value, one launch and in runs."""
+    k, v = torch.zeros((1, 1, 16, dim), dtype=BF, device=DEV), torch.ones((1, 1, 16, dim), dtype=BF, device=DEV)
+    k[0, 0, 1, 0], v[0, 0, 1] = score, value
+    q = torch.zeros((1, 1, dim), dtype=BF, device=DEV)
+    q[0, 0, 0] = 1
+    two = torch.tensor([2], dtype=torch.int32, device=DEV)
+    outs = [binding.torq_paged_attention(q, binding.KVCache(k, v), torch.zeros((1, width), dtype=torch.int32, device=DEV), two, 1.0) for width in (1, 200)]
+    assert torch.equal(*outs) or all(torch.isnan(o).all() for o in outs)
+    assert (outs[0] == outs[0][0, 0, 0]).all() or torch.isnan(outs[0]).all()
+    return float(outs[0][0, 0, 0])
+
+
+@gpu
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("value", [2.0 ** 100, 2.0 ** 118, 2.0 ** 120, 2.0 ** 127, -2.0 ** 127])
+def test_a_weight_of_nothing_leaves_out_values_of_any_size(dim, value):
+    # exp(-300) is nothing in 32 bits (and 1e-130 by the formula): the other token's value alone
+    assert two_tokens(-300.0, value, dim) == 1.0
+    # a weight that is something: p value + 1, to the output's rounding and 2^-16 of the term
+    for score in (-40.0, -60.0, -80.0):
+        p = 2.718281828459045 ** score
+        want, term = (1.0 + p * value) / (1.0 + p), p * abs(value)
+        assert abs(two_tokens(score, value, dim) - want) <= 2.0 ** -8 * abs(want) + (2.0 ** -15 + 2.0 ** -17) * term + 2.0 ** -20
+
+
+@gpu
+@pytest.mark.parametrize("score", [0.0, -1.0, -8.0, -40.0, -80.0])
+def test_an_infinite_value_stays_infinite_under_any_weight(score):
+    # weights with low bits and without (that of score 0 is 1)
+    assert two_tokens(score, float("inf")) == float("inf") and two_tokens(score, -float("inf")) == -float("inf")
