@@ -295,8 +295,8 @@ typedef struct torq_kv_cache {
  *                 is; entries of pages held are read.  A request never has more than `width` pages.
  *   slots         [tokens]: page * page_size + place in it, for each new token, request after request in order; -1 for a
  *                 token without a page and past the last token
- *   cursor_out    *cursor + pages wanted; may be `cursor`.  Above free_count: the list ran out, and the entries that it
- *                 has no page for are -1.
+ *   cursor_out    *cursor + pages wanted, 2^31 - 1 where that is more; may be `cursor`.  Above free_count: the list ran
+ *                 out, and the entries that it has no page for are -1.
  * All arrays on the device.  Nothing is copied to the host, so the call can be captured; `tokens` is the host's bound. */
 int torq_block_tables(const int32_t *held, const int32_t *lengths, int64_t B, const int32_t *free_pages, int64_t free_count,
                       const int32_t *cursor, int32_t *cursor_out, int32_t *block_tables, int64_t table_stride, int width,

@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(256) block_tables_kernel(const int *__restrict
   }
   if (!cursor_only)
     for (int64_t v = tokens_before + gid; v < tokens; v += stride) slots[v] = -1;
-  if (cursor_out && gid == 0) *cursor_out = (int)(first + pages_before);
+  if (cursor_out && gid == 0) *cursor_out = (int)min(first + pages_before, (int64_t)0x7FFFFFFF);
 }
 
 hipError_t launch_block_tables(const int32_t *held, const int32_t *lengths, int64_t B, const int32_t *free_pages,

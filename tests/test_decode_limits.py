@@ -273,3 +273,20 @@ def test_a_weight_of_nothing_leaves_out_values_of_any_size(dim, value):
 def test_an_infinite_value_stays_infinite_under_any_weight(score):
     # weights with low bits and without (that of score 0 is 1)
     assert two_tokens(score, float("inf")) == float("inf") and two_tokens(score, -float("inf")) == -float("inf")
+
+
+# ---- counts past 32 bits -----------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("before,B,width", [(2 ** 31 - 5, 1, 1000), (2 ** 31 - 1, 3, 70), (2 ** 30 + 2 ** 29, 520, 1 << 20), (2 ** 31 - 1, 2, 0)])
+def test_a_cursor_stays_at_the_end_of_its_type(before, B, width, in_place):
+    # pages wanted beyond what 32 bits count: the list has long run out, and says so
+    i32 = dict(dtype=torch.int32, device=DEV)
+    held, lengths, free, cursor = torch.zeros(B, **i32), torch.full((B,), 2 ** 31 - 1, **i32), torch.arange(9, **i32), torch.full((1,), before, **i32)
+    tables = torch.full((B, width), 77, **i32)
+    slots, after = binding.torq_block_tables(held, lengths, free, cursor, tables, 16, 40, cursor_out=cursor if in_place else None)
+    assert after.tolist() == [min(before + B * width, 2 ** 31 - 1)]
+    had = max(0, len(free) - before)
+    assert tables.flatten()[:had].tolist() == list(range(before, before + had)) and (tables.flatten()[had:] == -1).all()
+    assert slots.tolist() == [((before + i // 16) * 16 + i % 16 if i // 16 < had else -1) for i in range(40)]
