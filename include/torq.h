@@ -329,7 +329,7 @@ int torq_paged_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64
 /* Residual addition and root-mean-square norm of rows of d values, d a multiple of 32, at most TORQ_MAX_NORM_D:
  *   s = x + residual,  residual_out = bf16(s),  out = s / sqrt(mean(s^2) + eps) * weight
  * x, residual, weight, residual_out bf16; arithmetic in fp32 on s as it is before its rounding.  residual and
- * residual_out NULL: s = x.  residual_out may be residual or x.
+ * residual_out NULL: s = x.  residual_out may be residual or x.  out and residual_out are two arrays.
  *   out     TORQ_FMT_BF16: [M][d] bf16, what torq_linear reads; may be x.  TORQ_FMT_MXFP8: [M][d] bytes
  *   scales  TORQ_FMT_MXFP8: [M][d/32] bytes; else ignored */
 #define TORQ_MAX_NORM_D 32768

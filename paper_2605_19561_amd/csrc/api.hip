@@ -936,6 +936,7 @@ int torq_add_rms_norm(const void *x_bf16, const void *residual_bf16, const void 
   if (!x_bf16 || !weight_bf16 || !out || (format == TORQ_FMT_MXFP8 && !scales)) return TORQ_EINVAL;
   if (misaligned(x_bf16) || misaligned(residual_bf16) || misaligned(weight_bf16) || misaligned(residual_out_bf16) || misaligned(out))
     return TORQ_EALIGN;
+  if (residual_out_bf16 && out == residual_out_bf16) return TORQ_EINVAL;
   hipError_t e = torq::launch_add_rms_norm(x_bf16, residual_bf16, weight_bf16, M, d, eps, format, residual_out_bf16, out, scales,
                                            (hipStream_t)stream);
   return e == hipSuccess ? TORQ_OK : hip_fail(e);

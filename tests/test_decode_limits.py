@@ -92,6 +92,27 @@ def test_a_cache_cannot_be_given_other_tensors():
     assert cache._struct.k == k.data_ptr()
 
 
+# ---- places that may not be shared -------------------------------------------------------------
+
+def test_the_norms_two_outputs_are_two_arrays(launches):
+    # each would overwrite the other's rows
+    assert len(launches("""
+        P2 = C.c_void_p(1 << 21)
+        call = lambda x, r, ro, out, M=4: L.torq_add_rms_norm(x, r, P, M, 256, 1e-5, 8, ro, out, None, None)
+        assert call(P, P2, P, P) == call(P, P2, P2, P2) == binding.TORQ_EINVAL
+        assert call(P, P2, P2, P) == call(P, P2, P, P2) == call(P, None, None, P) == call(P, P2, P, P, M=0) == OK
+        """)) == 3
+
+
+@gpu
+def test_one_tensor_for_the_norms_two_outputs(either_way):
+    x, r, w = torch.randn((3, 64), device=DEV).to(BF), torch.randn((3, 64), device=DEV).to(BF), torch.ones(64, dtype=BF, device=DEV)
+    before = x.clone()
+    with pytest.raises(binding.TorqError) as e:
+        binding.torq_add_rms_norm(x, r, w, 1e-5, residual_out=x, out=x)
+    assert e.value.status == binding.TORQ_EINVAL and torch.equal(x, before)
+
+
 # ---- sizes of a launch -------------------------------------------------------------------------
 # The runtime refuses launches whose workgroups times threads reach 2^32 along a dimension.  A stand-in for it takes note of what is asked
 # of it; addresses are made up, and nothing goes to them.
