@@ -304,7 +304,8 @@ int torq_block_tables(const int32_t *held, const int32_t *lengths, int64_t B, co
 
 /* key and value [tokens][heads][head_dim] bf16 (strides in elements, multiples of 8, not negative) into the cache: token t at
  * slot slots[t] = page * page_size + place in the page.  A slot outside the cache (-1 among them) is passed over.
- * Two tokens with one slot: either's values, block by block. */
+ * The other slots of a call differ from one another: what two tokens with one slot leave in it is undefined (in MXFP8 a block's elements
+ * and its scale, which are several stores, can be different tokens', so that it has neither's values).  No other slot is touched. */
 int torq_cache_append(const torq_kv_cache_t *cache, const void *key_bf16, int64_t key_token_stride, int64_t key_head_stride,
                       const void *value_bf16, int64_t value_token_stride, int64_t value_head_stride,
                       const int64_t *slots, int64_t tokens, void *stream);

@@ -799,7 +799,8 @@ def torq_block_tables(held, lengths, free_pages, cursor, block_tables, page_size
 
 
 def torq_cache_append(cache: KVCache, key, value, slots, stream=None):
-    """key and value [tokens, heads, head_dim] bf16 (views of a projection's output will do) to the cache's slots [tokens] int64."""
+    """key and value [tokens, heads, head_dim] bf16 (views of a projection's output will do) to the cache's slots [tokens] int64, which
+    differ from one another but for those outside the cache (-1), whose tokens are passed over."""
     if (_host or _native()).cache_append(cache, key, value, slots, stream):
         return
     handle = _kv(cache, key, "key")

@@ -158,7 +158,8 @@ hipError_t launch_block_tables(const int32_t *held, const int32_t *lengths, int6
 // ---- new keys and values -----------------------------------------------------------------------
 // A copy with a place to look up, and to MXFP8 a rounding: HBM-bound, 4 bytes a value to bf16, 3 1/32 to MXFP8.  A lane moves 16
 // consecutive values of a token's head (8 to bf16), so it stores 16 bytes and two lanes have a block of MXFP8; the values and slots of
-// APPEND_PASSES tokens are on their way together.  Measured: [8192 tokens, 8, 128] to MXFP8 10.8 us (4.7 TB/s), to bf16 11.7 (5.7).
+// APPEND_PASSES tokens are on their way together.  (A block's elements and scale are three stores in no order with other workgroups', so a
+// slot named twice is left to no one's values.)  Measured: [8192 tokens, 8, 128] to MXFP8 10.8 us (4.7 TB/s), to bf16 11.7 (5.7).
 struct AppendArgs {
   torq_kv_cache_t cache;
   const uint16_t *key, *value;

@@ -113,6 +113,30 @@ def test_one_tensor_for_the_norms_two_outputs(either_way):
     assert e.value.status == binding.TORQ_EINVAL and torch.equal(x, before)
 
 
+@gpu
+@pytest.mark.parametrize("fmt", [binding.TORQ_FMT_BF16, binding.TORQ_FMT_MXFP8])
+def test_a_slot_named_twice_spoils_no_other(fmt):
+    # what it holds itself is undefined; the slots beside it, and the tokens passed over, are as without it
+    T, heads, dim, pages = 600, 4, 64, 40
+    x = torch.randn((T, 2, heads, dim), device=DEV).to(BF)
+    slots = torch.randperm(pages * 16, device=DEV)[:T]
+    twice, several = slots.clone(), slots[5].clone()
+    twice[300], twice[17], twice[599], twice[100:110] = several, several, several, -1
+    alone = slots.clone()
+    alone[torch.tensor([5, 300, 17, 599] + list(range(100, 110)), device=DEV)] = -1
+
+    def filled(at):
+        cache = binding.KVCache.empty(pages, heads, 16, dim, fmt)
+        arrays = [t for t in (cache.k, cache.v, cache.k_scales, cache.v_scales) if t is not None]
+        for t in arrays:
+            t.view(torch.uint8).fill_(0x33)
+        binding.torq_cache_append(cache, x[:, 0], x[:, 1], at)
+        return [t.view(torch.uint8) for t in arrays]
+    for got, want in zip(filled(twice), filled(alone)):
+        got[several // 16, :, several % 16] = want[several // 16, :, several % 16] = 0
+        assert torch.equal(got, want)
+
+
 # ---- sizes of a launch -------------------------------------------------------------------------
 # The runtime refuses launches whose workgroups times threads reach 2^32 along a dimension.  A stand-in for it takes note of what is asked
 # of it; addresses are made up, and nothing goes to them.
