@@ -318,8 +318,8 @@ int torq_cache_append(const torq_kv_cache_t *cache, const void *key_bf16, int64_
  *                 ceil(heads / cache->heads / 16) * (width * page_size / 32 + 8) below 2^31.  A position past `width` pages counts as past the length; tokens of
  *                 a page outside [0, pages) are left out.  What lies in a page behind the length is not used, NaN or not.
  *   out_bf16      [B][heads][head_dim], contiguous
- *   workspace     16-byte aligned, torq_paged_attention_workspace_bytes() of the same sizes; contents do not matter.  Fewer
- *                 requests or narrower tables can need more, not less; 66 MiB are enough for any call.
+ *   workspace     16-byte aligned, torq_paged_attention_workspace_bytes() of the same sizes; contents do not matter.  The
+ *                 size neither only grows nor only falls with B or width: it is asked for each, or 66 MiB, enough for any call, are kept.
  * Products of bf16 values with fp32 sums (MXFP8 values are bf16 values), softmax statistics in fp32, the weights p as two bf16 parts in
  * the product with v: the output's is the only rounding to bf16.  The same inputs give the same bits.  scale has to be finite.  All pointers 16-byte aligned, tables and lengths 4. */
 size_t torq_paged_attention_workspace_bytes(const torq_kv_cache_t *cache, int heads, int64_t B, int width);

@@ -335,3 +335,13 @@ def test_a_cursor_stays_at_the_end_of_its_type(before, B, width, in_place):
     had = max(0, len(free) - before)
     assert tables.flatten()[:had].tolist() == list(range(before, before + had)) and (tables.flatten()[had:] == -1).all()
     assert slots.tolist() == [((before + i // 16) * 16 + i % 16 if i // 16 < had else -1) for i in range(40)]
+
+
+def test_workspace_sizes_go_up_and_down_with_requests_and_tables():
+    # what the header says of them: a workspace for the largest sizes is not one for all
+    need = binding.lib().torq_paged_attention_workspace_bytes
+    size = lambda B, width, kv=1, dim=64: need(binding.C.byref(binding._KVCacheStruct(1, 1, None, None, 10, kv * 16 * dim, 16 * dim, dim, 8, kv, dim, 16)), kv, B, width)
+    assert size(1, 32) == 0 < size(1, 33) < size(1, 128)                     # a wider table, more
+    assert size(16, 63, 8, 128) == size(16, 64, 8, 128) == 0 < size(16, 65, 8, 128)
+    assert size(15, 64, 8, 128) > size(16, 64, 8, 128)                       # fewer requests, more
+    assert size(1, 65, 8, 128) < size(4, 65, 8, 128) < size(300, 65, 8, 128) <= 66 << 20
