@@ -320,7 +320,8 @@ int torq_cache_append(const torq_kv_cache_t *cache, const void *key_bf16, int64_
  *   out_bf16      [B][heads][head_dim], contiguous
  *   workspace     16-byte aligned, torq_paged_attention_workspace_bytes() of the same sizes; contents do not matter.  The
  *                 size neither only grows nor only falls with B or width: it is asked for each, or 66 MiB, enough for any call, are kept.
- * Products of bf16 values with fp32 sums (MXFP8 values are bf16 values), softmax statistics in fp32, the weights p as two bf16 parts in
+ * Products of bf16 values with fp32 sums (MXFP8 values are bf16 values for scale bytes from 3 to 246; below, the least elements are rounded
+ * to bf16's, multiples of 2^-133, ties to even, and above, values from 2^128 on are infinite; byte 0xFF: NaN), softmax statistics in fp32, the weights p as two bf16 parts in
  * the product with v: the output's is the only rounding to bf16.  The same inputs give the same bits.  scale has to be finite.  All pointers 16-byte aligned, tables and lengths 4. */
 size_t torq_paged_attention_workspace_bytes(const torq_kv_cache_t *cache, int heads, int64_t B, int width);
 int torq_paged_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads,

@@ -19,7 +19,8 @@
 //                                                            which the lanes hold them, so P^T is already its B operand
 // Its A operand wants 8 tokens of one i in a lane.  The lane loads, for its 8 tokens, E consecutive values of V (coalesced
 // rows), and pairs of them are put together by v_perm_b32: slot j holds V[its tokens][E * (l % 16) + j].
-// In MXFP8 the elements are widened to bf16 with their scale in one instruction (exact: 4 bits of significand).
+// In MXFP8 the elements are widened to bf16 with their scale in one instruction, which takes of the scale its exponent field (so 0 is 2^-127 and
+// 0xFF NaN).  4 bits of significand: exact from scale byte 3 on, whose least element is 2^-133 as bf16's, up to 2^128.
 //
 // K and V of a wave's next tile are on their way while it works on this one, K from the moment that S is there, V from the
 // moment that O is.  The loads are buffer loads over the 16 tokens of a group (a group lies in one page) as far as they are tokens of

@@ -345,3 +345,40 @@ def test_workspace_sizes_go_up_and_down_with_requests_and_tables():
     assert size(16, 63, 8, 128) == size(16, 64, 8, 128) == 0 < size(16, 65, 8, 128)
     assert size(15, 64, 8, 128) > size(16, 64, 8, 128)                       # fewer requests, more
     assert size(1, 65, 8, 128) < size(4, 65, 8, 128) < size(300, 65, 8, 128) <= 66 << 20
+
+
+@gpu
+def test_every_mxfp8_value_as_attention_reads_it():
+    # one token a request, whose value is its output: every element under every scale byte, as bf16
+    codes, bytes_ = torch.arange(256, dtype=torch.uint8), torch.arange(256, dtype=torch.uint8)
+    elements, scales = codes.view(F8).double(), bytes_.view(E8).double()
+    want = (scales[:, None] * elements).float().to(BF)                       # (no value has more bits than fp32 holds)
+    e = torch.zeros((256, 1, 16, 256), dtype=torch.uint8, device=DEV)
+    s = torch.full((256, 1, 16, 8), 127, dtype=torch.uint8, device=DEV)
+    v, v_scales = e.clone(), s.clone()
+    v[:, 0, 0], v_scales[:, 0, 0] = codes.to(DEV), bytes_[:, None].to(DEV)
+    cache = binding.KVCache(e.view(F8), v.view(F8), s.view(E8), v_scales.view(E8))
+    got = binding.torq_paged_attention(torch.zeros((256, 1, 256), dtype=BF, device=DEV), cache, torch.arange(256, dtype=torch.int32, device=DEV)[:, None].contiguous(),
+                                       torch.ones(256, dtype=torch.int32, device=DEV), 1.0)[:, 0].cpu()
+    same = (got == want) | (got.isnan() & want.isnan())
+    assert same.all(), [(int(b), int(c), float(got[b, c]), float(want[b, c])) for b, c in (~same).nonzero()[:8]]
+    assert float(want[0, 0x78]) == 2.0 ** -119 and want[255].isnan().all() and float(want[3, 1]) == 2.0 ** -133
+
+
+@gpu
+@pytest.mark.parametrize("byte", [0, 1, 2, 3, 60, 127, 200, 254])
+def test_keys_under_every_kind_of_scale(byte):
+    # keys of 1 and 1/2 times the scale, a query that brings the scores to 1 and 1/2 (byte 0: 2^-127 and 2^-128, which are no normal bf16 values)
+    e = torch.zeros((1, 1, 16, 32), dtype=torch.uint8, device=DEV)
+    s = torch.full((1, 1, 16, 1), 127, dtype=torch.uint8, device=DEV)
+    k, v, k_scales = e.clone(), e.clone(), s.clone()
+    k[0, 0, 0, 5], k[0, 0, 1, 5], v[0, 0, 0], v[0, 0, 1], k_scales[0, 0, :2] = 0x38, 0x30, 0x38, 0x40, byte
+    q = torch.zeros((1, 1, 32), dtype=BF, device=DEV)
+    q[0, 0, 5] = 2.0 ** (127 - byte)
+    cache = binding.KVCache(k.view(F8), v.view(F8), k_scales.view(E8), s.view(E8))
+    got = binding.torq_paged_attention(q, cache, torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.full((1,), 2, dtype=torch.int32, device=DEV), 1.0)
+    p = 1 / (1 + 2.718281828459045 ** -0.5)
+    want = p + 2 * (1 - p)
+    assert ((got.double() - want).abs() <= (2.0 ** -9 + 2.0 ** -12) * 2 * want).all()
+    k_scales[0, 0, 1] = 255
+    assert binding.torq_paged_attention(q, cache, torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.full((1,), 2, dtype=torch.int32, device=DEV), 1.0).isnan().all()
