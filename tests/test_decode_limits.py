@@ -7,6 +7,7 @@ import sys
 import textwrap
 import types
 
+import numpy as np
 import pytest
 import torch
 
@@ -382,3 +383,88 @@ def test_keys_under_every_kind_of_scale(byte):
     assert ((got.double() - want).abs() <= (2.0 ** -9 + 2.0 ** -12) * 2 * want).all()
     k_scales[0, 0, 1] = 255
     assert binding.torq_paged_attention(q, cache, torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.full((1,), 2, dtype=torch.int32, device=DEV), 1.0).isnan().all()
+
+
+# ---- sizes from which another form of a kernel runs --------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("M,d,fmt,place", [(8192, 4096, 8, None), (8192, 4096, 9, "residual"), (8192, 4096, 8, "x"), (4099, 8192, 8, "residual"), (250000, 128, 8, None),
+                                           (250000, 128, 9, "x"), (500001, 64, 9, None), (65000, 512, 8, "residual"), (1100, 28672, 9, "x"), (2050, 16384, 8, None)])
+def test_norm_of_more_than_the_cache_holds(M, d, fmt, place):
+    # over 120 MiB of inputs: read, and the residual written, with the non-temporal hint
+    assert 4 * M * d > 120 << 20
+    x, r, w = (torch.randn((M, d), device=DEV) * 3).to(BF), torch.randn((M, d), device=DEV).to(BF), (1 + 0.2 * torch.randn(d, device=DEV)).to(BF)
+    x[:, ::19] *= 20
+    a, b = x.clone(), r.clone()
+    out, scales, total = binding.torq_add_rms_norm(a, b, w, 1e-5, fmt, residual_out={"x": a, "residual": b, None: None}[place])
+    assert place is None or total is (a if place == "x" else b)
+    if place != "x":
+        assert torch.equal(a, x)
+    if place != "residual":
+        assert torch.equal(b, r)
+    part = 2.0 ** -16                                # fp32's part of y, as of smaller rows
+    for i in range(0, M, max(1, (1 << 25) // d)):
+        rows = slice(i, i + max(1, (1 << 25) // d))
+        s = x[rows].double() + r[rows].double()
+        y = s / (s.pow(2).mean(-1, keepdim=True) + 1e-5).sqrt() * w.double()
+        assert ((total[rows].double() - s).abs() <= (2.0 ** -8 + 2.0 ** -23) * s.abs()).all()
+        if fmt == binding.TORQ_FMT_BF16:
+            assert ((out[rows].double() - y).abs() <= (2.0 ** -8 + part) * y.abs() + 1e-38).all()
+            continue
+        unit = 2.0 ** (scales[rows].view(torch.uint8).double() - 127)
+        amax = y.abs().unflatten(-1, (-1, 32)).amax(-1)
+        assert (amax * (1 - part) <= 448 * unit).all() and (amax * (1 + part) > 224 * unit).all()
+        unit = unit.repeat_interleave(32, -1)
+        assert ((out[rows].double() * unit - y).abs() <= (2.0 ** -4 + 2 * part) * y.abs() + unit * 2.0 ** -10).all()
+
+
+def check_tables(held, lengths, page, width, before, tokens, pages=None):
+    """torq_block_tables against running sums over arrays of the host, in 64 bits."""
+    held, lengths = np.asarray(held, dtype=np.int64), np.asarray(lengths, dtype=np.int64)
+    B = len(held)
+    had, have = np.minimum(-(-held // page), width), np.minimum(-(-lengths // page), width)
+    need, new = np.maximum(have - had, 0), np.maximum(lengths - held, 0)
+    g = np.random.default_rng(B + page)
+    pages = int(need.sum()) + before + 3 if pages is None else pages
+    free, tables = g.permutation(pages).astype(np.int32), g.integers(0, pages, (B, width)).astype(np.int32)
+    first, want = before + np.cumsum(need) - need, tables.copy()
+    for b in np.nonzero(need)[0]:
+        at = first[b] + np.arange(need[b])
+        want[b, had[b]:have[b]] = np.where(at < pages, free[np.minimum(at, pages - 1)], -1)
+    ends = np.cumsum(new)
+    token = np.arange(tokens)
+    owner = np.minimum(np.searchsorted(ends, token, side="right"), B - 1)
+    position = held[owner] + token - (ends - new)[owner]
+    entry = want[owner, np.minimum(position // page, max(width - 1, 0))].astype(np.int64)
+    slots = np.where((token < ends[-1]) & (position // page < width) & (entry >= 0), entry * page + position % page, -1)
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(DEV)
+    t, cursor = dev(tables), torch.full((1,), before, dtype=torch.int32, device=DEV)
+    got, after = binding.torq_block_tables(dev(held), dev(lengths), dev(free), cursor, t, page, tokens)
+    assert np.array_equal(t.cpu().numpy(), want) and np.array_equal(got.cpu().numpy(), slots) and after.tolist() == [before + int(need.sum())]
+
+
+@gpu
+@pytest.mark.parametrize("held,lengths,page,width,tokens", [
+    ([0, 100, 7, 0], [700000, 500001, 7, 90], 16, 44000, None), ([0, 100, 7, 0], [700000, 500001, 7, 90], 16, 44000, (1 << 20) + 77), ([5] * 3, [1 << 19] * 3, 1, 1 << 19, None),
+    ([16, 0], [40, 20], 16, (1 << 20) + 3, None), ([16, 0, 3], [1 << 25, 20, 9], 16, (1 << 20) + 3, 50)])
+def test_block_tables_of_more_than_a_million(held, lengths, page, width, tokens):
+    # 2^20 tokens or entries of a row: sums in 64 bits
+    tokens = int(np.maximum(np.array(lengths) - np.array(held), 0).sum()) if tokens is None else tokens
+    assert tokens >= 1 << 20 or width > 1 << 20
+    check_tables(held, lengths, page, width, 4, tokens)
+
+
+@gpu
+@pytest.mark.parametrize("B", [1024, 1025, 2500, 7001])
+@pytest.mark.parametrize("more", ["one", "two", "first", "second", "third"])
+def test_block_tables_of_many_requests_that_go_on_by_a_token(B, more):
+    # 1024 requests at a time: entries written by their own lanes, except where one of the 1024 has more than two
+    g = np.random.default_rng(B)
+    held = g.integers(0, 100, B)
+    new = np.full(B, 2 if more == "two" else 1)
+    if more in ("first", "second", "third"):
+        at = 1024 * ("first", "second", "third").index(more) + 5
+        new[at if at < B else B - 1] = 300
+        new[g.integers(0, B, B // 9)] = 0
+    check_tables(held, held + new, 16, 30, 3, int(new.sum()))
+    check_tables(held, held + new, 16, 30, 3, int(new.sum()) + 700, pages=40)
