@@ -69,7 +69,6 @@ struct AttentionArgs {
   int64_t table_stride, page16_magic; // t / page_size = (t / 16) * page16_magic >> 38
   int64_t most;                       // width * page_size
   int B, page_size, kv_heads, group, rows, row_groups, dim;            // rows: query heads of a column at most
-  int solo;                           // a workgroup for each (request, columns that it works on), which is its run
   float scale_log2;                   // scale * log2(e): the softmax is taken to base 2
   uint16_t *out;
   float *part, *part_ml;              // [run][2][columns at a time][rows][dim] and [2]: O, and m and l, of what is not whole in a run
@@ -128,8 +127,9 @@ __device__ __forceinline__ float over_column(float v, F &&op) {
 __device__ __forceinline__ int length_of(const AttentionArgs &a, int n) { return n < 0 ? 0 : n < a.most ? n : (int)a.most; }
 
 // DP: head_dim rounded up to what the operands hold.  WAYS: 4, the waves take turns at the tiles of a column; 1, each has a column
-// of its own and all of its tiles in the run.  RT: products side by side, for up to 16 query heads each.
-template <int DP, bool F8, bool ONCE, int WAYS, int RT>
+// of its own and all of its tiles in the run.  RT: products side by side, for up to 16 query heads each.  SOLO: a workgroup for each
+// (request, columns that it works on), which is its run.
+template <int DP, bool F8, bool ONCE, int WAYS, int RT, bool SOLO>
 __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   constexpr int KS = DP / 32;                       // k-steps of S
   constexpr int E = DP < 128 ? DP / 16 : 8;         // consecutive values of V in a lane
@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
       }
   };
   Segment seg;
-  if (a.solo) {
+  if constexpr (SOLO) {
     const int b = blockIdx.x / columns, column = blockIdx.x - b * columns;
     const int length = length_of(a, lengths[b]), tiles = (length + ATT_TILE - 1) / ATT_TILE;
     seg = Segment{b, 0, tiles, length, 0, 0, 0, tiles, 0};      // (end: that of no run)
@@ -348,15 +348,15 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   load_k(here);
   __builtin_amdgcn_sched_barrier(0);
   load_v(here);
-  if (!a.solo) zeros();
+  if constexpr (!SOLO) zeros();
   for (int second = 0;; second = 1) {               // second: the run's second segment, or a later one
     const bool whole = seg.first == 0 && seg.last == seg.tiles;
     // what comes behind this segment: its first tile is on the way when this one's last is worked on
     Segment behind = seg;
     behind.last = 0;                                // (no tile of it is there)
-    if (seg.end < run_end) behind = behind_of(seg);
-    const bool more = behind.last > 0;
-    if (!a.solo && tid == 0 && (a.by_item ? seg.first == 0 : !more)) {
+    if (!SOLO && seg.end < run_end) behind = behind_of(seg);
+    const bool more = !SOLO && behind.last > 0;
+    if (!SOLO && tid == 0 && (a.by_item ? seg.first == 0 : !more)) {
       a.cuts[a.by_item ? seg.b * columns + seg.column : run] = Cut{
           seg.b, seg.column, seg.first == 0 && !whole ? 2 * run + second : -1, seg.end - seg.last + seg.tiles - 1, tiles_each, tiles_more};
     }
@@ -411,6 +411,7 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
         }
       }
       load_k(next);
+      if constexpr (SOLO) __builtin_amdgcn_sched_barrier(0);       // (else some of them wait for V: 333 tokens 6.6 -> 7.0 us)
       // p as two bf16 parts, the first the next below p (its bits less one, cut off) and the second what is left, rounded: p to 2^-16, so the
       // output's own rounding is the only one to bf16 that shows.  Both are positive where p is, so that an infinite v stays infinite, and
       // both zero where p is: masked tokens, and weights that are nothing in 32 bits, however large their v.
@@ -683,19 +684,23 @@ hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, i
                   cache.head_stride * bytes, (int)cache.pages, (int)cache.token_stride * bytes, (const uint16_t *)q, q_stride,
                   q_head_stride, block_tables, lengths, table_stride, ((int64_t)1 << 38) / page16 + 1,
                   (int64_t)width * cache.page_size, (int)B, cache.page_size, cache.heads, heads / cache.heads, plan.rows, row_groups_of(cache, heads, B),
-                  cache.head_dim, plan.solo, scale * 1.44269504088896340736f, (uint16_t *)out, part, part + part_rows(plan) * cache.head_dim,
+                  cache.head_dim, scale * 1.44269504088896340736f, (uint16_t *)out, part, part + part_rows(plan) * cache.head_dim,
                   (Cut *)workspace, plan.by_item};
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(plan.groups), dim3(256), 0, stream, a); };
   auto of_hint = [&](auto dp, auto of8, auto hint) {
     constexpr int DP = decltype(dp)::value;
     constexpr bool F8 = decltype(of8)::value, ONCE = decltype(hint)::value;
-    if constexpr (DP <= 128)
-      if (plan.rows > ATT_ROWS) {
-        // (a column for each wave: short tables, or lines that are read more than once)
-        if (plan.ways == 1) return go(paged_attention_kernel<DP, F8, false, 1, 2>);
-        return go(paged_attention_kernel<DP, F8, ONCE, ATT_WAVES, 2>);
-      }
-    plan.ways > 1 ? go(paged_attention_kernel<DP, F8, ONCE, ATT_WAVES, 1>) : go(paged_attention_kernel<DP, F8, ONCE, 1, 1>);
+    auto of_launch = [&](auto solo) {
+      constexpr bool SOLO = decltype(solo)::value;
+      if constexpr (DP <= 128)
+        if (plan.rows > ATT_ROWS) {
+          // (a column for each wave: short tables, or lines that are read more than once)
+          if (plan.ways == 1) return go(paged_attention_kernel<DP, F8, false, 1, 2, SOLO>);
+          return go(paged_attention_kernel<DP, F8, ONCE, ATT_WAVES, 2, SOLO>);
+        }
+      plan.ways > 1 ? go(paged_attention_kernel<DP, F8, ONCE, ATT_WAVES, 1, SOLO>) : go(paged_attention_kernel<DP, F8, ONCE, 1, 1, SOLO>);
+    };
+    plan.solo ? of_launch(std::true_type{}) : of_launch(std::false_type{});
   };
   auto of_format = [&](auto dp, auto of8) {
     // (rows of up to 64 bytes never go past the cache)
