@@ -626,33 +626,49 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   Plan p;
   p.rows = rows_of(cache, heads, B);
   const int64_t columns = (int64_t)cache.heads * row_groups_of(cache, heads, B), tiles = ((int64_t)width * cache.page_size + ATT_TILE - 1) / ATT_TILE;
-  // Every request within so few tokens that a workgroup each is done before runs would be made out and joined.  333 tokens, 8 key heads 13 ->
-  // 7.2 us; up to 1000 tokens, 8 key heads, 1, 4, 16, 64, 256 requests in runs / a workgroup each: 10.1 / 12.8, 13.8 / 14.7, 20.4 / 15.5,
-  // 49.8 / 44.2, 175 / 165 us, ragged (1 to 1000) 4, 16, 64 of them 10.9 / 13.2, 16.3 / 14.6, 32.5 / 32.9; up to 2000, ragged, 64 of
-  // them 52.5 / 61.5
+  // Every request within so few tokens that a workgroup each is done before runs would be made out and joined.  In runs / a workgroup each, us: 333
+  // tokens, 8 key heads, 1, 16, 64 requests 9.3 / 6.7, 13.9 / 8.0, 20.2 / 17.0; 900 to 1000 tokens, 1, 4, 16, 64, 256 of them 9.9 / 12.1, 13.5 / 13.3,
+  // 20.5 / 14.3, 50.0 / 44.0, 175 / 165, ragged (1 to 1000) 9.9 / 9.1, 10.7 / 10.2, 17.5 / 13.4, 32.2 / 34.3, 101 / 100; up to 2000, ragged, 16, 64 of
+  // them 23.3 / 25.2, 53.7 / 65.7
   // (and within a launch, which runs always are)
   p.solo = (tiles <= 16 || (tiles <= 32 && B * columns >= 128)) && B * columns <= most_workgroups(256);
   bool own;                                         // each wave has a column of its own
-  // Short tables: 820 columns of 1 to 3 tokens, head_dim 256, 26 -> 8 us.  Over 128 a CU has one workgroup, so the waves' getting ready and putting
-  // together are not hidden by others'; but a column a wave for 512 leaves half of the CUs without.  512 of 100 to 128 tokens 20.8 -> 17.5, 120 to
-  // 192 23.8 -> 21.9, 130 to 208 24.5 -> 25.2, 130 to 256 27.5 -> 34.7 (MXFP8 18.2 -> 14.7, 20.9 -> 17.8, -, 21.6 -> 21.1), over two key heads, so 256
-  // workgroups, 24.7 -> 20.4, 29.0 -> 25.6; 640 of 130 to 256 37.5 -> 35.9; 1024 of 300 to 500 87 -> 79, MXFP8 63.5 -> 48.1
-  const bool alone = cache.head_dim > 128;
-  // A workgroup's waves have columns of one request, so that some have none where those are no multiple of four.  All four / one each, us: 4096
-  // columns of 60 to 256 tokens, head_dim 128, one key head 65 / 102 (MXFP8 53 / 106), two 65 / 72 (53 / 64), five 65 / 89 (53 / 61), three 64 / 67
-  // (53 / 52, up to 160 tokens 45 / 40); head_dim 256, one 188 / 225, two 188 / 163 (MXFP8 155 / 111), three 185 / 148 (153 / 93), five 186 / 189 (153 /
-  // 112); 1024 of 300 to 1000 tokens, head_dim 256, one 139 / 188 (96 / 176), two 143 / 149 (96 / 115), three 138 / 169 (94 / 125)
-  const int64_t idle = -columns & (ATT_WAVES - 1);
+  const bool alone = cache.head_dim > 128, mx = cache.format == FMT_MXFP8;
+  const int64_t idle = -columns & (ATT_WAVES - 1), workgroups = B * (columns + idle) / ATT_WAVES;
   auto busy = [&](int eighths) { return 8 * columns >= eighths * (columns + idle); };
-  const bool mx = cache.format == FMT_MXFP8;
-  if (p.solo)
-    own = alone ? (tiles <= (mx || B * (columns + idle) > 512 ? 8 : 6) && columns > 1 && B * columns >= 512) || (busy(7) && B * columns > 768)
-                : tiles <= 8 && busy(6) && B * columns >= (tiles <= 4 ? 512 : 2048);
-  // Two columns of 16, 8 key heads, 1, 4, 16 requests: 12.5 -> 15.7, 33.8 -> 28.9, 102 -> 80 us.  In MXFP8, where it is the vector instructions that
-  // idle waves leave to others: 64 and 128 requests of 1000 to 4000, 24 query heads of 256 for one key head 39 -> 49, 66 -> 93, 40 of 128 31 -> 39,
-  // 44 -> 62, for three 59 -> 70, 87 -> 121; of 256 for three 88 -> 105, but from 128 requests on 184 -> 174
-  else if (row_groups_of(cache, heads, B) > 1) own = !mx || busy(7) ? B * columns >= 64 : alone && columns > 2 && B * columns >= ATT_WAYS_ITEMS;
-  else own = columns % ATT_WAVES == 0 && (alone || heads / cache.heads <= 2) && B * columns >= ATT_WAYS_ITEMS;
+  if (p.solo) {
+    // It saves the putting together, where there are columns for the waves of all CUs (a workgroup's are of one request, so that some have
+    // none where its columns are no multiple of four) and few tiles of each.  Over 128 a CU has one workgroup.  All four / one each, us:
+    //   columns  tokens       head_dim  key heads  bf16         MXFP8
+    //   512      20 to 128    128       8          7.6 / 8.8    7.1 / 8.2
+    //   1024     20 to 128    128       8          11.3 / 10.3  10.7 / 8.7
+    //   1024     20 to 128    128       7          11.5 / 14.5  11.6 / 12.0
+    //   4096     20 to 128    128       7                       31.8 / 24.1
+    //   4096     60 to 160    128       8          49.0 / 47.9
+    //   4096     60 to 192    128       8          53.5 / 55.3
+    //   4096     60 to 256    128       8          62.9 / 68.4  49.2 / 45.1
+    //   4096     60 to 192    64        8          31.6 / 30.4
+    //   8192     60 to 256    64        8          68.5 / 66.1
+    //   512      100 to 128   256       8          17.0 / 14.9  11.6 / 12.3
+    //   512      130 to 256   256       8          24.7 / 32.9  15.3 / 18.9
+    //   1024     100 to 128   256       8          32.6 / 22.9  19.2 / 14.3
+    //   1024     130 to 256   256       8          47.1 / 40.9  30.9 / 25.7
+    //   2048     60 to 160    256       3          66.0 / 52.9  43.3 / 40.2
+    //   2048     60 to 160    256       2          65.0 / 56.1  43.2 / 45.0
+    //   2048     60 to 160    256       1          66.0 / 81.5  42.8 / 69.1
+    //   2048     60 to 256    256       3          84.1 / 74.9  52.0 / 54.1
+    //   2048     300 to 1000  256       8          246 / 260
+    //   2048     900 to 1000  256       8          337 / 320
+    own = alone ? workgroups >= 128 && (tiles <= 6 ? busy(mx ? 6 : 4) : tiles <= 8 && idle == 0 && workgroups >= 256)
+                : tiles <= (mx || cache.head_dim <= 64 ? 8 : 5) && (mx ? busy(6) : idle == 0) && B * columns >= (tiles <= 4 ? 768 : 2048);
+  } else if (row_groups_of(cache, heads, B) > 1) {
+    // Two columns of 16, 8 key heads, 1, 4, 16 requests: 12.5 / 15.7, 33.8 / 28.9, 102 / 80 us.  In MXFP8, where it is the vector instructions that
+    // idle waves leave to others: 64 and 128 requests of 1000 to 4000, 24 query heads of 256 for one key head 39 / 49, 66 / 93, 40 of 128 31 / 39,
+    // 44 / 62, for three 59 / 70, 87 / 121; of 256 for three 88 / 105, but from 128 requests on 184 / 174
+    own = !mx || busy(7) ? B * columns >= 64 : alone && columns > 2 && B * columns >= ATT_WAYS_ITEMS;
+  } else {
+    own = idle == 0 && (alone || heads / cache.heads <= 2) && B * columns >= ATT_WAYS_ITEMS;
+  }
   p.ways = own ? 1 : ATT_WAVES;
   // workgroups: three, two or one for each CU by the registers that a wave takes.  head_dim 64 with 512, 768, 1024: 64 requests of 100 to
   // 3000 tokens 52.3, 50.1, 49.6 us, 16 long ones 34.6, 35.4, 35.8; 128: 16 58.3, 59.4, 64.6; 256 with 256, 512, 768: 64.9, 72.6, 79.9

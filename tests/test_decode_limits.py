@@ -261,14 +261,18 @@ def attention_kernels(launches, cases):
 @pytest.mark.parametrize("fmt", [binding.TORQ_FMT_BF16, binding.TORQ_FMT_MXFP8])
 def test_waves_with_columns_of_their_own_have_one(launches, fmt):
     # tables for up to 512 tokens: a launch a call.  Where a request has one column the waves take turns at it as they do for a single request,
-    # and so they do where it has five for eight waves, but for the shortest of head_dim 256; where its columns are enough each has one
-    for dim in (64, 128, 256):
-        single, *few = attention_kernels(launches, [(1, 8, dim, 1, 512, fmt)] + [(1, 8, dim, 4096, tokens, fmt) for tokens in (128, 256, 512)]
-                                         + [(kv, 8 * kv, dim, 4096, 256 if dim < 256 else 512, fmt) for kv in (2, 5)])
-        assert few == [single] * len(few), dim
-        enough = attention_kernels(launches, [(kv, 8 * kv, dim, 4096, tokens, fmt) for kv in (3, 4, 7, 8, 15, 18) + ((2, 5) if dim == 256 else ())
-                                              for tokens in (64, 128, 256)])
-        assert len(set(enough)) == 1 and enough[0] != single, dim
+    # and so they do where the last of them would have none, but for a few in MXFP8 and in the shortest tables of head_dim 256
+    mx = fmt == binding.TORQ_FMT_MXFP8
+    full, most, half = (4, 8, 16, 20), (3, 7, 15, 18), (2, 5)
+    cases = lambda dim, heads, *tokens: [(kv, 8 * kv, dim, 4096, t, fmt) for kv in heads for t in tokens]
+    for dim, own, turns in ((64, cases(64, full + most * mx, 64, 128, 256), cases(64, (1,) + half + most * (not mx), 128, 256) + cases(64, full, 288, 512)),
+                            (128, cases(128, full + most * mx, 64, 128, 160) + cases(128, full, 256) * mx,
+                             cases(128, (1,) + half + most * (not mx), 128, 256) + cases(128, full, 192, 256) * (not mx) + cases(128, full, 288, 512)),
+                            (256, cases(256, full + most + half * (not mx), 64, 192) + cases(256, full, 208, 256),
+                             cases(256, (1,) + half * mx, 64, 192) + cases(256, (1,) + most + half, 208, 256) + cases(256, full, 288, 512))):
+        single, *kernels = attention_kernels(launches, [(1, 8, dim, 1, 512, fmt)] + turns + own)
+        assert kernels[:len(turns)] == [single] * len(turns), dim
+        assert set(kernels[len(turns):]) != {single} and len(set(kernels[len(turns):])) == 1, dim
 
 
 def test_idle_waves_do_not_take_columns_of_mxfp8(launches):
@@ -278,12 +282,13 @@ def test_idle_waves_do_not_take_columns_of_mxfp8(launches):
         assert (many != single) == alone, (kv, B)
 
 
-def test_512_columns_of_seven_and_eight_tiles_are_no_waves_own(launches):
-    # head_dim 256, bf16: four columns a workgroup would leave half of the CUs without; whether a table has a page to spare says nothing
-    for requests, kv, tokens, fmt, alone in ((64, 8, 192, 8, True), (64, 8, 208, 8, False), (64, 8, 256, 8, False), (64, 8, 272, 8, False),
-                                             (80, 8, 256, 8, True), (256, 2, 256, 8, True), (64, 8, 256, 9, True)):
-        single, *_, kernel = attention_kernels(launches, [(1, 8, 256, 1, 512, fmt), (kv, 4 * kv, 256, requests, tokens, fmt)])
-        assert (kernel != single) == alone, (requests, kv, tokens, fmt)
+def test_few_columns_of_head_dim_256_are_no_waves_own(launches):
+    # four columns a workgroup would leave CUs without one; whether a table has a page to spare says nothing
+    cases = [(64, 8, 192, 8, True), (60, 8, 192, 8, False), (64, 8, 208, 8, False), (64, 8, 256, 8, False), (64, 8, 272, 8, False), (128, 8, 256, 8, True),
+             (256, 2, 192, 8, True), (256, 2, 256, 8, False), (64, 8, 256, 9, False), (128, 8, 256, 9, True)]
+    kernels = attention_kernels(launches, [(1, 8, 256, 1, 512, 8), (1, 8, 256, 1, 512, 9)] + [(kv, 4 * kv, 256, B, tokens, fmt) for B, kv, tokens, fmt, _ in cases])
+    for (B, kv, tokens, fmt, own), kernel in zip(cases, kernels[2:]):
+        assert (kernel != kernels[fmt - 8]) == own, (B, kv, tokens, fmt)
 
 
 # ---- values at the ends of their types ---------------------------------------------------------
