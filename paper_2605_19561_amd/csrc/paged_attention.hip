@@ -638,7 +638,8 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   auto busy = [&](int eighths) { return 8 * columns >= eighths * (columns + idle); };
   if (p.solo) {
     // It saves the putting together, where there are columns for the waves of all CUs (a workgroup's are of one request, so that some have
-    // none where its columns are no multiple of four) and few tiles of each.  Over 128 a CU has one workgroup.  All four / one each, us:
+    // none where its columns are no multiple of four) and few tiles of each; over 128, where a CU has one workgroup at a time, also of more,
+    // if their rounds of the CUs are whole.  All four / one each, us:
     //   columns  tokens       head_dim  key heads  bf16         MXFP8
     //   512      20 to 128    128       8          7.6 / 8.8    7.1 / 8.2
     //   1024     20 to 128    128       8          11.3 / 10.3  10.7 / 8.7
@@ -657,9 +658,14 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
     //   2048     60 to 160    256       2          65.0 / 56.1  43.2 / 45.0
     //   2048     60 to 160    256       1          66.0 / 81.5  42.8 / 69.1
     //   2048     60 to 256    256       3          84.1 / 74.9  52.0 / 54.1
+    //   1024     1 to 320     256       8          47.3 / 44.2  26.8 / 23.3
+    //   1024     1 to 512     256       8          61.7 / 67.4  41.5 / 42.0
+    //   1024     460 to 512   256       8          91.6 / 83.5  53.2 / 48.0
+    //   1280     160 to 320   256       8          66.8 / 73.7  41.9 / 51.0
     //   2048     300 to 1000  256       8          246 / 260
     //   2048     900 to 1000  256       8          337 / 320
-    own = alone ? workgroups >= 128 && (tiles <= 6 ? busy(mx ? 6 : 4) : tiles <= 8 && idle == 0 && workgroups >= 256)
+    const int64_t rounds = (workgroups + 255) / 256;
+    own = alone ? (tiles <= 6 ? workgroups >= 128 && busy(mx ? 6 : 4) : tiles <= 16 && busy(7) && 8 * workgroups >= 7 * 256 * rounds)
                 : tiles <= (mx || cache.head_dim <= 64 ? 8 : 5) && (mx ? busy(6) : idle == 0) && B * columns >= (tiles <= 4 ? 768 : 2048);
   } else if (row_groups_of(cache, heads, B) > 1) {
     // Two columns of 16, 8 key heads, 1, 4, 16 requests: 12.5 / 15.7, 33.8 / 28.9, 102 / 80 us.  In MXFP8, where it is the vector instructions that

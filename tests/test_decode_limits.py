@@ -268,8 +268,8 @@ def test_waves_with_columns_of_their_own_have_one(launches, fmt):
     for dim, own, turns in ((64, cases(64, full + most * mx, 64, 128, 256), cases(64, (1,) + half + most * (not mx), 128, 256) + cases(64, full, 288, 512)),
                             (128, cases(128, full + most * mx, 64, 128, 160) + cases(128, full, 256) * mx,
                              cases(128, (1,) + half + most * (not mx), 128, 256) + cases(128, full, 192, 256) * (not mx) + cases(128, full, 288, 512)),
-                            (256, cases(256, full + most + half * (not mx), 64, 192) + cases(256, full, 208, 256),
-                             cases(256, (1,) + half * mx, 64, 192) + cases(256, (1,) + most + half, 208, 256) + cases(256, full, 288, 512))):
+                            (256, cases(256, full + most + half * (not mx), 64, 192) + cases(256, full, 208, 256, 512),
+                             cases(256, (1,) + half * mx, 64, 192) + cases(256, (1, 3) + half, 208, 256, 512))):
         single, *kernels = attention_kernels(launches, [(1, 8, dim, 1, 512, fmt)] + turns + own)
         assert kernels[:len(turns)] == [single] * len(turns), dim
         assert set(kernels[len(turns):]) != {single} and len(set(kernels[len(turns):])) == 1, dim
@@ -282,10 +282,11 @@ def test_idle_waves_do_not_take_columns_of_mxfp8(launches):
         assert (many != single) == alone, (kv, B)
 
 
-def test_few_columns_of_head_dim_256_are_no_waves_own(launches):
-    # four columns a workgroup would leave CUs without one; whether a table has a page to spare says nothing
+def test_head_dim_256_has_a_column_a_wave_where_whole_rounds_of_the_cus_do(launches):
+    # a CU has one workgroup at a time: half a round would leave half of them without; whether a table has a page to spare says nothing
     cases = [(64, 8, 192, 8, True), (60, 8, 192, 8, False), (64, 8, 208, 8, False), (64, 8, 256, 8, False), (64, 8, 272, 8, False), (128, 8, 256, 8, True),
-             (256, 2, 192, 8, True), (256, 2, 256, 8, False), (64, 8, 256, 9, False), (128, 8, 256, 9, True)]
+             (128, 8, 272, 8, True), (128, 8, 512, 8, True), (128, 8, 528, 8, False), (160, 8, 272, 8, False), (256, 8, 272, 8, True), (256, 2, 192, 8, True),
+             (256, 2, 256, 8, False), (64, 8, 256, 9, False), (128, 8, 256, 9, True), (136, 8, 272, 9, False)]
     kernels = attention_kernels(launches, [(1, 8, 256, 1, 512, 8), (1, 8, 256, 1, 512, 9)] + [(kv, 4 * kv, 256, B, tokens, fmt) for B, kv, tokens, fmt, _ in cases])
     for (B, kv, tokens, fmt, own), kernel in zip(cases, kernels[2:]):
         assert (kernel != kernels[fmt - 8]) == own, (B, kv, tokens, fmt)
