@@ -312,7 +312,8 @@ int torq_cache_append(const torq_kv_cache_t *cache, const void *key_bf16, int64_
 
 /* Attention of one new token of each request over its cached tokens (the new one's among them):
  *   out[b][h] = sum_t p_t v_t,  p = softmax over t < lengths[b] of scale * q[b][h] . k_t,
- * k_t, v_t: position t of request b under key head h / (heads / cache->heads).  A request without tokens: zeros.
+ * k_t, v_t: position t of request b under key head h / (heads / cache->heads).  A request without tokens: zeros, as is one whose
+ * scores are all minus infinity (such scores weigh nothing beside others).
  *   q_bf16        [B][heads][head_dim], strides in elements, multiples of 8, not negative; heads a multiple of cache->heads
  *   block_tables  as torq_block_tables leaves them, width * page_size at most 2^30, and B * cache->heads *
  *                 ceil(heads / cache->heads / 16) * (width * page_size / 32 + 8) below 2^31.  A position past `width` pages counts as past the length; tokens of
@@ -330,9 +331,11 @@ int torq_paged_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64
 
 /* Residual addition and root-mean-square norm of rows of d values, d a multiple of 32, at most TORQ_MAX_NORM_D:
  *   s = x + residual,  residual_out = bf16(s),  out = s / sqrt(mean(s^2) + eps) * weight
- * x, residual, weight, residual_out bf16; arithmetic in fp32 on s as it is before its rounding.  residual and
+ * x, residual, weight, residual_out bf16; arithmetic in fp32 on s as it is before its rounding (a row whose squares sum to more than fp32
+ * holds, so with an s above 1.8e19 or so, comes out as zeros).  residual and
  * residual_out NULL: s = x.  residual_out may be residual or x.  out and residual_out are two arrays.
- *   out     TORQ_FMT_BF16: [M][d] bf16, what torq_linear reads; may be x.  TORQ_FMT_MXFP8: [M][d] bytes
+ *   out     TORQ_FMT_BF16: [M][d] bf16, what torq_linear reads; may be x.  TORQ_FMT_MXFP8: [M][d] bytes, for a product of the
+ *           caller's (none of this library's reads them)
  *   scales  TORQ_FMT_MXFP8: [M][d/32] bytes; else ignored */
 #define TORQ_MAX_NORM_D 32768
 int torq_add_rms_norm(const void *x_bf16, const void *residual_bf16, const void *weight_bf16, int64_t M, int d, float eps,

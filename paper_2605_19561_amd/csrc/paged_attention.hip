@@ -27,10 +27,11 @@
 // the request: what is past the length, in no page or past the last tile has no records, costs no traffic and comes back as
 // zeros, so the loop knows no other case (and a NaN behind the length is not read).
 //
-// Measured (called in turn over three caches, 303 MB to 1.9 GB): 16 requests of 1000 to 8192 tokens, 64 query and 8 key heads of 128, 55.7 us =
-// 5.4 TB/s; one of 131072 87.8 us = 6.1; 45 of 8000 to 32768 in MXFP8 311 us = 6.2; 77 with 20 heads of 80 each, 85.9 us = 4.9.  The traffic
+// Measured (called in turn over three caches, 303 MB to 1.9 GB; 7.1 TB/s is what reading alone reaches): 16 requests of 1000 to 8192 tokens, 64 query
+// and 8 key heads of 128, 55.2 us = 5.5 TB/s; one of 131072 87.6 us = 6.1; 45 of 8000 to 32768 in MXFP8 312 us = 6.2; 77 with 20 heads of 80 each, 85.9 us = 4.9.  The traffic
 // is what has to be read (counters within 1 %); vector instructions take a third (bf16) to half (MXFP8) of the time.  What is left over HBM's time: 5 to 7 us until
-// the first tiles are there, 5 for the join and its launch.  One request of 333 tokens 7.2 us, one launch: three rounds that hang on one another.
+// the first tiles are there, 5 for the join and its launch.  One request of 333 tokens 6.2 us, one launch: three rounds that
+// hang on one another; compiled apart, since the runs' code in the same kernel cost it 0.4 to 0.6.
 #include <algorithm>
 
 #include "torq_device.h"
@@ -599,7 +600,7 @@ namespace {
 // Query heads of a column: 32 where there are more than 16, the registers hold two products side by side, and there are columns
 // enough without the second 16.  24 heads for each of 8 key heads of 128, 1, 4, 16 requests of 1000 to 8192 tokens with 16 / 32:
 // 12.3 / 13.1, 28.9 / 26.4, 79.8 / 65.6 us (32 heads 83.1 / 68.6, heads of 64 49.1 / 39.2, MXFP8 up to 32768 199 / 139); for one
-// key head, 1 request of 60000, 64 of up to 8192: 23.2 / 26.3, 53.0 / 39.1; one of 333 tokens 7.9 / 10.0.
+// key head, 1 request of 60000, 64 of up to 8192: 23.2 / 26.3, 53.0 / 39.1; 333 tokens, 8 key heads, 1, 4, 16 requests 6.9 / 8.2, 7.6 / 8.2, 10.8 / 9.5.
 int rows_of(const torq_kv_cache_t &cache, int heads, int64_t B) {
   return heads / cache.heads > ATT_ROWS && cache.head_dim <= 128 && B * cache.heads >= 32 ? 2 * ATT_ROWS : ATT_ROWS;
 }

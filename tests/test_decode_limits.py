@@ -391,6 +391,27 @@ def test_keys_under_every_kind_of_scale(byte):
     assert binding.torq_paged_attention(q, cache, torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.full((1,), 2, dtype=torch.int32, device=DEV), 1.0).isnan().all()
 
 
+@gpu
+def test_scores_of_minus_infinity_weigh_nothing():
+    assert two_tokens(-float("inf"), 5.0) == 1.0
+    k, v = torch.zeros((1, 1, 16, 64), dtype=BF, device=DEV), torch.ones((1, 1, 16, 64), dtype=BF, device=DEV)
+    k[..., 3] = -float("inf")
+    q = torch.ones((1, 1, 64), dtype=BF, device=DEV)
+    for width in (1, 200):
+        got = binding.torq_paged_attention(q, binding.KVCache(k, v), torch.zeros((1, width), dtype=torch.int32, device=DEV), torch.full((1,), 9, dtype=torch.int32, device=DEV), 1.0)
+        assert not got.any()
+
+
+@gpu
+def test_norm_of_rows_past_fp32():
+    # squares whose sum fp32 does not hold; half of that is held
+    w = torch.ones(256, dtype=BF, device=DEV)
+    x = torch.full((2, 256), 2.0 ** 62, device=DEV).to(BF)
+    x[1] = 2.0 ** 59
+    out = binding.torq_add_rms_norm(x, None, w, 1e-5)[0].double()
+    assert not out[0].any() and ((out[1] - 1).abs() <= 2.0 ** -8 + 2.0 ** -16).all()
+
+
 # ---- sizes from which another form of a kernel runs --------------------------------------------
 
 @gpu
