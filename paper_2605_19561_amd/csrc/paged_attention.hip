@@ -31,7 +31,7 @@
 // and 8 key heads of 128, 55.2 us = 5.5 TB/s; one of 131072 87.6 us = 6.1; 45 of 8000 to 32768 in MXFP8 312 us = 6.2; 77 with 20 heads of 80 each, 85.9 us = 4.9.  The traffic
 // is what has to be read (counters within 1 %); vector instructions take a third (bf16) to half (MXFP8) of the time.  What is left over HBM's time: 5 to 7 us until
 // the first tiles are there, 5 for the join and its launch.  One request of 333 tokens 6.2 us, one launch: three rounds that
-// hang on one another; compiled apart, since the runs' code in the same kernel cost it 0.4 to 0.6.
+// hang on one another; compiled apart, since the runs' code in the same kernel cost it 0.45 in a graph and 0.85 in a call.
 #include <algorithm>
 
 #include "torq_device.h"
