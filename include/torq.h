@@ -258,31 +258,35 @@ int torq_linear_single_launch_probe(const torq_rotation_t *r, const void *x_bf16
                                     size_t workspace_bytes, int spin_limit, int withhold_ready, void *stream);
 
 /* ------------------------------------------------------------------------ */
-/* The attention side of a decoder block: the residual norm ahead of the linear layers above, and one
- * new token's attention over a paged key-value cache.  Values of all of them are bf16 or MXFP8:
+/* The attention side of a decoder block: the residual norm ahead of the linear layers above, and the attention
+ * of one or several new tokens of each request over a paged key-value cache.  Values are bf16 or MXFP8, those of a cache also MXFP4:
  *   TORQ_FMT_BF16   bf16 elements, no scales
  *   TORQ_FMT_MXFP8  OCP FP8 E4M3 elements, one E8M0 byte for each block of 32 along the last dimension:
  *                   2^(byte-127) is the least power of two (from 2^-127 on) that leaves no element of the
  *                   block above 448, E4M3's largest value; element = E4M3 nearest to x / 2^(byte-127),
  *                   ties to the even code.  (Rounding log2 amax down instead, as MXFP4 above, would put
  *                   maxima of up to 511 on 448.)  A block with an infinity or NaN: byte 0xFF, every element NaN (0x7F).
- * The 4-bit formats above are not among them, nor these among those of torq_rotate_quantize_fmt. */
+ *   TORQ_FMT_MXFP4  (caches) the E2M1 codes and E8M0 scales of torq_rotate_quantize, two codes to a byte, the first in the low
+ *                   half: byte = floor(log2 amax) - 2 + 127, at least 0; code = E2M1 nearest to x / 2^(byte-127), ties to the even code,
+ *                   at most 6 in magnitude.  A block with an infinity or NaN: byte 0xFF, which makes every value of it NaN, and codes 0.
+ * The other 4-bit formats above are not among them, nor BF16 and MXFP8 among those of torq_rotate_quantize_fmt. */
 #define TORQ_FMT_BF16  8
 #define TORQ_FMT_MXFP8 9
 
 /* A paged cache of keys and values: `pages` pages of page_size tokens for each of `heads` heads, in memory that the
  * caller owns.  Element (page, head, token in the page, i) of k and of v lies at page * page_stride + head *
  * head_stride + token * token_stride + i, so a page's heads may lie ahead of its tokens or behind, and k and v in one
- * array or two; the scale byte of a block of 32 lies at a 32nd of the block's place, counted from k_scales or v_scales.
- *   format     TORQ_FMT_BF16 or TORQ_FMT_MXFP8
- *   head_dim   at most TORQ_MAX_HEAD_DIM, a multiple of 8 (bf16) or 32 (MXFP8)
+ * array or two (in MXFP4 an element is half a byte); the scale byte of a block of 32 lies at a 32nd of the block's place, counted from
+ * k_scales or v_scales.
+ *   format     TORQ_FMT_BF16, TORQ_FMT_MXFP8 or TORQ_FMT_MXFP4
+ *   head_dim   at most TORQ_MAX_HEAD_DIM, a multiple of 8 (bf16) or 32 (MXFP8, MXFP4)
  *   page_size  a multiple of 16, at most 65536
- *   strides    in elements, not negative, multiples of 8 (bf16) or 32 (MXFP8); head_dim <= token_stride < 2^29 / page_size
+ *   strides    in elements, not negative, multiples of 8 (bf16) or 32 (MXFP8, MXFP4); head_dim <= token_stride < 2^29 / page_size
  * k and v 16-byte aligned.  The struct is read during a call only. */
 #define TORQ_MAX_HEAD_DIM 256
 typedef struct torq_kv_cache {
     void *k, *v;
-    uint8_t *k_scales, *v_scales;   /* MXFP8 only */
+    uint8_t *k_scales, *v_scales;   /* MXFP8 and MXFP4 only */
     int64_t pages, page_stride, head_stride, token_stride;
     int format, heads, head_dim, page_size;
 } torq_kv_cache_t;
@@ -304,7 +308,7 @@ int torq_block_tables(const int32_t *held, const int32_t *lengths, int64_t B, co
 
 /* key and value [tokens][heads][head_dim] bf16 (strides in elements, multiples of 8, not negative) into the cache: token t at
  * slot slots[t] = page * page_size + place in the page.  A slot outside the cache (-1 among them) is passed over.
- * The other slots of a call differ from one another: what two tokens with one slot leave in it is undefined (in MXFP8 a block's elements
+ * The other slots of a call differ from one another: what two tokens with one slot leave in it is undefined (in MXFP8 and MXFP4 a block's elements
  * and its scale, which are several stores, can be different tokens', so that it has neither's values).  No other slot is touched. */
 int torq_cache_append(const torq_kv_cache_t *cache, const void *key_bf16, int64_t key_token_stride, int64_t key_head_stride,
                       const void *value_bf16, int64_t value_token_stride, int64_t value_head_stride,
@@ -328,6 +332,47 @@ size_t torq_paged_attention_workspace_bytes(const torq_kv_cache_t *cache, int he
 int torq_paged_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads,
                          const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths, int64_t B,
                          float scale, void *out_bf16, void *workspace, size_t workspace_bytes, void *stream);
+
+/* How a model gives its scores, beyond s = scale * q . k, for a query at position p of its request and a key at position t:
+ *   cap      > 0, at most 1e30: s -> cap * tanh(s / cap); 0: as they are
+ *   slopes   [heads] fp32 on the device, finite: s -> s - slopes[h] * |p - t|, behind the cap; NULL: none
+ *   window   > 0: a query sees the keys p - window < t <= p; 0: all of t <= p
+ *   prefix   [B] int32 on the device: a query of request b sees the keys t < prefix[b] besides, whatever its own position (a prompt whose tokens
+ *            see one another, or, with a window, the first tokens of a text); below 0 counts as 0; NULL: none
+ * A key that a query does not see takes no part for it, NaN and infinities in its key and value included.  The struct is read during a call
+ * only, the arrays by its kernels. */
+typedef struct torq_scores {
+    float cap;
+    int window;
+    const float *slopes;
+    const int32_t *prefix;
+} torq_scores_t;
+
+/* torq_paged_attention with scores by a rule: request b's new token is at position lengths[b] - 1.  Same workspace.  NULL scores: as above. */
+int torq_paged_attention_scores(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads,
+                                const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths, int64_t B,
+                                float scale, const torq_scores_t *scores, void *out_bf16, void *workspace, size_t workspace_bytes,
+                                void *stream);
+
+/* Attention of several new tokens of each request (a prompt, a piece of one, a draft to be checked) over its cached tokens, the new ones' among
+ * them: rows starts[b] ... starts[b + 1] - 1 of q are request b's new tokens, the last of them at position lengths[b] - 1, so that the first is at
+ * lengths[b] - (starts[b + 1] - starts[b]), and
+ *   out[row][h] = sum_t p_t v_t,  p = softmax of the scores over the t < lengths[b] that the row's query sees,
+ * which are those up to its own position, or what `scores` says.  A row that sees nothing, or whose scores are all minus infinity: zeros.
+ *   q_bf16        [tokens][heads][head_dim], strides in elements, multiples of 8, not negative; heads a multiple of cache->heads
+ *   starts        [B + 1] int32 on the device, not falling; numbers outside [0, tokens] count as the nearer end.  Rows of no request are left
+ *                 as they were in out
+ *   most          new tokens of a request at most, at least 1; of a request with more the first `most` are computed, the others' rows left
+ *   block_tables, lengths, width, out_bf16 ([tokens][heads][head_dim], contiguous), scale: as above, lengths[b] the tokens after the step;
+ *                 B * cache->heads * ceil(heads * most / cache->heads / 16) * (width * page_size / 32 + 8) below 2^31, and tokens * heads below 2^31
+ *   workspace     16-byte aligned, torq_chunk_attention_workspace_bytes() of the same sizes; contents do not matter
+ * Products of bf16 values with fp32 sums, statistics in fp32.  Where few rows (heads * most / cache->heads up to 32) see the keys the weights are
+ * two bf16 parts as above, else one, rounded to nearest, whose sum they are divided by.  The same inputs give the same bits. */
+size_t torq_chunk_attention_workspace_bytes(const torq_kv_cache_t *cache, int heads, int64_t tokens, int most, int64_t B, int width);
+int torq_chunk_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads, int64_t tokens,
+                         const int32_t *starts, int most, const int32_t *block_tables, int64_t table_stride, int width,
+                         const int32_t *lengths, int64_t B, float scale, const torq_scores_t *scores, void *out_bf16, void *workspace,
+                         size_t workspace_bytes, void *stream);
 
 /* Residual addition and root-mean-square norm of rows of d values, d a multiple of 32, at most TORQ_MAX_NORM_D:
  *   s = x + residual,  residual_out = bf16(s),  out = s / sqrt(mean(s^2) + eps) * weight

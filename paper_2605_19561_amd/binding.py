@@ -25,6 +25,7 @@ EXPORTS = [
     "torq_equalize_inter", "torq_code_histogram_workspace_bytes", "torq_code_histogram", "torq_intra_pair_scores",
     "torq_intra_best_angle", "torq_calibrate_intra", "torq_diag_mfma_burn", "torq_linear_static",
     "torq_block_tables", "torq_cache_append", "torq_paged_attention", "torq_paged_attention_workspace_bytes", "torq_add_rms_norm",
+    "torq_paged_attention_scores", "torq_chunk_attention", "torq_chunk_attention_workspace_bytes",
     "torq_diag_copy", "torq_diag_gemm_ablation", "torq_diag_gemm_persistent", "torq_diag_gemm_plan", "torq_diag_gemm_ring", "torq_diag_gemm_form", "torq_diag_rotate_ablation", "torq_linear_single_launch_reset", "torq_linear_single_launch_gave_up", "torq_linear_single_launch_probe",
 ]
 
@@ -42,6 +43,11 @@ class _KVCacheStruct(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
                 ("pages", C.c_int64), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
                 ("format", C.c_int), ("heads", C.c_int), ("head_dim", C.c_int), ("page_size", C.c_int)]
+
+
+class _ScoresStruct(C.Structure):
+    """torq_scores_t of include/torq.h."""
+    _fields_ = [("cap", C.c_float), ("window", C.c_int), ("slopes", C.c_void_p), ("prefix", C.c_void_p)]
 
 
 class TorqError(RuntimeError):
@@ -137,6 +143,12 @@ def lib():
         L.torq_paged_attention_workspace_bytes.argtypes = [vp, i32, i64, i32]
         L.torq_paged_attention.restype = i32
         L.torq_paged_attention.argtypes = [vp, vp, i64, i64, i32, vp, i64, i32, vp, i64, C.c_float, vp, vp, sz, vp]
+        L.torq_paged_attention_scores.restype = i32
+        L.torq_paged_attention_scores.argtypes = [vp, vp, i64, i64, i32, vp, i64, i32, vp, i64, C.c_float, vp, vp, vp, sz, vp]
+        L.torq_chunk_attention_workspace_bytes.restype = sz
+        L.torq_chunk_attention_workspace_bytes.argtypes = [vp, i32, i64, i32, i64, i32]
+        L.torq_chunk_attention.restype = i32
+        L.torq_chunk_attention.argtypes = [vp, vp, i64, i64, i32, i64, vp, i32, vp, i64, i32, vp, i64, C.c_float, vp, vp, vp, sz, vp]
         L.torq_add_rms_norm.restype = i32
         L.torq_add_rms_norm.argtypes = [vp, vp, vp, i64, i32, C.c_float, i32, vp, vp, vp, vp]
         L.torq_diag_mfma_burn.restype = i32
@@ -202,6 +214,7 @@ class _Interpreted:
     """In the place of the C++ module where there is none for this interpreter and torch: it takes no call."""
     linear = rotate_quantize = gram = histogram = staticmethod(lambda *args: None)
     block_tables = cache_append = paged_attention = add_rms_norm = staticmethod(lambda *args: None)
+    chunk_attention = staticmethod(lambda *args: None)
 
 
 _host = None
@@ -227,7 +240,8 @@ def _native():
         names = ["torq_linear", "torq_linear_workspace_bytes_n", "torq_rotate_quantize", "torq_rotate_quantize_fmt",
                  "torq_block_gram", "torq_block_gram_positions", "torq_block_gram_workspace_bytes", "torq_code_histogram",
                  "torq_code_histogram_workspace_bytes", "torq_block_tables", "torq_cache_append", "torq_paged_attention",
-                 "torq_paged_attention_workspace_bytes", "torq_add_rms_norm"]
+                 "torq_paged_attention_workspace_bytes", "torq_paged_attention_scores", "torq_chunk_attention",
+                 "torq_chunk_attention_workspace_bytes", "torq_add_rms_norm"]
         module.bind({n: C.cast(getattr(L, n), C.c_void_p).value for n in names}, _stream, _check)
         _host = module
     return _host
@@ -721,8 +735,9 @@ def _rows(t: torch.Tensor, dtype, dims: int, what):
 
 
 class KVCache:
-    """A paged cache of keys and values: k and v [pages, heads, page_size, head_dim], bf16 or float8_e4m3fn, the latter with scales
-    [pages, heads, page_size, head_dim / 32] float8_e8m0fnu (or the same bytes as uint8).  k and v may be views, with a page's
+    """A paged cache of keys and values: k and v [pages, heads, page_size, head_dim], bf16 or float8_e4m3fn (MXFP8), or uint8 [..., head_dim / 2],
+    two E2M1 codes to a byte (MXFP4); the last two with scales [pages, heads, page_size, head_dim / 32] float8_e8m0fnu (or the same bytes as
+    uint8).  k and v may be views, with a page's
     tokens ahead of its heads or the two in one tensor, but lie alike; the scales lie like the elements.  The tensors are the
     caller's: the cache keeps them alive, and what they hold may change at any time, but not where they lie: the calls go by the addresses
     of the construction, and other tensors take a KVCache of their own.  The calls below take caches on the GPU of their other tensors
@@ -733,26 +748,28 @@ class KVCache:
                                           for name in ("format", "heads", "head_dim", "page_size"))
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales=None, v_scales=None):
-        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.dtype not in (torch.bfloat16, _E4M3):
-            raise ValueError("k and v must be [pages, heads, page_size, head_dim], both bfloat16 or both float8_e4m3fn")
-        mx = k.dtype == _E4M3
+        formats = {torch.bfloat16: (TORQ_FMT_BF16, 1), _E4M3: (TORQ_FMT_MXFP8, 1), torch.uint8: (TORQ_FMT_MXFP4, 2)}
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.dtype not in formats:
+            raise ValueError("k and v must be [pages, heads, page_size, head_dim], both bfloat16 or both float8_e4m3fn, or of codes in bytes, both uint8")
+        fmt, packed = formats[k.dtype]
         scales = [t for t in (k_scales, v_scales) if t is not None]
-        if len(scales) != (2 if mx else 0):
-            raise ValueError("float8_e4m3fn keys and values come with scales for both, bfloat16 ones without")
+        if len(scales) != (2 if fmt != TORQ_FMT_BF16 else 0):
+            raise ValueError("float8_e4m3fn and 4-bit keys and values come with scales for both, bfloat16 ones without")
         # a dimension of one entry has no stride to speak of
-        strides = [st if n > 1 else 0 for n, st in zip(k.shape, k.stride())]
+        strides = [st * packed if n > 1 else 0 for n, st in zip(k.shape, k.stride())]
         alike = lambda t, unit: all(n <= 1 or st * unit == mine for n, st, mine in zip(t.shape[:3], t.stride()[:3], strides))
-        if (k.shape[3] > 1 and (k.stride(3) != 1 or v.stride(3) != 1)) or not alike(v, 1):
+        if (k.shape[3] > 1 and (k.stride(3) != 1 or v.stride(3) != 1)) or not alike(v, packed):
             raise ValueError("k and v must have the same strides and be contiguous along the last dimension")
+        pages, heads, page_size, head_dim = k.shape
+        head_dim *= packed
         for t in scales:
-            if t.dtype not in (_E8M0, torch.uint8) or t.shape != (*k.shape[:3], k.shape[3] // 32) or t.device != k.device:
+            if t.dtype not in (_E8M0, torch.uint8) or t.shape != (*k.shape[:3], head_dim // 32) or t.device != k.device:
                 raise ValueError("scales must be [pages, heads, page_size, head_dim / 32], float8_e8m0fnu or uint8")
             if not alike(t, 32) or (t.shape[3] > 1 and t.stride(3) != 1):
                 raise ValueError("scales must lie like the elements, a 32nd of the strides")
         self._tensors = k, v, k_scales, v_scales
-        pages, heads, page_size, head_dim = k.shape
-        self._struct = _KVCacheStruct(k.data_ptr(), v.data_ptr(), *((t.data_ptr() for t in scales) if mx else (None, None)),
-                                      pages, *strides[:3], TORQ_FMT_MXFP8 if mx else TORQ_FMT_BF16, heads, head_dim, page_size)
+        self._struct = _KVCacheStruct(k.data_ptr(), v.data_ptr(), *((t.data_ptr() for t in scales) if scales else (None, None)),
+                                      pages, *strides[:3], fmt, heads, head_dim, page_size)
         # what the calls go by; on the host there is nothing that a kernel could be given
         self.kv_handle, self.kv_device = (C.c_void_p(C.addressof(self._struct)), k.get_device()) if k.is_cuda else (None, -1)
 
@@ -761,10 +778,37 @@ class KVCache:
         """A cache of its own, not initialised."""
         if fmt == TORQ_FMT_BF16:
             return cls(*(torch.empty((pages, heads, page_size, head_dim), dtype=torch.bfloat16, device=device) for _ in "kv"))
-        if fmt != TORQ_FMT_MXFP8 or head_dim % 32:
-            raise ValueError("a cache is TORQ_FMT_BF16, or TORQ_FMT_MXFP8 with a head_dim that is a multiple of 32")
-        return cls(*(torch.empty((pages, heads, page_size, n), dtype=t, device=device)
-                     for t, n in ((_E4M3, head_dim), (_E8M0, head_dim // 32)) for _ in "kv"))
+        if fmt not in (TORQ_FMT_MXFP8, TORQ_FMT_MXFP4) or head_dim % 32:
+            raise ValueError("a cache is TORQ_FMT_BF16, or TORQ_FMT_MXFP8 or TORQ_FMT_MXFP4 with a head_dim that is a multiple of 32")
+        elements = (_E4M3, head_dim) if fmt == TORQ_FMT_MXFP8 else (torch.uint8, head_dim // 2)
+        return cls(*(torch.empty((pages, heads, page_size, n), dtype=t, device=device) for t, n in (elements, (_E8M0, head_dim // 32)) for _ in "kv"))
+
+
+class Scores:
+    """How a model gives its scores beyond scale q . k (see include/torq.h): capped by cap tanh(s / cap), less slopes[heads] (float32) times the
+    distance, of the last `window` keys only, with the first prefix [B] (int32) keys of a request seen from everywhere.  The tensors are the
+    caller's; the object keeps them alive, and what they hold may change at any time."""
+
+    cap, window = (property(lambda self, name=name: getattr(self._struct, name)) for name in ("cap", "window"))
+    slopes, prefix = (property(lambda self, i=i: self._tensors[i]) for i in range(2))
+
+    def __init__(self, cap: float = 0.0, slopes=None, window: int = 0, prefix=None):
+        for t, dtype, what in ((slopes, torch.float32, "slopes [heads]"), (prefix, torch.int32, "prefix [B]")):
+            if t is not None and (t.dtype != dtype or t.dim() != 1 or not t.is_contiguous()):
+                raise ValueError(f"{what}: expected a contiguous {dtype} tensor of one dimension")
+        if not 0 <= cap <= 1e30:
+            raise ValueError("cap must be at least 0 (none) and at most 1e30")
+        if not 0 <= window < 1 << 31:
+            raise ValueError("window must be at least 0 (none) and below 2^31")
+        self._tensors = slopes, prefix
+        self._struct = _ScoresStruct(cap, window, *(None if t is None else t.data_ptr() for t in self._tensors))
+        self.scores_handle = C.c_void_p(C.addressof(self._struct))
+
+    def check(self, heads: int, B: int, device):
+        """Raises where it does not go with so many query heads and requests on that GPU."""
+        for t, n, what in ((self.slopes, heads, "slopes"), (self.prefix, B, "prefix")):
+            if t is not None and (t.shape != (n,) or t.device != device):
+                raise ValueError(f"scores: {what} must be [{n}] on {device}, is {list(t.shape)} on {t.device}")
 
 
 def _kv(cache: KVCache, with_it: torch.Tensor, what):
@@ -816,10 +860,20 @@ def torq_paged_attention_workspace_bytes(cache: KVCache, heads: int, B: int, wid
     return int(lib().torq_paged_attention_workspace_bytes(C.addressof(cache._struct), heads, B, width))
 
 
-def torq_paged_attention(q, cache: KVCache, block_tables, lengths, scale: float, out=None, workspace=None, stream=None):
+def _scores(scores, heads, B, device):
+    """The handle of a call's scores, None without."""
+    if scores is None:
+        return None
+    if not isinstance(scores, Scores):
+        raise ValueError("scores: expected a Scores")
+    scores.check(heads, B, device)
+    return scores.scores_handle
+
+
+def torq_paged_attention(q, cache: KVCache, block_tables, lengths, scale: float, out=None, workspace=None, stream=None, scores=None):
     """q [B, heads, head_dim] bf16 (a view will do), one new token of each request, over its first lengths[b] tokens, which
-    block_tables [B, width] finds in the cache.  Returns out [B, heads, head_dim] bf16."""
-    y = (_host or _native()).paged_attention(q, cache, block_tables, lengths, scale, out, workspace, stream)
+    block_tables [B, width] finds in the cache, with scores by a rule where `scores` (Scores) is given.  Returns out [B, heads, head_dim] bf16."""
+    y = (_host or _native()).paged_attention(q, cache, block_tables, lengths, scale, out, workspace, stream, scores)
     if y is not None:
         return y
     handle = _kv(cache, q, "q")
@@ -827,6 +881,7 @@ def torq_paged_attention(q, cache: KVCache, block_tables, lengths, scale: float,
     width = block_tables.shape[-1]
     if dim != cache.head_dim or block_tables.shape != (B, width) or lengths.shape != (B,):
         raise ValueError("q must be [B, heads, head_dim], block_tables [B, width], lengths [B]")
+    rule = _scores(scores, heads, B, q.device)
     if workspace is None:
         workspace = _scratch(q, max(torq_paged_attention_workspace_bytes(cache, heads, B, width), 16), stream)
     if out is None:
@@ -834,11 +889,48 @@ def torq_paged_attention(q, cache: KVCache, block_tables, lengths, scale: float,
     if out.shape != q.shape:
         raise ValueError("out must be [B, heads, head_dim]")
     at = [st if n > 1 else 0 for n, st in zip(q.shape[:2], q.stride())]
-    _check(lib().torq_paged_attention(handle, _rows(q, torch.bfloat16, 3, "q"), *at, heads,
-                                      _rows(block_tables, torch.int32, 2, "block_tables"), block_tables.stride(0) if B > 1 else width,
-                                      width, _dev(lengths, torch.int32, "lengths"), B, float(scale), _dev(out, torch.bfloat16, "out"),
+    head = (handle, _rows(q, torch.bfloat16, 3, "q"), *at, heads, _rows(block_tables, torch.int32, 2, "block_tables"),
+            block_tables.stride(0) if B > 1 else width, width, _dev(lengths, torch.int32, "lengths"), B, float(scale))
+    tail = (_dev(out, torch.bfloat16, "out"), _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    if rule is None:
+        _check(lib().torq_paged_attention(*head, *tail), "torq_paged_attention")
+    else:
+        _check(lib().torq_paged_attention_scores(*head, rule, *tail), "torq_paged_attention_scores")
+    return out
+
+
+def torq_chunk_attention_workspace_bytes(cache: KVCache, heads: int, tokens: int, most: int, B: int, width: int) -> int:
+    return int(lib().torq_chunk_attention_workspace_bytes(C.addressof(cache._struct), heads, tokens, most, B, width))
+
+
+def torq_chunk_attention(q, starts, cache: KVCache, block_tables, lengths, scale: float, most=None, scores=None, out=None, workspace=None,
+                         stream=None):
+    """q [tokens, heads, head_dim] bf16 (a view will do), rows starts[b] ... starts[b + 1] - 1 the last tokens of request b, each over the keys up
+    to its own (or by `scores`) among the first lengths[b] tokens, which block_tables [B, width] finds in the cache; starts [B + 1] int32.  most: no
+    request has more new tokens (all of them, if not given: what is known goes into the choice of the kernel).  Returns out [tokens, heads,
+    head_dim] bf16, where rows of no request are left as they were."""
+    y = (_host or _native()).chunk_attention(q, starts, cache, block_tables, lengths, scale, most, scores, out, workspace, stream)
+    if y is not None:
+        return y
+    handle = _kv(cache, q, "q")
+    T, heads, dim = q.shape
+    B, width = block_tables.shape
+    if dim != cache.head_dim or starts.shape != (B + 1,) or lengths.shape != (B,):
+        raise ValueError("q must be [tokens, heads, head_dim], starts [B + 1], block_tables [B, width], lengths [B]")
+    rule = _scores(scores, heads, B, q.device)
+    most = max(T, 1) if most is None else int(most)
+    if workspace is None:
+        workspace = _scratch(q, max(torq_chunk_attention_workspace_bytes(cache, heads, T, most, B, width), 16), stream)
+    if out is None:
+        out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=q.device)
+    if out.shape != q.shape:
+        raise ValueError("out must be [tokens, heads, head_dim]")
+    at = [st if n > 1 else 0 for n, st in zip(q.shape[:2], q.stride())]
+    _check(lib().torq_chunk_attention(handle, _rows(q, torch.bfloat16, 3, "q"), *at, heads, T, _dev(starts, torch.int32, "starts"), most,
+                                      _rows(block_tables, torch.int32, 2, "block_tables"), block_tables.stride(0) if B > 1 else width, width,
+                                      _dev(lengths, torch.int32, "lengths"), B, float(scale), rule, _dev(out, torch.bfloat16, "out"),
                                       _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)),
-           "torq_paged_attention")
+           "torq_chunk_attention")
     return out
 
 

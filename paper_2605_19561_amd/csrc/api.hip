@@ -843,7 +843,7 @@ inline bool misaligned_to(const void *p, size_t n) { return (reinterpret_cast<ui
 
 // TORQ_OK, or what is wrong with the sizes of a cache (its arrays are looked at by the calls that touch them)
 int cache_sizes(const torq_kv_cache_t *c) {
-  if (!c || (c->format != TORQ_FMT_BF16 && c->format != TORQ_FMT_MXFP8)) return TORQ_EINVAL;
+  if (!c || (c->format != TORQ_FMT_BF16 && c->format != TORQ_FMT_MXFP8 && c->format != TORQ_FMT_MXFP4)) return TORQ_EINVAL;
   const int unit = c->format == TORQ_FMT_BF16 ? 8 : 32;
   if (c->heads <= 0 || c->head_dim <= 0 || c->head_dim > TORQ_MAX_HEAD_DIM || c->head_dim % unit) return TORQ_EINVAL;
   if (c->page_size <= 0 || c->page_size % 16 || c->page_size > 65536 || c->pages < 0 || c->pages > 0x7FFFFFFF) return TORQ_EINVAL;
@@ -854,7 +854,7 @@ int cache_sizes(const torq_kv_cache_t *c) {
 }
 int cache_arrays(const torq_kv_cache_t *c) {
   if (c->pages == 0) return TORQ_OK;                 // (nothing of them is touched)
-  if (!c->k || !c->v || (c->format == TORQ_FMT_MXFP8 && (!c->k_scales || !c->v_scales))) return TORQ_EINVAL;
+  if (!c->k || !c->v || (c->format != TORQ_FMT_BF16 && (!c->k_scales || !c->v_scales))) return TORQ_EINVAL;
   return misaligned(c->k) || misaligned(c->v) ? TORQ_EALIGN : TORQ_OK;
 }
 inline bool bad_stride(int64_t stride) { return stride < 0 || stride % 8; }
@@ -866,6 +866,18 @@ bool attention_sizes(const torq_kv_cache_t *c, int heads, int64_t B, int width) 
   const int64_t most = (int64_t)width * c->page_size, columns = B * c->heads * ((heads / c->heads + 15) / 16);
   return most <= (int64_t)1 << 30 && columns <= 0x7FFFFFFF / (most / 32 + 8);
 }
+
+// the same for `tokens` new tokens, up to `most` of a request, whose heads are then the query heads
+bool chunk_sizes(const torq_kv_cache_t *c, int heads, int64_t tokens, int most, int64_t B, int width) {
+  if (heads <= 0 || heads % c->heads || heads > (1 << 20) || tokens < 0 || tokens > 0x7FFFFFFF / heads || most <= 0 || B < 0 || width < 0) return false;
+  if (B > 0x7FFFFFFF) return false;
+  const int64_t keys = (int64_t)width * c->page_size, rows = (int64_t)(heads / c->heads) * most;
+  if (keys > (int64_t)1 << 30) return false;
+  const int64_t columns = (rows + 15) / 16, left = 0x7FFFFFFF / (keys / 32 + 8);
+  return columns <= left && (B == 0 || columns * c->heads <= left / B);
+}
+bool scores_fine(const torq_scores_t *s) { return !s || (s->window >= 0 && s->cap >= 0.0f && s->cap <= 1e30f); }
+bool scores_misaligned(const torq_scores_t *s) { return s && (misaligned_to(s->slopes, 4) || misaligned_to(s->prefix, 4)); }
 
 }  // namespace
 
@@ -907,23 +919,57 @@ size_t torq_paged_attention_workspace_bytes(const torq_kv_cache_t *cache, int he
   return torq::paged_attention_workspace_bytes(*cache, heads, B, width);
 }
 
-int torq_paged_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads,
-                         const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths, int64_t B,
-                         float scale, void *out_bf16, void *workspace, size_t workspace_bytes, void *stream) {
+int torq_paged_attention_scores(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads,
+                                const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths, int64_t B,
+                                float scale, const torq_scores_t *scores, void *out_bf16, void *workspace, size_t workspace_bytes,
+                                void *stream) {
   int status = cache_sizes(cache);
   if (status != TORQ_OK) return status;
   if (!attention_sizes(cache, heads, B, width) || table_stride < width || bad_stride(q_stride) || bad_stride(q_head_stride) ||
-      !std::isfinite(scale))
+      !std::isfinite(scale) || !scores_fine(scores))
     return TORQ_EINVAL;
   if (B == 0) return TORQ_OK;
   const size_t need = torq::paged_attention_workspace_bytes(*cache, heads, B, width);
   status = cache_arrays(cache);
   if (status == TORQ_EINVAL || !q_bf16 || (width > 0 && !block_tables) || !lengths || !out_bf16 || (need && !workspace)) return TORQ_EINVAL;
   if (status != TORQ_OK || misaligned(q_bf16) || misaligned(out_bf16) || misaligned(workspace)) return TORQ_EALIGN;
-  if (misaligned_to(block_tables, 4) || misaligned_to(lengths, 4)) return TORQ_EALIGN;
+  if (misaligned_to(block_tables, 4) || misaligned_to(lengths, 4) || scores_misaligned(scores)) return TORQ_EALIGN;
   if (workspace_bytes < need) return TORQ_EWORKSPACE;
   hipError_t e = torq::launch_paged_attention(*cache, q_bf16, q_stride, q_head_stride, heads, block_tables, table_stride, width,
-                                              lengths, B, scale, out_bf16, workspace, (hipStream_t)stream);
+                                              lengths, B, scale, out_bf16, workspace, scores, nullptr, 1, B, (hipStream_t)stream);
+  return e == hipSuccess ? TORQ_OK : hip_fail(e);
+}
+
+int torq_paged_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads,
+                         const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths, int64_t B,
+                         float scale, void *out_bf16, void *workspace, size_t workspace_bytes, void *stream) {
+  return torq_paged_attention_scores(cache, q_bf16, q_stride, q_head_stride, heads, block_tables, table_stride, width, lengths, B, scale, nullptr,
+                                     out_bf16, workspace, workspace_bytes, stream);
+}
+
+size_t torq_chunk_attention_workspace_bytes(const torq_kv_cache_t *cache, int heads, int64_t tokens, int most, int64_t B, int width) {
+  if (cache_sizes(cache) != TORQ_OK || !chunk_sizes(cache, heads, tokens, most, B, width) || B == 0 || tokens == 0) return 0;
+  return torq::chunk_attention_workspace_bytes(*cache, heads, tokens, most, B, width);
+}
+
+int torq_chunk_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads, int64_t tokens,
+                         const int32_t *starts, int most, const int32_t *block_tables, int64_t table_stride, int width,
+                         const int32_t *lengths, int64_t B, float scale, const torq_scores_t *scores, void *out_bf16, void *workspace,
+                         size_t workspace_bytes, void *stream) {
+  int status = cache_sizes(cache);
+  if (status != TORQ_OK) return status;
+  if (!chunk_sizes(cache, heads, tokens, most, B, width) || table_stride < width || bad_stride(q_stride) || bad_stride(q_head_stride) ||
+      !std::isfinite(scale) || !scores_fine(scores))
+    return TORQ_EINVAL;
+  if (B == 0 || tokens == 0) return TORQ_OK;
+  const size_t need = torq::chunk_attention_workspace_bytes(*cache, heads, tokens, most, B, width);
+  status = cache_arrays(cache);
+  if (status == TORQ_EINVAL || !q_bf16 || !starts || (width > 0 && !block_tables) || !lengths || !out_bf16 || (need && !workspace)) return TORQ_EINVAL;
+  if (status != TORQ_OK || misaligned(q_bf16) || misaligned(out_bf16) || misaligned(workspace)) return TORQ_EALIGN;
+  if (misaligned_to(block_tables, 4) || misaligned_to(lengths, 4) || misaligned_to(starts, 4) || scores_misaligned(scores)) return TORQ_EALIGN;
+  if (workspace_bytes < need) return TORQ_EWORKSPACE;
+  hipError_t e = torq::launch_chunk_attention(*cache, q_bf16, q_stride, q_head_stride, heads, tokens, starts, most, block_tables, table_stride,
+                                              width, lengths, B, scale, scores, out_bf16, workspace, (hipStream_t)stream);
   return e == hipSuccess ? TORQ_OK : hip_fail(e);
 }
 

@@ -1,6 +1,6 @@
 // The calls of the binding that a program makes again and again, marshalled in C++ (module _host): torq_linear,
 // torq_rotate_quantize (and _fmt), torq_block_gram (and _positions), torq_code_histogram, torq_block_tables, torq_cache_append,
-// torq_paged_attention and torq_add_rms_norm.  The kernels of the smallest of
+// torq_paged_attention, torq_chunk_attention and torq_add_rms_norm.  The kernels of the smallest of
 // them take 3 to 6 us, the interpreter 8 to 13 for the attribute look-ups, checks, allocations and a ctypes call.  One row
 // through a 4096 x 4096 layer, a call among others: 10.2 us -> 5.6 or 6.4 from one process to the next (the kernel, replayed from a
 // graph, 5.7).
@@ -40,9 +40,12 @@ decltype(&torq_block_tables) f_tables;
 decltype(&torq_cache_append) f_append;
 decltype(&torq_paged_attention) f_attention;
 decltype(&torq_paged_attention_workspace_bytes) f_attention_bytes;
+decltype(&torq_paged_attention_scores) f_attention_scores;
+decltype(&torq_chunk_attention) f_chunk;
+decltype(&torq_chunk_attention_workspace_bytes) f_chunk_bytes;
 decltype(&torq_add_rms_norm) f_norm;
 PyObject *py_stream, *py_check;
-PyObject *s_handle, *s_kv_handle, *s_kv_device, *s_value, *s_d;
+PyObject *s_handle, *s_kv_handle, *s_kv_device, *s_scores_handle, *s_tensors, *s_value, *s_d;
 
 struct NotPlain {};
 
@@ -338,10 +341,24 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// paged_attention(q, cache, block_tables, lengths, scale, out, workspace, stream)
+// the scores of a call, whose tensors have the call's sizes and lie on its GPU; nullptr without
+const torq_scores_t *scores_of(PyObject *scores, int64_t heads, int64_t B, const Tensor &with_it) {
+  if (scores == Py_None) return nullptr;
+  Ref tensors(PyObject_GetAttr(scores, s_tensors));
+  if (!PyTuple_CheckExact(tensors.p) || PyTuple_GET_SIZE(tensors.p) != 2) throw NotPlain{};
+  for (int i = 0; i < 2; ++i) {
+    const Tensor *t = optional(PyTuple_GET_ITEM(tensors.p, i));
+    if (t && (t->dim() != 1 || t->size(0) != (i ? B : heads) || t->get_device() != with_it.get_device())) throw NotPlain{};
+  }
+  const torq_scores_t *s = static_cast<const torq_scores_t *>(handle_of(scores, s_scores_handle));
+  if (!s) throw NotPlain{};
+  return s;
+}
+
+// paged_attention(q, cache, block_tables, lengths, scale, out, workspace, stream, scores)
 PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return plain_or_none([&]() -> PyObject * {
-    if (n != 8) throw NotPlain{};
+    if (n != 9) throw NotPlain{};
     const Tensor &q = tensor(a[0]), &tables = tensor(a[2]), &lengths = tensor(a[3]);
     const torq_kv_cache_t *const cache = cache_of(a[1], q);
     const float scale = (float)number(a[4]);
@@ -353,6 +370,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     shape(q, {B, heads, cache->head_dim});
     if (tables.size(0) != B || heads > 0x7FFFFFFF || width > 0x7FFFFFFF) throw NotPlain{};
     if (out_in) shape(*out_in, q.sizes());
+    const torq_scores_t *const scores = scores_of(a[8], heads, B, q);
     void *const stream_p = stream_of(a[7]);
     const std::optional<c10::Stream> user = user_of(a[7], ws_in);
     Tensor out;
@@ -361,10 +379,48 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
       Unlocked unlocked;
       const Tensor ws = scratch(ws_in, q, ws_in ? 1 : std::max<int64_t>((int64_t)f_attention_bytes(cache, (int)heads, B, (int)width), 16), user);
       out = given_or_new(out_in, q, q.sizes(), at::kBFloat16);
-      status = f_attention(cache, qp, step(q, 0), step(q, 1), (int)heads, tp, B > 1 ? tables.stride(0) : width, (int)width, lp, B, scale,
-                           address(out, at::kBFloat16), address(ws, at::kByte), (size_t)ws.numel(), stream_p);
+      void *const op = address(out, at::kBFloat16), *const wp = address(ws, at::kByte);
+      const int64_t table_step = B > 1 ? tables.stride(0) : width;
+      status = scores ? f_attention_scores(cache, qp, step(q, 0), step(q, 1), (int)heads, tp, table_step, (int)width, lp, B, scale, scores, op, wp,
+                                           (size_t)ws.numel(), stream_p)
+                      : f_attention(cache, qp, step(q, 0), step(q, 1), (int)heads, tp, table_step, (int)width, lp, B, scale, op, wp,
+                                    (size_t)ws.numel(), stream_p);
     }
-    return ok(status, "torq_paged_attention") ? wrapped(a[5], out) : nullptr;
+    return ok(status, scores ? "torq_paged_attention_scores" : "torq_paged_attention") ? wrapped(a[5], out) : nullptr;
+  });
+}
+
+// chunk_attention(q, starts, cache, block_tables, lengths, scale, most or None, scores, out, workspace, stream)
+PyObject *chunk_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return plain_or_none([&]() -> PyObject * {
+    if (n != 11) throw NotPlain{};
+    const Tensor &q = tensor(a[0]), &starts = tensor(a[1]), &tables = tensor(a[3]), &lengths = tensor(a[4]);
+    const torq_kv_cache_t *const cache = cache_of(a[2], q);
+    const float scale = (float)number(a[5]);
+    const Tensor *out_in = optional(a[8]), *ws_in = optional(a[9]);
+    const void *const qp = rows(q, at::kBFloat16, 3);
+    const int32_t *const tp = static_cast<const int32_t *>(rows(tables, at::kInt, 2)), *const lp = static_cast<const int32_t *>(address(lengths, at::kInt)),
+                  *const sp = static_cast<const int32_t *>(address(starts, at::kInt));
+    const int64_t T = q.size(0), heads = q.size(1), B = tables.size(0), width = tables.size(1);
+    if (heads > 0x7FFFFFFF || width > 0x7FFFFFFF || T > 0x7FFFFFFF) throw NotPlain{};
+    shape(starts, {B + 1});
+    shape(lengths, {B});
+    shape(q, {T, heads, cache->head_dim});
+    if (out_in) shape(*out_in, q.sizes());
+    const int most = a[6] == Py_None ? (int)std::max<int64_t>(T, 1) : small_integer(a[6]);
+    const torq_scores_t *const scores = scores_of(a[7], heads, B, q);
+    void *const stream_p = stream_of(a[10]);
+    const std::optional<c10::Stream> user = user_of(a[10], ws_in);
+    Tensor out;
+    int status;
+    {
+      Unlocked unlocked;
+      const Tensor ws = scratch(ws_in, q, ws_in ? 1 : std::max<int64_t>((int64_t)f_chunk_bytes(cache, (int)heads, T, most, B, (int)width), 16), user);
+      out = given_or_new(out_in, q, q.sizes(), at::kBFloat16);
+      status = f_chunk(cache, qp, step(q, 0), step(q, 1), (int)heads, T, sp, most, tp, B > 1 ? tables.stride(0) : width, (int)width, lp, B, scale,
+                       scores, address(out, at::kBFloat16), address(ws, at::kByte), (size_t)ws.numel(), stream_p);
+    }
+    return ok(status, "torq_chunk_attention") ? wrapped(a[8], out) : nullptr;
   });
 }
 
@@ -432,6 +488,9 @@ PyObject *bind(PyObject *, PyObject *args) {
   TORQ_BIND(f_append, "torq_cache_append")
   TORQ_BIND(f_attention, "torq_paged_attention")
   TORQ_BIND(f_attention_bytes, "torq_paged_attention_workspace_bytes")
+  TORQ_BIND(f_attention_scores, "torq_paged_attention_scores")
+  TORQ_BIND(f_chunk, "torq_chunk_attention")
+  TORQ_BIND(f_chunk_bytes, "torq_chunk_attention_workspace_bytes")
   TORQ_BIND(f_norm, "torq_add_rms_norm")
 #undef TORQ_BIND
   Py_INCREF(stream);
@@ -452,6 +511,7 @@ PyMethodDef methods[] = {
     {"block_tables", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(block_tables)), METH_FASTCALL, nullptr},
     {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_append)), METH_FASTCALL, nullptr},
     {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attention)), METH_FASTCALL, nullptr},
+    {"chunk_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(chunk_attention)), METH_FASTCALL, nullptr},
     {"add_rms_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(add_rms_norm)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -462,9 +522,11 @@ PyMODINIT_FUNC PyInit__host() {
   s_handle = PyUnicode_InternFromString("handle");
   s_kv_handle = PyUnicode_InternFromString("kv_handle");
   s_kv_device = PyUnicode_InternFromString("kv_device");
+  s_scores_handle = PyUnicode_InternFromString("scores_handle");
+  s_tensors = PyUnicode_InternFromString("_tensors");
   s_value = PyUnicode_InternFromString("value");
   s_d = PyUnicode_InternFromString("d");
-  if (!s_handle || !s_kv_handle || !s_kv_device || !s_value || !s_d) return nullptr;
+  if (!s_handle || !s_kv_handle || !s_kv_device || !s_scores_handle || !s_tensors || !s_value || !s_d) return nullptr;
   PyObject *m = PyModule_Create(&module);
   // (binding.py binds no module built against another torch)
   if (m && PyModule_AddStringConstant(m, "torch_version", TORQ_TORCH_VERSION) != 0) Py_CLEAR(m);

@@ -1,131 +1,11 @@
-// torq_paged_attention: one new token of each request over its pages, out = softmax(scale q K^T) V for each head.
-//
-// The query heads of a key head are the columns of one matrix product, up to 16, or of two side by side, up to 32, so K and V are
-// read once for all of them: HBM-bound, 2 (bf16) or 1 1/32 (MXFP8) bytes for 2 heads / kv_heads flops.
-//
-// Work: the tokens of every (request, key head) in tiles of 32, all of them in one row of tiles (with room for what each one costs
-// besides), cut into equal runs, one for each workgroup: lengths may be as ragged as they like, and the host need not know them, since every
-// workgroup adds them up itself.  A run goes through one or several (request, key head)s.  The four waves of a workgroup take turns at
-// the tiles of one, each with a softmax of its own in one pass (running maximum m, sum l, unnormalised O), put together in LDS at its end; or
-// (few query heads for a key head and many of those, or more query heads than fit a column, whose waves then find the same lines in the cache)
-// each has one for itself and they need not wait for one another.  What lies whole within a run is written as output; of the others
-// O, m and l go to the workspace, two at most for a run (and wave), and a second kernel joins them in the order of the tokens.  Tables for
-// at most 512 tokens (1024 if there are many): one launch, a workgroup for each (request, key head).
-//
-// A tile goes through the matrix cores transposed, and nothing of it passes between lanes but the column maxima:
-//   S^T [token][head] = K [token][i] Q^T [i][head]           v_mfma_f32_16x16x32_bf16, two groups of 16 tokens
-//   lane (n = l % 16, g = l / 16) then holds head n's S for tokens 4g + r of both groups, r < 4
-//   O^T [i][head] += V^T [i][token] P^T [token][head]        the k index of this product runs over the 32 tokens in the order in
-//                                                            which the lanes hold them, so P^T is already its B operand
-// Its A operand wants 8 tokens of one i in a lane.  The lane loads, for its 8 tokens, E consecutive values of V (coalesced
-// rows), and pairs of them are put together by v_perm_b32: slot j holds V[its tokens][E * (l % 16) + j].
-// In MXFP8 the elements are widened to bf16 with their scale in one instruction, which takes of the scale its exponent field (so 0 is 2^-127 and
-// 0xFF NaN).  4 bits of significand: exact from scale byte 3 on, whose least element is 2^-133 as bf16's, up to 2^128.
-//
-// K and V of a wave's next tile are on their way while it works on this one, K from the moment that S is there, V from the
-// moment that O is.  The loads are buffer loads over the 16 tokens of a group (a group lies in one page) as far as they are tokens of
-// the request: what is past the length, in no page or past the last tile has no records, costs no traffic and comes back as
-// zeros, so the loop knows no other case (and a NaN behind the length is not read).
-//
-// Measured (called in turn over three caches, 303 MB to 1.9 GB; 7.1 TB/s is what reading alone reaches): 16 requests of 1000 to 8192 tokens, 64 query
-// and 8 key heads of 128, 55.2 us = 5.5 TB/s; one of 131072 87.6 us = 6.1; 45 of 8000 to 32768 in MXFP8 312 us = 6.2; 77 with 20 heads of 80 each, 85.9 us = 4.9.  The traffic
-// is what has to be read (counters within 1 %); vector instructions take a third (bf16) to half (MXFP8) of the time.  What is left over HBM's time: 5 to 7 us until
-// the first tiles are there, 5 for the join and its launch.  One request of 333 tokens 6.2 us, one launch: three rounds that
-// hang on one another; compiled apart, since the runs' code in the same kernel cost it 0.45 in a graph and 0.85 in a call.
+// torq_paged_attention: one new token of each request over its pages (and what torq_chunk_attention runs for few rows).  The mathematics, the
+// layout and what was measured stand in paged_attention_body.h; here are its kernels for bf16 and MXFP8 caches, the join, and who runs which.
 #include <algorithm>
+#include <cfloat>
 
-#include "torq_device.h"
-#include "torq_internal.h"
+#include "paged_attention_body.h"
 
 namespace torq {
-
-constexpr int ATT_TILE = 32;          // tokens of a wave's step
-constexpr int ATT_WAVES = 4;
-constexpr int ATT_ROWS = 16;          // query heads of a product's columns
-constexpr int ATT_JOIN = 512;         // threads of a workgroup that joins, at most
-// Columns from which each wave has one of its own, with up to 2 query heads for each or head_dim over 128.  77 x 20 heads 120 -> 91 us, 256 requests x 8 key heads
-// with 2 query heads each 144.6 -> 139.7; with 4 146.7 -> 151.1, with 8 153 -> 162 (four times the parts to join).  head_dim 256, 4 query heads each, 128 x 8
-// of 1000 to 1500 tokens 217 -> 213, MXFP8 of 1000 to 2500 174 -> 164.
-constexpr int ATT_WAYS_ITEMS = 768;
-// What a (request, key head) costs besides its tiles (its place, its query, putting it together), in tiles of the row of them that is cut
-// into runs, by the waves that take turns.  64 requests of 1 to 600 tokens, 64 / 8 heads, with 0, 4, 8, 16: 35.4, 24.1, 23.9, 23.7 us;
-// 16 of 1000 to 8192 58.6, 58.7, 59.1, 60.4; 77 x 20 heads, a wave each, with 0, 1, 2, 5: 89.6, 89.8, 92.8, 95.0.
-constexpr int att_setup(int ways) { return ways > 1 ? 4 : 1; }
-constexpr int ATT_FAR = 0x7FFFFF00;   // an offset past every buffer
-
-// What begins in a run and does not end there: a request, which of the columns that a workgroup works on at a time, the place of its first
-// part (that of nothing: -1; the others are first in their runs), its last tile, and the runs' lengths.
-struct alignas(16) Cut {
-  int b, column, place, last_tile, each, more;
-};
-
-struct AttentionArgs {
-  const char *k, *v;
-  const uint8_t *k_scales, *v_scales;
-  int64_t page_bytes, head_bytes;     // from one to the next
-  int pages, token_bytes;
-  const uint16_t *q;
-  int64_t q_stride, q_head_stride;
-  const int *tables, *lengths;
-  int64_t table_stride, page16_magic; // t / page_size = (t / 16) * page16_magic >> 38
-  int64_t most;                       // width * page_size
-  int B, page_size, kv_heads, group, rows, row_groups, dim;            // rows: query heads of a column at most
-  float scale_log2;                   // scale * log2(e): the softmax is taken to base 2
-  uint16_t *out;
-  float *part, *part_ml;              // [run][2][columns at a time][rows][dim] and [2]: O, and m and l, of what is not whole in a run
-  Cut *cuts;                          // [run], or [request][columns that a workgroup works on at a time]
-  int by_item;
-};
-
-// The runs: `tiles` tiles (of a column, or of several side by side) over `runs` workgroups, the first `more` of which have one more
-// than the others; a tile at least for each wave.
-struct Runs {
-  int each, more, runs;
-  __device__ Runs(int each, int more) : each(each), more(more), runs(0) {}
-  __device__ Runs(int tiles, int groups, int ways) {
-    runs = max(1, min(groups, (tiles + ways - 1) / ways));
-    each = tiles / runs, more = tiles - each * runs;
-  }
-  __device__ int begin(int run) const { return run * each + min(run, more); }
-  __device__ int of(int tile) const {
-    const int wide = more * (each + 1);
-    return tile < wide ? tile / (each + 1) : more + (tile - wide) / each;
-  }
-};
-
-__device__ __forceinline__ bf16x8 as_bf16(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
-// four E4M3 bytes -> two words of two bf16, times scale
-__device__ __forceinline__ void widen4(uint32_t v, float scale, uint32_t &a, uint32_t &b) {
-  a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, scale, false));
-  b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, scale, true));
-}
-typedef const __attribute__((address_space(4))) int *uniform_ints;      // read by scalar loads
-
-// `bytes` bytes from p as a raw buffer; all three the same in every lane
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t records(const void *base, int64_t at, int bytes) {
-  const uint64_t p = reinterpret_cast<uint64_t>(base) + at;
-  const uint64_t u = (uint32_t)__builtin_amdgcn_readfirstlane((int)p) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32;
-  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(u), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
-}
-template <int N, bool ONCE>
-__device__ __forceinline__ auto buffer_load(__amdgpu_buffer_rsrc_t r, int at) {
-  if constexpr (N == 16) return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, LOAD_POLICY<ONCE>);
-  else if constexpr (N == 8) return __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, LOAD_POLICY<ONCE>);
-  else return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, LOAD_POLICY<ONCE>);
-}
-
-// Over the four lanes l, l ^ 16, l ^ 32, l ^ 48 of a column: the rows of 16 lanes (then the halves of the wave) of a register with itself
-// exchanged, so that each lane has its own and the other's
-template <class F>
-__device__ __forceinline__ float over_column(float v, F &&op) {
-  const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = op(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
-  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return op(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
-}
-
-// Tokens of a request.
-__device__ __forceinline__ int length_of(const AttentionArgs &a, int n) { return n < 0 ? 0 : n < a.most ? n : (int)a.most; }
 
 // DP: head_dim rounded up to what the operands hold.  WAYS: 4, the waves take turns at the tiles of a column; 1, each has a column
 // of its own and all of its tiles in the run.  RT: products side by side, for up to 16 query heads each.  SOLO: a workgroup for each
@@ -596,7 +476,12 @@ __global__ void __launch_bounds__(ATT_JOIN) paged_attention_join_kernel(Attentio
   *reinterpret_cast<bf16x4 *>(out + 4 * c) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
 }
 
+__global__ void __launch_bounds__(ATT_JOIN) scored_attention_join_kernel(AttentionArgs a, int together, int many) {
+  attention_join_body<true>(a, together, many);
+}
+
 namespace {
+int bits_of(const torq_kv_cache_t &cache) { return cache.format == FMT_BF16 ? 16 : cache.format == FMT_MXFP8 ? 8 : 4; }
 // Query heads of a column: 32 where there are more than 16, the registers hold two products side by side, and there are columns
 // enough without the second 16.  24 heads for each of 8 key heads of 128, 1, 4, 16 requests of 1000 to 8192 tokens with 16 / 32:
 // 12.3 / 13.1, 28.9 / 26.4, 79.8 / 65.6 us (32 heads 83.1 / 68.6, heads of 64 49.1 / 39.2, MXFP8 up to 32768 199 / 139); for one
@@ -614,17 +499,12 @@ int row_groups_of(const torq_kv_cache_t &cache, int heads, int64_t B) {
 // lose: heads of 80 168 MB 40.1 / 42.7, of 96 in MXFP8, tokens outermost, 208 MB 70.8 / 83.6.
 bool once_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   if (row_groups_of(cache, heads, B) > 1) return false;
-  const int bytes = cache.format == FMT_BF16 ? 2 : 1;
   const double pages = (double)std::min<int64_t>(cache.pages, B * (int64_t)width);
-  return cache.head_dim * bytes % 128 == 0 && 2.0 * pages * cache.page_size * cache.heads * cache.head_dim * bytes > ONE_PASS_WEIGHT_BYTES;
+  const int row = cache.head_dim * bits_of(cache) / 8;
+  return row % 128 == 0 && 2.0 * pages * cache.page_size * cache.heads * row > ONE_PASS_WEIGHT_BYTES;
 }
-struct Plan {
-  int ways, groups, rows;
-  bool solo, by_item;
-  int64_t items;
-};
-Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
-  Plan p;
+AttentionPlan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
+  AttentionPlan p;
   p.rows = rows_of(cache, heads, B);
   const int64_t columns = (int64_t)cache.heads * row_groups_of(cache, heads, B), tiles = ((int64_t)width * cache.page_size + ATT_TILE - 1) / ATT_TILE;
   // Every request within so few tokens that a workgroup each is done before runs would be made out and joined.  In runs / a workgroup each, us: 333
@@ -634,7 +514,7 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   // (and within a launch, which runs always are)
   p.solo = (tiles <= 16 || (tiles <= 32 && B * columns >= 128)) && B * columns <= most_workgroups(256);
   bool own;                                         // each wave has a column of its own
-  const bool alone = cache.head_dim > 128, mx = cache.format == FMT_MXFP8;
+  const bool alone = cache.head_dim > 128, mx = cache.format != FMT_BF16;
   const int64_t idle = -columns & (ATT_WAVES - 1), workgroups = B * (columns + idle) / ATT_WAVES;
   auto busy = [&](int eighths) { return 8 * columns >= eighths * (columns + idle); };
   if (p.solo) {
@@ -686,29 +566,46 @@ Plan plan_of(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
   p.by_item = p.items < p.groups;
   return p;
 }
-size_t cuts_bytes(const Plan &p) { return (p.by_item ? (size_t)p.items : (size_t)p.groups) * sizeof(Cut); }
-size_t part_rows(const Plan &p) { return (size_t)p.groups * 2 * (ATT_WAVES / p.ways) * p.rows; }
+size_t cuts_bytes(const AttentionPlan &p) { return (p.by_item ? (size_t)p.items : (size_t)p.groups) * sizeof(Cut); }
+size_t part_rows(const AttentionPlan &p) { return (size_t)p.groups * 2 * (ATT_WAVES / p.ways) * p.rows; }
 }  // namespace
 
 size_t paged_attention_workspace_bytes(const torq_kv_cache_t &cache, int heads, int64_t B, int width) {
-  const Plan p = plan_of(cache, heads, B, width);
+  const AttentionPlan p = plan_of(cache, heads, B, width);
   return p.solo ? 0 : cuts_bytes(p) + part_rows(p) * (cache.head_dim + 2) * sizeof(float);
+}
+
+AttentionArgs attention_args(const torq_kv_cache_t &cache, const void *q, int64_t q_stride, int64_t q_head_stride, int heads,
+                             const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths, int64_t B, float scale,
+                             void *out, const torq_scores_t *scores, const int32_t *starts, int most, int64_t tokens) {
+  if (cache.pages == 0) width = 0;                  // no token has a page: nothing of the cache is touched
+  const int bits = bits_of(cache), each = heads / cache.heads;
+  const torq_scores_t plain = {}, &rule = scores ? *scores : plain;
+  const float log2e = 1.44269504088896340736f;
+  AttentionArgs a{};
+  a.k = (const char *)cache.k, a.v = (const char *)cache.v, a.k_scales = cache.k_scales, a.v_scales = cache.v_scales;
+  a.page_bytes = cache.page_stride * bits / 8, a.head_bytes = cache.head_stride * bits / 8, a.token_bytes = (int)(cache.token_stride * bits / 8);
+  a.pages = (int)cache.pages, a.page_size = cache.page_size, a.page16_magic = ((int64_t)1 << 38) / (cache.page_size / 16) + 1;
+  a.q = (const uint16_t *)q, a.q_stride = q_stride, a.q_head_stride = q_head_stride, a.out = (uint16_t *)out;
+  a.tables = block_tables, a.lengths = lengths, a.table_stride = table_stride, a.most = (int64_t)width * cache.page_size;
+  a.B = (int)B, a.kv_heads = cache.heads, a.group = each * most, a.dim = cache.head_dim, a.scale_log2 = scale * log2e;
+  a.rule = ScoreArgs{0.0f, 0.0f, rule.slopes, rule.prefix, starts, rule.window, most, each, tokens};
+  if (rule.cap > 0.0f) a.rule.cap_in = std::max(-FLT_MAX, std::min(FLT_MAX, scale / rule.cap)), a.rule.cap_out = rule.cap * log2e;
+  return a;
 }
 
 hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, int64_t q_stride, int64_t q_head_stride, int heads,
                                   const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths,
-                                  int64_t B, float scale, void *out, void *workspace, hipStream_t stream) {
-  const Plan plan = plan_of(cache, heads, B, width);
-  const bool f8 = cache.format == FMT_MXFP8, once = once_of(cache, heads, B, width);
-  if (cache.pages == 0) width = 0;                  // no token has a page: nothing of the cache is touched
-  const int page16 = cache.page_size / 16, bytes = f8 ? 1 : 2;
-  float *const part = (float *)((uintptr_t)workspace + cuts_bytes(plan));
-  AttentionArgs a{(const char *)cache.k, (const char *)cache.v, cache.k_scales, cache.v_scales, cache.page_stride * bytes,
-                  cache.head_stride * bytes, (int)cache.pages, (int)cache.token_stride * bytes, (const uint16_t *)q, q_stride,
-                  q_head_stride, block_tables, lengths, table_stride, ((int64_t)1 << 38) / page16 + 1,
-                  (int64_t)width * cache.page_size, (int)B, cache.page_size, cache.heads, heads / cache.heads, plan.rows, row_groups_of(cache, heads, B),
-                  cache.head_dim, scale * 1.44269504088896340736f, (uint16_t *)out, part, part + part_rows(plan) * cache.head_dim,
-                  (Cut *)workspace, plan.by_item};
+                                  int64_t B, float scale, void *out, void *workspace, const torq_scores_t *scores,
+                                  const int32_t *starts, int most, int64_t tokens, hipStream_t stream) {
+  const int rows = heads * most;                    // a request's new tokens' heads
+  const AttentionPlan plan = plan_of(cache, rows, B, width);
+  const bool f8 = cache.format == FMT_MXFP8, once = once_of(cache, rows, B, width);
+  AttentionArgs a = attention_args(cache, q, q_stride, q_head_stride, heads, block_tables, table_stride, width, lengths, B, scale, out, scores, starts,
+                                   most, tokens);
+  a.rows = plan.rows, a.row_groups = row_groups_of(cache, rows, B);
+  a.cuts = (Cut *)workspace, a.by_item = plan.by_item;
+  a.part = (float *)((uintptr_t)workspace + cuts_bytes(plan)), a.part_ml = a.part + part_rows(plan) * cache.head_dim;
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(plan.groups), dim3(256), 0, stream, a); };
   auto of_hint = [&](auto dp, auto of8, auto hint) {
     constexpr int DP = decltype(dp)::value;
@@ -732,14 +629,17 @@ hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, i
     of_hint(dp, of8, std::false_type{});
   };
   auto of_dim = [&](auto dp) { f8 ? of_format(dp, std::true_type{}) : of_format(dp, std::false_type{}); };
-  if (cache.head_dim <= 64) of_dim(std::integral_constant<int, 64>{});
+  const bool ruled = scores || starts;
+  if (ruled) (cache.format == FMT_BF16 ? go_scored_bf16 : f8 ? go_scored_mxfp8 : go_scored_mxfp4)(plan, a, once, stream);
+  else if (cache.format == FMT_MXFP4) go_attention4(plan, a, once, stream);
+  else if (cache.head_dim <= 64) of_dim(std::integral_constant<int, 64>{});
   else if (cache.head_dim <= 128) of_dim(std::integral_constant<int, 128>{});
   else of_dim(std::integral_constant<int, 256>{});
   if (!plan.solo) {
     // fewer (request, key head)s than runs: many parts each, over more threads; else two or three, one for most runs
     const int together = ATT_WAVES / plan.ways, values = together * std::min(a.rows, a.group) * (a.dim / 4);
     const int threads = plan.by_item ? ATT_JOIN : 256, many = plan.by_item ? 64 : 256;
-    hipLaunchKernelGGL(paged_attention_join_kernel, dim3(plan.by_item ? (unsigned)plan.items : (unsigned)plan.groups, (values + many - 1) / many),
+    hipLaunchKernelGGL(ruled ? scored_attention_join_kernel : paged_attention_join_kernel, dim3(plan.by_item ? (unsigned)plan.items : (unsigned)plan.groups, (values + many - 1) / many),
                        dim3(threads), 0, stream, a, together, many);
   }
   return hipGetLastError();

@@ -157,7 +157,7 @@ hipError_t launch_block_tables(const int32_t *held, const int32_t *lengths, int6
 
 // ---- new keys and values -----------------------------------------------------------------------
 // A copy with a place to look up, and to MXFP8 a rounding: HBM-bound, 4 bytes a value to bf16, 3 1/32 to MXFP8.  A lane moves 16
-// consecutive values of a token's head (8 to bf16), so it stores 16 bytes and two lanes have a block of MXFP8; the values and slots of
+// consecutive values of a token's head (8 to bf16), so it stores 16 bytes (8 to MXFP4) and two lanes have a block; the values and slots of
 // APPEND_PASSES tokens are on their way together.  (A block's elements and scale are three stores in no order with other workgroups', so a
 // slot named twice is left to no one's values.)  Measured: [8192 tokens, 8, 128] to MXFP8 10.8 us (4.7 TB/s), to bf16 11.7 (5.7).
 struct AppendArgs {
@@ -209,6 +209,7 @@ __global__ void __launch_bounds__(256) cache_append_kernel(AppendArgs a) {
         if constexpr (FMT == FMT_BF16) {
           *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(to) + where) = v[i][0];
         } else {
+          constexpr bool FOUR = FMT == FMT_MXFP4;
           float f[2][8];
           uint32_t amax = 0;
 #pragma unroll
@@ -221,9 +222,18 @@ __global__ void __launch_bounds__(256) cache_append_kernel(AppendArgs a) {
             amax = max(amax, __float_as_uint(amax8_nan(f[c])));
           }
           amax = max(amax, (uint32_t)__builtin_amdgcn_mov_dpp((int)amax, 0xB1, 0xF, 0xF, true));
-          const uint32_t byte = mxfp8_scale_from_amax(__uint_as_float(amax));
-          const uint2 lo = pack8_e4m3(f[0], byte), hi = pack8_e4m3(f[1], byte);
-          *reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(to) + where) = u32x4{lo.x, lo.y, hi.x, hi.y};
+          uint32_t byte;
+          if constexpr (FOUR) {
+            // (a block that is not finite: codes 0 under the scale that makes them NaN)
+            byte = amax >= 0x7F800000u ? 0xFFu : e8m0_from_amax(__uint_as_float(amax));
+            const float scale = e8m0_to_f32(byte);
+            const uint2 codes = make_uint2(pack8_e2m1(f[0], scale), pack8_e2m1(f[1], scale));
+            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(to) + (where >> 1)) = byte == 0xFFu ? make_uint2(0, 0) : codes;
+          } else {
+            byte = mxfp8_scale_from_amax(__uint_as_float(amax));
+            const uint2 lo = pack8_e4m3(f[0], byte), hi = pack8_e4m3(f[1], byte);
+            *reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(to) + where) = u32x4{lo.x, lo.y, hi.x, hi.y};
+          }
           if ((piece & 1) == 0) (is_value ? a.cache.v_scales : a.cache.k_scales)[where >> 5] = (uint8_t)byte;
         }
       }
@@ -241,7 +251,7 @@ hipError_t launch_cache_append(const torq_kv_cache_t &cache, const void *key, in
   const int64_t at_a_time = (int64_t)abreast * APPEND_PASSES;
   int64_t groups = (tokens + at_a_time - 1) / at_a_time;
   if (groups > 256 * 64) groups = 256 * 64;
-  auto kernel = cache.format == FMT_BF16 ? cache_append_kernel<FMT_BF16> : cache_append_kernel<FMT_MXFP8>;
+  auto kernel = cache.format == FMT_BF16 ? cache_append_kernel<FMT_BF16> : cache.format == FMT_MXFP8 ? cache_append_kernel<FMT_MXFP8> : cache_append_kernel<FMT_MXFP4>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, stream, a);
   return hipGetLastError();
 }

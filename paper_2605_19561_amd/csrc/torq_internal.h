@@ -194,11 +194,20 @@ hipError_t launch_cache_append(const torq_kv_cache_t &cache, const void *key, in
                                const void *value, int64_t value_token_stride, int64_t value_head_stride,
                                const int64_t *slots, int64_t tokens, hipStream_t stream);
 
-// Attention of one new token over a paged cache (paged_attention.hip).
+// Attention of one new token over a paged cache (paged_attention.hip), or, with `starts`, of up to `most` of each request, as rows of one
+// product: sizes then those of heads * most query heads.
 size_t paged_attention_workspace_bytes(const torq_kv_cache_t &cache, int heads, int64_t B, int width);
 hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, int64_t q_stride, int64_t q_head_stride, int heads,
                                   const int32_t *block_tables, int64_t table_stride, int width, const int32_t *lengths,
-                                  int64_t B, float scale, void *out, void *workspace, hipStream_t stream);
+                                  int64_t B, float scale, void *out, void *workspace, const torq_scores_t *scores,
+                                  const int32_t *starts, int most, int64_t tokens, hipStream_t stream);
+
+// Attention of many new tokens over a paged cache (chunk_attention.hip).
+size_t chunk_attention_workspace_bytes(const torq_kv_cache_t &cache, int heads, int64_t tokens, int most, int64_t B, int width);
+hipError_t launch_chunk_attention(const torq_kv_cache_t &cache, const void *q, int64_t q_stride, int64_t q_head_stride, int heads, int64_t tokens,
+                                  const int32_t *starts, int most, const int32_t *block_tables, int64_t table_stride, int width,
+                                  const int32_t *lengths, int64_t B, float scale, const torq_scores_t *scores, void *out, void *workspace,
+                                  hipStream_t stream);
 
 // Residual addition and RMS norm (rms_norm.hip).
 hipError_t launch_add_rms_norm(const void *x, const void *residual, const void *weight, int64_t M, int d, float eps,
