@@ -15,8 +15,8 @@ HOST_LIB = os.path.join(HERE, "_host" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.hip", "quantize.hip", "rotate_quant.hip", "rotate_butterfly.hip", "mxfp4_gemm.hip", "mxfp4_gemm_ring.hip",
            "mxfp4_gemm_skinny.hip", "mxfp4_gemm_stream.hip", "block_gram.hip", "code_histogram.hip",
            "intra_calib.hip", "rms_norm.hip", "paged_cache.hip", "paged_attention.hip", "paged_attention_mxfp4.hip",
-           "paged_attention_scores_bf16.hip", "paged_attention_scores_mxfp8.hip", "paged_attention_scores_mxfp4.hip", "chunk_attention.hip", "chunk_attention_256.hip",
-           "diag.hip"]
+           "paged_attention_scores_bf16.hip", "paged_attention_scores_mxfp8.hip", "paged_attention_scores_mxfp4.hip", "chunk_attention.hip", "chunk_attention_64.hip",
+           "chunk_attention_96.hip", "chunk_attention_128.hip", "chunk_attention_192.hip", "chunk_attention_256.hip", "diag.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
          # packed fp32 arithmetic is kept off for all device code
@@ -32,8 +32,9 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
 EXTRA = {"rotate_quant.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
          "mxfp4_gemm_ring.hip": ["-Wno-inline-asm"],
          **{name + ".hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for name in
-            ("paged_attention", "paged_attention_mxfp4", "paged_attention_scores_bf16", "paged_attention_scores_mxfp8", "paged_attention_scores_mxfp4",
-             "chunk_attention")},
+            ("paged_attention", "paged_attention_mxfp4", "paged_attention_scores_bf16", "paged_attention_scores_mxfp8", "paged_attention_scores_mxfp4")},
+         **{"chunk_attention_%d.hip" % n: ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"] for n in (64, 96, 128)},
+         **{"chunk_attention_%d.hip" % n: ["-Wno-inline-asm"] for n in (192, 256)},
          "rotate_butterfly.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "mxfp4_gemm_skinny.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
          "mxfp4_gemm_stream.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"]}

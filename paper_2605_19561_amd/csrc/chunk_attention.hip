@@ -14,24 +14,24 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a) {
   if (!row_tile_of(a, slot, b, row_tile)) return;
   const int2 there = rows_of_request(a, a.rule.starts[b], a.rule.starts[b + 1]);
   const int rows = min(there.y - there.x, a.rule.most) * a.rule.heads_each, quads = a.dim / 4;
-  const int64_t part0 = ((int64_t)slot * a.kv_heads + kv_head) * a.splits * CHUNK_ROWS;
-  for (int x = blockIdx.y * 256 + threadIdx.x; x < CHUNK_ROWS * quads; x += gridDim.y * 256) {
+  const int64_t part0 = ((int64_t)slot * a.kv_heads + kv_head) * a.splits * a.tile_rows;
+  for (int x = blockIdx.y * 256 + threadIdx.x; x < a.tile_rows * quads; x += gridDim.y * 256) {
     const int r = x / quads, c = x - r * quads;
-    if (row_tile * CHUNK_ROWS + r >= rows) break;
+    if (row_tile * a.tile_rows + r >= rows) break;
     float top = -INFINITY;
-    for (int i = 0; i < a.splits; ++i) top = fmaxf(top, a.part_ml[2 * (part0 + (int64_t)i * CHUNK_ROWS + r)]);
+    for (int i = 0; i < a.splits; ++i) top = fmaxf(top, a.part_ml[2 * (part0 + (int64_t)i * a.tile_rows + r)]);
     const float base = top == -INFINITY ? 0.0f : top;
     float l = 0.0f;
     f32x4 v = {0, 0, 0, 0};
 #pragma unroll 4
     for (int i = 0; i < a.splits; ++i) {
-      const int64_t part = part0 + (int64_t)i * CHUNK_ROWS + r;
+      const int64_t part = part0 + (int64_t)i * a.tile_rows + r;
       const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * part] - base);
       l += f * a.part_ml[2 * part + 1];
       v += f * *reinterpret_cast<const f32x4 *>(a.part + part * a.dim + 4 * c);
     }
     v *= l != 0.0f ? 1.0f / l : 0.0f;
-    uint16_t *const out = a.out + ruled_row(a, there.x, kv_head, row_tile * CHUNK_ROWS + r) * a.dim;
+    uint16_t *const out = a.out + ruled_row(a, there.x, kv_head, row_tile * a.tile_rows + r) * a.dim;
     *reinterpret_cast<bf16x4 *>(out + 4 * c) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
   }
 }
@@ -41,15 +41,18 @@ namespace {
 bool few_rows(const torq_kv_cache_t &cache, int heads, int most) { return (int64_t)(heads / cache.heads) * most <= 32; }
 struct ChunkPlan {
   int64_t slots, items;
-  int splits;
+  int splits, rows;
+  bool tall;
 };
 ChunkPlan chunk_plan(const torq_kv_cache_t &cache, int heads, int64_t tokens, int most, int64_t B, int width) {
   ChunkPlan p;
   const int64_t each = heads / cache.heads;
-  p.slots = std::min(tokens * each / CHUNK_ROWS + std::min(B, tokens), B * ((most * each + CHUNK_ROWS - 1) / CHUNK_ROWS));
+  p.tall = most * each > 64 || cache.head_dim > 128;
+  p.rows = p.tall ? 128 : 64;
+  p.slots = std::min(tokens * each / p.rows + std::min(B, tokens), B * ((most * each + p.rows - 1) / p.rows));
   p.items = p.slots * cache.heads;
-  const int64_t tiles = ((int64_t)width * cache.page_size + CHUNK_KEYS - 1) / CHUNK_KEYS, full = cache.head_dim <= 128 ? 512 : 256;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(full + p.items - 1) / std::max<int64_t>(p.items, 1), tiles / 4, 64}));
+  const int64_t steps = ((int64_t)width * cache.page_size + CHUNK_STEP - 1) / CHUNK_STEP, full = cache.head_dim <= 128 ? 512 : 256;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(full + p.items - 1) / std::max<int64_t>(p.items, 1), steps / 8, 64}));
   return p;
 }
 }  // namespace
@@ -57,7 +60,7 @@ ChunkPlan chunk_plan(const torq_kv_cache_t &cache, int heads, int64_t tokens, in
 size_t chunk_attention_workspace_bytes(const torq_kv_cache_t &cache, int heads, int64_t tokens, int most, int64_t B, int width) {
   if (few_rows(cache, heads, most)) return paged_attention_workspace_bytes(cache, heads * most, B, width);
   const ChunkPlan p = chunk_plan(cache, heads, tokens, most, B, width);
-  return p.splits == 1 ? 0 : (size_t)p.items * p.splits * CHUNK_ROWS * (cache.head_dim + 2) * sizeof(float);
+  return p.splits == 1 ? 0 : (size_t)p.items * p.splits * p.rows * (cache.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_chunk_attention(const torq_kv_cache_t &cache, const void *q, int64_t q_stride, int64_t q_head_stride, int heads, int64_t tokens,
@@ -71,14 +74,16 @@ hipError_t launch_chunk_attention(const torq_kv_cache_t &cache, const void *q, i
   ChunkArgs a;
   static_cast<AttentionArgs &>(a) = attention_args(cache, q, q_stride, q_head_stride, heads, block_tables, table_stride, width, lengths, B, scale,
                                                    out, scores, starts, most, tokens);
-  a.part = (float *)workspace, a.part_ml = a.part + plan.items * plan.splits * CHUNK_ROWS * cache.head_dim;
+  a.part = (float *)workspace, a.part_ml = a.part + plan.items * plan.splits * plan.rows * cache.head_dim;
   a.c = std::fabs(a.scale_log2), a.flip = a.scale_log2 < 0.0f;
-  a.slots = (int)plan.slots, a.splits = plan.splits;
+  a.slots = (int)plan.slots, a.splits = plan.splits, a.tile_rows = plan.rows;
   const bool bent = a.rule.cap_out > 0.0f || a.rule.slopes || a.c < FLT_MIN;
   const unsigned groups = (unsigned)(plan.items * plan.splits);
-  if (cache.head_dim <= 64) go_chunk<64>(a, cache.format, bent, groups, stream);
-  else if (cache.head_dim <= 128) go_chunk<128>(a, cache.format, bent, groups, stream);
-  else go_chunk_256(a, cache.format, bent, groups, stream);
+  (cache.head_dim <= 64    ? go_chunk_64
+   : cache.head_dim <= 96  ? go_chunk_96
+   : cache.head_dim <= 128 ? go_chunk_128
+   : cache.head_dim <= 192 ? go_chunk_192
+                           : go_chunk_256)(a, cache.format, bent, plan.tall, groups, stream);
   if (plan.splits > 1)
     hipLaunchKernelGGL(chunk_join_kernel, dim3((unsigned)plan.items, 8), dim3(256), 0, stream, a);
   return hipGetLastError();

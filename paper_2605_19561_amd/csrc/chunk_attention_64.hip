@@ -1,0 +1,10 @@
+// torq_chunk_attention for head_dim up to 64.
+#include "chunk_attention_body.h"
+
+namespace torq {
+
+void go_chunk_64(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream) {
+  go_chunk<64, 64>(a, format, bent, tall, groups, stream);
+}
+
+}  // namespace torq

@@ -1,0 +1,10 @@
+// torq_chunk_attention for head_dim up to 96.
+#include "chunk_attention_body.h"
+
+namespace torq {
+
+void go_chunk_96(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream) {
+  go_chunk<128, 96>(a, format, bent, tall, groups, stream);
+}
+
+}  // namespace torq

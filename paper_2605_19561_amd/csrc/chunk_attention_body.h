@@ -24,21 +24,25 @@
 
 namespace torq {
 
-constexpr int CHUNK_ROWS = 128, CHUNK_KEYS = 64, CHUNK_WAVE_ROWS = 32;
+constexpr int CHUNK_STEP = 32;         // keys of a step
 
 struct ChunkArgs : AttentionArgs {
   float c;                             // what scores are times in the exponent of 2
   int flip;                            // q's signs (a scale below 0)
+  int tile_rows;                       // rows of a workgroup
   int slots, splits;                   // row tiles of a key head at most; parts of the keys of one
 };
 
-// 16-byte pieces of a row of LDS are permuted by the row, so that what lanes read at a time lies in different banks: K, a piece of 32 rows (DP / 8
-// pieces each); V, eight pieces (128 bytes) of four rows
+// Where 16-byte pieces of keys lie in LDS, so that what lanes read at a time lies in different banks.  K, a piece of 16 rows: groups of 1024 bytes (what a
+// wave's load brings) with room between them, the pieces within a group permuted by the row.  V, eight pieces (128 bytes) of four rows: permuted by the row.
 template <int DP>
-__device__ __forceinline__ int k_place(int key, int piece) {
-  const int by = DP == 64 ? key >> 1 & 7 : key & 15;
-  return key * DP * 2 + (piece ^ by) * 16;
-}
+struct KLayout {
+  static constexpr int GROUP_ROWS = 512 / DP, PERMUTED = DP == 256 ? 2 : 4, GROUP = 1024 + 16 * PERMUTED, BYTES = CHUNK_STEP / GROUP_ROWS * GROUP;
+  static __device__ __forceinline__ int by(int key) { return DP == 64 ? key >> 1 & 3 : key & (PERMUTED - 1); }
+  static __device__ __forceinline__ int at(int key, int piece) {
+    return key / GROUP_ROWS * GROUP + key % GROUP_ROWS * DP * 2 + (piece ^ by(key)) * 16;
+  }
+};
 template <int DP>
 __device__ __forceinline__ int v_place(int key, int piece) {
   const int by = DP == 64 ? (key >> 1 & 1) << 2 : (key & 3) << 2;
@@ -51,7 +55,7 @@ __device__ __forceinline__ bool row_tile_of(const ChunkArgs &a, int slot, int &b
   auto tiles_of = [&](int i) {
     if (i >= a.B) return 0;
     const int2 rows = rows_of_request(a, a.rule.starts[i], a.rule.starts[i + 1]);
-    return (int)(((int64_t)min(rows.y - rows.x, a.rule.most) * a.rule.heads_each + CHUNK_ROWS - 1) / CHUNK_ROWS);
+    return (int)(((int64_t)min(rows.y - rows.x, a.rule.most) * a.rule.heads_each + a.tile_rows - 1) / a.tile_rows);
   };
   int before = 0, found = -1, at_it = 0, there = 0;
   for (int b0 = 0; b0 < a.B && found < 0; b0 += 512) {          // a lane adds up eight requests
@@ -76,20 +80,28 @@ __device__ __forceinline__ bool row_tile_of(const ChunkArgs &a, int slot, int &b
   return b >= 0;
 }
 
-template <int DP, int FMT, bool BENT>
-__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) chunk_attention_kernel(ChunkArgs a) {
+// DP: values of a row in LDS, of which the first DV are multiplied.  RW: waves that share keys, each with 32 rows of its own; the other 4 / RW - 1 such
+// groups have the same rows and other keys.
+template <int DP, int DV, int FMT, bool BENT, int RW>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 256 || DP * (4 / RW) > 128 ? 1 : 2, DP == 256 || DP * (4 / RW) > 128 ? 1 : 2))) chunk_attention_kernel(ChunkArgs a) {
   constexpr bool SCALED = FMT != FMT_BF16;
   constexpr int BITS = FMT == FMT_BF16 ? 16 : FMT == FMT_MXFP8 ? 8 : 4;
-  constexpr int W = DP * BITS / 32 < 16 ? DP * BITS / 32 : 16;  // bytes of a lane's load
+  constexpr int KP = 4 / RW, WK = CHUNK_STEP / RW;              // groups of waves with keys of their own; keys that a wave brings
+  constexpr bool DIRECT = FMT == FMT_BF16;                      // from memory straight into LDS
+  constexpr int LANE = WK * DP * BITS / 512;                    // bytes of a lane's loads of them
+  constexpr int WIDE = DP * BITS / 32 < 16 ? DP * BITS / 32 : 16, W = LANE < WIDE ? LANE : WIDE, L = LANE / W;   // (a load's keys lie in one page)
   constexpr int PER = DP * BITS / 8 / W;                        // lanes of a key
-  constexpr int L = 16 * PER / 64;                              // loads of a lane for 16 keys
   constexpr int VALUES = W * 8 / BITS;                          // of a load
-  constexpr int SCALE_OF = 4 * BITS, KS = DP / 16, IB = DP / 32;
-  constexpr int SIDE = CHUNK_KEYS * DP * 2;                     // bytes of a tile's K
-  __shared__ __attribute__((aligned(1024))) char lds[2][2][SIDE];
-  // of the keys that a wave has brought: 1 a value of V that is not finite (looked for where not every row sees all keys), 2 they have no page
-  __shared__ __attribute__((aligned(16))) int odd[2][4];
+  constexpr int SCALE_OF = 4 * BITS, KS = DV / 16, IB = DV / 32, SIDE = CHUNK_STEP * DP * 2;
+  typedef KLayout<DP> K;
+  constexpr int SETS = 2;                                       // steps whose loads are on their way in registers
+  static_assert(W >= 4 && 64 % PER == 0 && (64 / PER <= 16) && WK <= 16);
+  constexpr int SLOTS = 4, ROWS = 32 * RW, PITCH = 9, RING = KP * SLOTS * (K::BYTES + SIDE), JOIN = KP * ROWS * (PITCH * 16 + 8);
+  __shared__ __attribute__((aligned(1024))) char lds[RING > JOIN ? RING : JOIN];     // [keys' group][K, V][step by turns]; then what is put together
+  __shared__ int strange;                                       // a value that is not finite has been left out
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+  const int rp = wave % RW, kp = wave / RW;
+  char *const ring_k = lds + kp * SLOTS * (K::BYTES + SIDE), *const ring_v = ring_k + SLOTS * K::BYTES;
   const uniform_ints lengths = (uniform_ints)(uintptr_t)a.lengths, starts = (uniform_ints)(uintptr_t)a.rule.starts;
   auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
 
@@ -102,21 +114,26 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) chunk_attention_kernel
   const int q_at = uniform(rows_there.x), fresh = uniform(min(rows_there.y - rows_there.x, a.rule.most)), each = a.rule.heads_each;
   const int length = uniform(length_of(a, lengths[b])), first = uniform(lengths[b] - (rows_there.y - rows_there.x));
   const int prefix = uniform(a.rule.prefix ? min(max(((uniform_ints)(uintptr_t)a.rule.prefix)[b], 0), length) : 0);
-  const int window = a.rule.window, rows = fresh * each, row0 = row_tile * CHUNK_ROWS;
+  const int window = a.rule.window, rows = fresh * each, row0 = row_tile * a.tile_rows;
   auto low_of = [&](int p) { return window && p >= window ? p - window + 1 : 0; };
   auto position_of = [&](int row) { return first + min(row, rows - 1) / each; };
-  // tiles of keys: those of the prefix, then those from the first to the last that some row sees, `skip` of them left out between
-  const int last_key = min(position_of(row0 + CHUNK_ROWS - 1) + 1, length);
-  const int prefix_tiles = (prefix + CHUNK_KEYS - 1) / CHUNK_KEYS, all = max((last_key + CHUNK_KEYS - 1) / CHUNK_KEYS, prefix_tiles);
-  const int skip = max(min(low_of(position_of(row0)) / CHUNK_KEYS, all) - prefix_tiles, 0), tiles = all - skip;
-  const int begin = (int)((int64_t)tiles * split / a.splits), end = (int)((int64_t)tiles * (split + 1) / a.splits);
-  auto key_of = [&](int tile) { return (tile < prefix_tiles ? tile : tile + skip) * CHUNK_KEYS; };
+  // steps over the keys: those of the prefix, then those from the first to the last that some row sees, `skip` of them left out between
+  const int wg_first = uniform(position_of(row0)), wg_last = uniform(position_of(row0 + a.tile_rows - 1));
+  const int prefix_steps = (prefix + CHUNK_STEP - 1) / CHUNK_STEP;
+  const int all = max((max(min(wg_last + 1, length), 0) + CHUNK_STEP - 1) / CHUNK_STEP, prefix_steps);
+  const int skip = max(min(low_of(wg_first) / CHUNK_STEP, all) - prefix_steps, 0), steps = all - skip;
+  const int begin = (int)((int64_t)steps * split / a.splits), end = (int)((int64_t)steps * (split + 1) / a.splits);
+  // this wave's: every KP-th, the same number for all of them
+  const int count = (end - begin + KP - 1) / KP;
+  auto key_of = [&](int j) {                        // the first key of the wave's step j; past the end: the length
+    const int step = begin + j * KP + kp;
+    return step >= end ? length : (step < prefix_steps ? step : step + skip) * CHUNK_STEP;
+  };
 
-  // this wave's rows, this lane's
-  const int wave_row = row0 + wave * CHUNK_WAVE_ROWS, row = wave_row + n, token = row / each, head = kv_head * each + row - token * each;
-  const bool wave_in = wave_row < rows, in = row < rows;
-  const int p_first = uniform(position_of(wave_row)), p_last = uniform(position_of(wave_row + CHUNK_WAVE_ROWS - 1));
-  const int position = first + token, low = low_of(position);
+  // this lane's row
+  const int row = row0 + rp * 32 + n, token = row / each, head = kv_head * each + row - token * each;
+  const bool wave_in = row0 + rp * 32 < rows, in = row < rows;
+  const int position = first + token, low = low_of(position), span = max(min(position + 1, length) - low, 0);    // its window's keys: span from low on
   const float slope = BENT && a.rule.slopes && in ? 1.44269504088896340736f * a.rule.slopes[head] : 0.0f;
   bf16x8 q[KS];
 #pragma unroll
@@ -128,252 +145,440 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) chunk_attention_kernel
     q[s] = as_bf16(v);
   }
 
-  // a tile's 16 keys of this wave: on their way, and into LDS
-  const int load_key = lane / PER, load_at = lane % PER;
-  const uniform_ints table = (uniform_ints)(uintptr_t)(a.tables + b * a.table_stride);
-  auto page_of = [&](int tile) {
-    const int t16 = max(min(key_of(tile) / 16 + wave, (length - 1) / 16), 0), entry = (int)((uint64_t)(uint32_t)t16 * (uint64_t)a.page16_magic >> 38);
-    return make_int2(length > 0 ? table[entry] : -1, 16 * (t16 - entry * (a.page_size / 16)));
+  // Where the keys lie.  A lane looks up one of the 64 groups of 16 keys of 32 steps from w on, two windows ahead of their use: its page, then its place in
+  // bytes, and whether it has none.
+  const int *const table = a.tables + b * a.table_stride;
+  auto group_of = [&](int w) { return max(min(key_of(w + lane / 2) / 16 + (lane & 1), (length - 1) / 16), 0); };
+  auto entry_of = [&](int group) { return (int)((uint64_t)(uint32_t)group * (uint64_t)a.page16_magic >> 38); };
+  struct Window {
+    int low, high;
+    uint64_t lost;
   };
-  uint32_t k[L][W / 4], v[L][W / 4];
-  uint8_t k_scales[L], v_scales[L];
-  bool absent = false;
-  auto load = [&](int tile, int2 page) {
-    absent = (uint32_t)page.x >= (uint32_t)a.pages;
-    const int left = absent ? 0 : length - (key_of(tile) + 16 * wave), count = max(min(left, 16), 0);
-    const int64_t at = (left > 0 ? page.x : 0) * a.page_bytes + (kv_head * a.head_bytes + (int64_t)(page.y * a.token_bytes));
-    auto side = [&](const char *base, const uint8_t *base_scales, uint32_t (&x)[L][W / 4], uint8_t (&scales)[L]) {
-      const __amdgpu_buffer_rsrc_t r = records(base, at, count ? (count - 1) * a.token_bytes + a.dim * BITS / 8 : 0);
-      __amdgpu_buffer_rsrc_t rs;
-      if constexpr (SCALED) rs = records(base_scales, at / SCALE_OF, count ? (count - 1) * (a.token_bytes / SCALE_OF) + a.dim / 32 : 0);
-#pragma unroll
-      for (int j = 0; j < L; ++j) {
-        const int where = (load_key + 64 / PER * j) * a.token_bytes + load_at * W;
-        const bool there = load_at * VALUES < a.dim;
-        const auto y = buffer_load<W, false>(r, there ? where : ATT_FAR);
-#pragma unroll
-        for (int c = 0; c < W / 4; ++c) x[j][c] = y[c];
-        if constexpr (SCALED) scales[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, there ? where / SCALE_OF : ATT_FAR, 0, 0);
-      }
-    };
-    side(a.k, a.k_scales, k, k_scales);
-    side(a.v, a.v_scales, v, v_scales);
+  auto window_of = [&](int w, int page) {
+    const int group = group_of(w), entry = entry_of(group);
+    const bool gone = (uint32_t)page >= (uint32_t)a.pages;
+    const int64_t at = (gone ? 0 : page) * a.page_bytes + (kv_head * a.head_bytes + (int64_t)(16 * (group - entry * (a.page_size / 16)) * a.token_bytes));
+    return Window{(int)at, (int)(at >> 32), __ballot(gone)};
   };
-  auto widened = [&](const uint32_t (&x)[L][W / 4], const uint8_t (&scales)[L], int j, int piece) {      // 8 values
-    const float scale = SCALED ? __uint_as_float((uint32_t)scales[j] << 23) : 0.0f;
-    if constexpr (FMT == FMT_BF16) return u32x4{x[j][0], x[j][1], x[j][2], x[j][3]};
-    else if constexpr (FMT == FMT_MXFP4) return widen8(x[j][piece], scale);
-    else {
-      u32x4 y;
-      uint32_t w[4];
-      widen4(x[j][2 * piece], scale, w[0], w[1]);
-      widen4(x[j][2 * piece + 1], scale, w[2], w[3]);
-      y = u32x4{w[0], w[1], w[2], w[3]};
-      return y;
+  // The wave's steps whose keys every row of the workgroup sees, if they have pages: those before sure_steps, and sure_count from sure_first on.
+  int sure_steps = 0, sure_first = 0, sure_count = 0;
+  {
+    auto first_from = [&](int step) { return max((step - begin - kp + KP - 1) / KP, 0); };            // its first step that is `step` or later
+    const int sure_from = low_of(wg_last), sure_to = min(wg_first, length - 1) - (CHUNK_STEP - 1);      // first keys of steps without a prefix
+    sure_steps = first_from(min(prefix / CHUNK_STEP, end));
+    if (sure_to >= sure_from) {
+      const int from = max((sure_from + CHUNK_STEP - 1) / CHUNK_STEP, skip ? prefix_steps + skip : 0) - skip, to = sure_to / CHUNK_STEP - skip + 1;
+      sure_first = first_from(from), sure_count = max(first_from(min(to, end)) - sure_first, 0);
+    }
+  }
+  auto edge_at = [&](int j, int lost) { return lost || !(j < sure_steps || (uint32_t)(j - sure_first) < (uint32_t)sure_count); };
+  auto base_of = [&](const void *base, int64_t at) {
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(reinterpret_cast<uint64_t>(base) + at), 0, 16 * a.token_bytes, 0x00020000);
+  };
+  // (loads of keys behind the length stay within their pages; their scores are masked, and what of their values is not finite is left out)
+  const int load_at = lane % PER, load_key = lane / PER + rp * WK, where = (load_key & 15) * a.token_bytes + load_at * W;
+  const bool load_in = load_at * VALUES < a.dim;
+  uint32_t k[SETS][L][W / 4], v[SETS][L][W / 4];
+  uint8_t k_scales[SETS][L], v_scales[SETS][L];
+  auto load = [&](const char *base, const uint8_t *base_scales, int64_t at, uint32_t (&x)[L][W / 4], uint8_t (&scales)[L]) {
+    const __amdgpu_buffer_rsrc_t r = base_of(base, at);
+    __amdgpu_buffer_rsrc_t rs;
+    if constexpr (SCALED) rs = base_of(base_scales, at / SCALE_OF);
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const int from = where + 64 / PER * i * a.token_bytes;
+      const auto y = buffer_load<W, false>(r, load_in ? from : ATT_FAR);
+      if constexpr (W == 4) x[i][0] = y;
+      else
+#pragma unroll
+        for (int c = 0; c < W / 4; ++c) x[i][c] = y[c];
+      if constexpr (SCALED) scales[i] = __builtin_amdgcn_raw_buffer_load_b8(rs, load_in ? from / SCALE_OF : ATT_FAR, 0, 0);
     }
   };
-  // whether every row of the workgroup sees all keys of a tile, or of this wave
-  const int wg_first = uniform(position_of(row0)), wg_last = uniform(position_of(row0 + CHUNK_ROWS - 1));
-  auto all_seen = [&](int key0, int from, int to) {
-    return key0 + CHUNK_KEYS <= length && (key0 + CHUNK_KEYS <= prefix || (key0 + CHUNK_KEYS - 1 <= from && key0 >= low_of(to)));
-  };
-  auto put = [&](int buffer, int tile) {
-    uint32_t bad = 0;
-    const bool edge = !all_seen(key_of(tile), wg_first, wg_last);
+  // straight into LDS: 64 pieces of 16 bytes in a row, so a lane brings the piece that lies at its place there
+  constexpr int PIECES_IN = DP / 8, DL = WK / K::GROUP_ROWS > 0 ? WK / K::GROUP_ROWS : 1;
+  int k_from[DL], v_from[DL];
+  if constexpr (DIRECT)
 #pragma unroll
-    for (int j = 0; j < L; ++j) {
-      const int key = 16 * wave + load_key + 64 / PER * j;
+    for (int i = 0; i < DL; ++i) {
+      const int key = rp * WK + lane / PIECES_IN + K::GROUP_ROWS * i, at = (key & 15) * a.token_bytes;
+      const int k_piece = lane % PIECES_IN ^ K::by(key), v_piece = (v_place<DP>(key, lane % PIECES_IN) - key * DP * 2) / 16;
+      k_from[i] = 8 * k_piece < a.dim ? at + 16 * k_piece : ATT_FAR, v_from[i] = 8 * v_piece < a.dim ? at + 16 * v_piece : ATT_FAR;
+    }
+  auto bring = [&](const char *base, int64_t at, char *to, int pitch, const int (&from)[DL]) {
+    const i32x4 r = raw_buffer(reinterpret_cast<const void *>(reinterpret_cast<uint64_t>(base) + at), 16 * a.token_bytes);
+    const uint32_t to_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)to + rp * DL * pitch;
+#pragma unroll
+    for (int i = 0; i < DL; ++i) load_to_lds16<false>(r, to_lds + i * pitch, from[i], 0);
+  };
+  auto widened = [&](const uint32_t (&x)[L][W / 4], const uint8_t (&scales)[L], int i, int piece) {      // 8 values
+    const float scale = SCALED ? __uint_as_float((uint32_t)scales[i] << 23) : 0.0f;
+    if constexpr (FMT == FMT_BF16) return u32x4{x[i][0], x[i][1], x[i][2], x[i][3]};
+    else if constexpr (FMT == FMT_MXFP4) return widen8(x[i][piece], scale);
+    else {
+      uint32_t w[4];
+      widen4(x[i][2 * piece], scale, w[0], w[1]);
+      widen4(x[i][2 * piece + 1], scale, w[2], w[3]);
+      return u32x4{w[0], w[1], w[2], w[3]};
+    }
+  };
+  auto put_k = [&](int turn, const uint32_t (&x)[L][W / 4], const uint8_t (&scales)[L]) {
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int piece = 0; piece < VALUES / 8; ++piece)
+        *reinterpret_cast<u32x4 *>(ring_k + turn * K::BYTES + K::at(load_key + 64 / PER * i, load_at * (VALUES / 8) + piece)) = widened(x, scales, i, piece);
+  };
+  // eight values of which what is not finite is left out: where not every row sees the key, 0 times that is no 0
+  auto finite = [&](u32x4 w) {
+    bool left_out = false;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t lo = (w[c] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u, hi = (w[c] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u;
+      left_out |= (lo | hi) != 0;
+      w[c] &= ~(lo | hi);
+    }
+    if (left_out) strange = 1;
+    return w;
+  };
+  auto put_v = [&](int turn, const uint32_t (&x)[L][W / 4], const uint8_t (&scales)[L], bool edge) {
+#pragma unroll
+    for (int i = 0; i < L; ++i)
 #pragma unroll
       for (int piece = 0; piece < VALUES / 8; ++piece) {
-        *reinterpret_cast<u32x4 *>(&lds[buffer][0][k_place<DP>(key, load_at * (VALUES / 8) + piece)]) = widened(k, k_scales, j, piece);
-        const u32x4 x = widened(v, v_scales, j, piece);
-        *reinterpret_cast<u32x4 *>(&lds[buffer][1][v_place<DP>(key, load_at * (VALUES / 8) + piece)]) = x;
-        if (edge)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) bad |= not_finite(x[c]);
+        u32x4 w = widened(x, scales, i, piece);
+        if (edge) w = finite(w);
+        *reinterpret_cast<u32x4 *>(ring_v + turn * SIDE + v_place<DP>(load_key + 64 / PER * i, load_at * (VALUES / 8) + piece)) = w;
       }
-    }
-    const bool any = __any(bad != 0);
-    if (lane == 0) odd[buffer][wave] = any + 2 * absent;
   };
 
   f32x16 o[IB];
+  float m = -INFINITY, l = 0.0f;                    // m in the exponent of 2
 #pragma unroll
   for (int i = 0; i < IB; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
   const float c = BENT ? 1.0f : a.c;
-  const int k_base = k_place<DP>(n, h);
+  // this lane's pieces of its key
+  int k_base[2] = {K::at(n, h), K::at(n, h + (DP < 256 ? 2 : 0))};
   // where this lane's part of four keys' values lies, those of i = 0 ... 31 of the keys 4 h ... 4 h + 3
+  constexpr int VB = DP == 64 ? 2 : 4;
   const int v_key = 4 * h + (lane & 15) / 4, v_piece = 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-  int v_base[DP == 64 ? 2 : 4];
+  int v_base[VB];
 #pragma unroll
-  for (int i = 0; i < (DP == 64 ? 2 : 4); ++i) v_base[i] = v_place<DP>(v_key, 4 * i + v_piece) + (lane & 1) * 8;
+  for (int i = 0; i < VB; ++i) v_base[i] = v_place<DP>(v_key, 4 * i + v_piece) + (lane & 1) * 8;
   typedef __attribute__((address_space(3))) i16x4 *lds_i16x4;
 
-  auto work = [&](int buffer, int key0) {
-    const i32x4 marks = *reinterpret_cast<const i32x4 *>(odd[buffer]);
-    const int mark = uniform(marks[0] | marks[1] | marks[2] | marks[3]);
-    const bool seen = mark < 2 && all_seen(key0, p_first, p_last);
-    if (!wave_in || (!seen && key0 >= prefix && (key0 > p_last || key0 >= length || key0 + CHUNK_KEYS <= low_of(p_first)))) return;
-    const char *const ks = lds[buffer][0], *const vs = lds[buffer][1];
-    f32x16 st[2];
+  // What a step computes: KS products for the scores of the next one's keys, 2 IB with the weights of the last one's, and this one's weights, in pieces.
+  auto k_operand = [&](int turn, int s) {
+    return as_bf16(*reinterpret_cast<const u32x4 *>(ring_k + k_base[DP < 256 ? s % 2 : 0] + (turn * K::BYTES + (DP < 256 ? s / 2 * 64 : s * 32))));
+  };
+  auto v_operand = [&](int turn, int i) {           // of the products with 16 keys of 32 values
+    const char *const at = ring_v + v_base[i % IB % VB] + (turn * SIDE + i % IB / VB * (VB * 64) + i / IB * 16 * DP * 2);
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + 8 * DP * 2));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto score = [&](f32x16 &st, bf16x8 x, int s) {
+    if (s == 0)
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+      for (int r = 0; r < 16; ++r) st[r] = 0.0f;
+    st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[s], st, 0, 0, 0);
+  };
+  auto product = [&](bf16x8 x, const u32x4 (&pt)[2], int i) {
+    o[i % IB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, as_bf16(pt[i / IB]), o[i % IB], 0, 0, 0);
+  };
+  constexpr int PIECES = 13;
+  float top = 0.0f, base = 0.0f, alpha = 1.0f;
+  bool moved = false;
+  auto piece = [&](auto at_edge, int i, int key0, int lost, f32x16 &st, u32x4 (&pt)[2]) {
+    constexpr bool EDGE = decltype(at_edge)::value;
+    const int from = key0 + 4 * h;
+    if (i < 4) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st[u][r] = 0.0f;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(ks + (k_base ^ 32 * s) + u * 32 * DP * 2);
-        st[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(x), q[s], st[u], 0, 0, 0);
+      for (int r = 4 * i; r < 4 * i + 4; ++r) {
+        const int t = 8 * (r / 4) + r % 4;
+        if constexpr (BENT) {
+          float x = st[r] * a.scale_log2;
+          if (a.rule.cap_out > 0.0f) x = capped(st[r], a.rule.cap_in, a.rule.cap_out);
+          if (a.rule.slopes) x -= slope * fabsf((float)(position - from) - (float)t);
+          st[r] = x;
+        }
+        if constexpr (EDGE) {
+          const bool seen = ((uint32_t)(from - low + t) < (uint32_t)span) | (from - prefix + t < 0);
+          st[r] = (seen & !(lost >> (r / 8) & 1)) ? st[r] : -INFINITY;
+        }
+        top = r ? fmaxf(top, st[r]) : st[r];
       }
-    }
-    auto key_at = [&](int u, int r) { return key0 + 32 * u + 8 * (r / 4) + 4 * h + r % 4; };
-    if constexpr (BENT) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float x = st[u][r] * a.scale_log2;
-          if (a.rule.cap_out > 0.0f) x = capped(st[u][r], a.rule.cap_in, a.rule.cap_out);
-          if (a.rule.slopes) x -= slope * fabsf((float)(position - key_at(u, r)));
-          st[u][r] = x;
-        }
-    }
-    if (!seen) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int t = key_at(u, r);
-          if (!(t < length && marks[2 * u + r / 8] < 2 && ((t <= position && t >= low) || t < prefix))) st[u][r] = -INFINITY;
-        }
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) top = fmaxf(top, st[u][r]);
-    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-    top = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
-    if (__any((top - m) * c > 8.0f)) {
-      const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.0f : m_new, alpha = __builtin_amdgcn_exp2f((m - base) * c);
-      m = m_new;
+    } else if (i == 4) {
+      const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1])) * c;
+      moved = top - m > 8.0f;
+      const float now = moved ? top : m;
+      alpha = moved ? __builtin_amdgcn_exp2f(m - now) : 1.0f;
+      m = now, base = now == -INFINITY ? 0.0f : now;
       l *= alpha;
-#pragma unroll
-      for (int i = 0; i < IB; ++i) o[i] *= alpha;
-    }
-    const float base = m == -INFINITY ? 0.0f : m * c;
-    u32x4 pt[4];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const bf16x2 pair = {(__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[u][r], c, -base)),
-                             (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[u][r + 1], c, -base))};
-        l = __builtin_amdgcn_fdot2_f32_bf16(pair, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l, false);
-        pt[2 * u + r / 8][r % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
-      }
-    // four keys of 32 i for each of two: keys 16 s + 4 h + 0 ... 3 and + 8
-    auto operand = [&](int s, int i) {
-      const int at = v_base[i % (DP == 64 ? 2 : 4)] + i / 4 * 256 + s * 16 * DP * 2;
-      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(vs + at)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(vs + at + 8 * DP * 2));
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    if (!seen && mark & 1) {
-      // 0 times what is not finite is no 0: a row at a time, with nothing in the place of the keys that it does not see
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int i = 0; i < IB; ++i) {
-          const auto there = operand(s, i);
-#pragma nounroll
-          for (int x = 0; x < CHUNK_WAVE_ROWS; ++x) {
-            const int its_position = __builtin_amdgcn_readlane(position, x), its_low = __builtin_amdgcn_readlane(low, x);
-            const u32x4 nothing = {0, 0, 0, 0}, p = n == x ? pt[s] : nothing;
-            auto w = there;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int t = key0 + 16 * s + 8 * (e / 4) + 4 * h + e % 4;
-              w[e] = t < length && ((t <= its_position && t >= its_low) || t < prefix) ? w[e] : (short)0;
-            }
-            f32x16 y;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) y[r] = 0.0f;
-            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), as_bf16(p), y, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[i][r] += n == x ? y[r] : 0.0f;
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        }
     } else {
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int i = 0; i < IB; ++i)
-          o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, operand(s, i)), as_bf16(pt[s]), o[i], 0, 0, 0);
+      const int r = 2 * (i - 5);
+      const bf16x2 pair = {(__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[r], c, -base)),
+                           (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[r + 1], c, -base))};
+      l = __builtin_amdgcn_fdot2_f32_bf16(pair, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l, false);
+      pt[r / 8][r % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
     }
   };
-
-  if (begin < end) {
-    int2 page = page_of(begin);
-    load(begin, page);
-    page = page_of(begin + 1);
-    put(0, begin);
+  // Step j: the scores of step j + 1, the weights of j and the products of j - 1, none of which needs another.  Meanwhile what later steps need is on its
+  // way into LDS, step x into slot x % SLOTS: straight from memory K of j + 3 and V of j + 2, or through registers K of j + 2 and V of j, with the loads for
+  // SETS steps later.
+  f32x16 st[2];
+  u32x4 pt[2][2];
+  if (tid == 0) strange = 0;
+  if (count > 0) {
+    constexpr int FAR = DIRECT ? 3 : 4;             // of the steps ahead, the one whose K sets out
+    int w = 0;
+    Window here = window_of(0, table[entry_of(group_of(0))]);
+    int next = table[entry_of(group_of(32))], lost_ahead = 0;
+    const int group = RW == 2 ? rp : rp / 2;        // of a step's two, the one that this wave brings keys of
+    auto place = [&](int x) -> int64_t {            // of step x, which is a step later each time
+      if (x == w + 32) {
+        w = x;
+        here = window_of(w, next);
+        next = table[entry_of(group_of(w + 32))];
+      }
+      const int i = 2 * (x - w);
+      lost_ahead = lost_ahead >> 2 | ((int)(here.lost >> i) & 3) << 2 * FAR;
+      return (int64_t)__builtin_amdgcn_readlane(here.high, i + group) << 32 | (uint32_t)__builtin_amdgcn_readlane(here.low, i + group);
+    };
+    int64_t before[2];                              // places of the last two steps whose K has set out, the last first
+    if constexpr (DIRECT) {
+#pragma unroll
+      for (int x = 0; x < 3; ++x) {
+        before[0] = place(x);
+        bring(a.k, before[0], ring_k + x * K::BYTES, K::GROUP, k_from);
+        if (x < 2) bring(a.v, before[0], ring_v + x * SIDE, 1024, v_from);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
+      const int64_t first_place = place(0), second_place = place(1);
+      load(a.k, a.k_scales, first_place, k[0], k_scales[0]);
+      load(a.k, a.k_scales, second_place, k[1], k_scales[1]);
+      load(a.v, a.v_scales, first_place, v[0], v_scales[0]);
+      load(a.v, a.v_scales, second_place, v[1], v_scales[1]);
+      put_k(0, k[0], k_scales[0]);
+      put_k(1, k[1], k_scales[1]);
+      before[1] = place(2), before[0] = place(3);
+      load(a.k, a.k_scales, before[1], k[0], k_scales[0]);
+      load(a.k, a.k_scales, before[0], k[1], k_scales[1]);
+    }
     __syncthreads();
-    int buffer = 0;
-    for (int tile = begin; tile < end; ++tile, buffer ^= 1) {
-      const bool more = tile + 1 < end;
-      if (more) {
-        load(tile + 1, page);
-        page = page_of(tile + 2);
+    static_for<KS>([&](auto s) {
+      if (s % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+      score(st[0], k_operand(0, s), s);
+    });
+    auto step = [&](auto with_products, auto parity, int j) {
+      constexpr int P = decltype(parity)::value;
+      const int64_t now = place(j + FAR);
+      const int lost = lost_ahead & 3;
+      const bool edge = edge_at(j, lost);
+      const int key0 = key_of(j);
+      if constexpr (DIRECT) {
+        bring(a.k, now, ring_k + (j + 3) % SLOTS * K::BYTES, K::GROUP, k_from);
+        bring(a.v, before[0], ring_v + (j + 2) % SLOTS * SIDE, 1024, v_from);
+        before[0] = now;
+        if (edge) {
+#pragma unroll
+          for (int i = 0; i < DL; ++i) {
+            u32x4 *const at = reinterpret_cast<u32x4 *>(ring_v + j % SLOTS * SIDE + (rp * DL + i) * 1024) + lane;
+            *at = finite(*at);
+          }
+        }
+      } else {
+        put_k((j + 2) % SLOTS, k[P], k_scales[P]);
+        put_v(j % SLOTS, v[P], v_scales[P], edge);
+        load(a.k, a.k_scales, now, k[P], k_scales[P]);
+        load(a.v, a.v_scales, before[1], v[P], v_scales[P]);
+        before[1] = before[0], before[0] = now;
       }
-      work(buffer, key_of(tile));
-      if (more) put(buffer ^ 1, tile + 1);
+      if (wave_in) {
+        constexpr int PRODUCTS = decltype(with_products)::value ? KS + 2 * IB : KS, AHEAD = 3;
+        auto operand = [&](int i) { return i < KS ? k_operand(P ^ 1, i) : v_operand(P ^ 1, i - KS); };
+        auto multiply = [&](bf16x8 x, int i) {
+          if (i < KS) score(st[P ^ 1], x, i);
+          else product(x, pt[P ^ 1], i - KS);
+        };
+        bf16x8 x[PRODUCTS];
+        if (edge) {                                 // (few steps: one after the other)
+          static_for<PIECES>([&](auto i) { piece(std::true_type{}, i, key0, lost, st[P], pt[P]); });
+          static_for<PRODUCTS>([&](auto i) {
+            if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);         // (two operands at a time, for the registers)
+            multiply(operand(i), i);
+          });
+        } else {
+          // a product, what a later one multiplies, a piece of the weights, and so on in this order
+          static_for<AHEAD>([&](auto i) { x[i] = operand(i); });
+          static_for<PRODUCTS>([&](auto i) {
+            constexpr int I = decltype(i)::value;
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(x[I], I);
+            if constexpr (I + AHEAD < PRODUCTS) x[I + AHEAD] = operand(I + AHEAD);
+            static_for<(I + 1) * PIECES / PRODUCTS - I * PIECES / PRODUCTS>(
+                [&](auto k) { piece(std::false_type{}, I * PIECES / PRODUCTS + decltype(k)::value, key0, lost, st[P], pt[P]); });
+          });
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (__any(moved))
+#pragma unroll
+          for (int i = 0; i < IB; ++i) o[i] *= alpha;
+      }
+      // (the loads of this step stay on their way)
+      if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * DL) : "memory");
       __syncthreads();
+    };
+    // (two steps of K from slot 2 on, of V from slot 0 on; then the other way round)
+    int k_move = 2 * K::BYTES, v_move = 2 * SIDE;
+    auto turn = [&](int (&base)[2], int &move) { base[0] += move, base[1] += move, move = -move; };
+    auto finish = [&](auto parity) {                // the products of the last step
+      constexpr int P = decltype(parity)::value;
+      static_for<2 * IB>([&](auto i) {
+        if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+        product(v_operand(P, i), pt[P], i);
+      });
+    };
+    step(std::false_type{}, std::integral_constant<int, 0>{}, 0);
+    turn(k_base, k_move);
+    int j = 1;
+    for (; j + 1 < count; j += 2) {
+      step(std::true_type{}, std::integral_constant<int, 1>{}, j);
+      step(std::true_type{}, std::integral_constant<int, 0>{}, j + 1);
+      turn(k_base, k_move);
+#pragma unroll
+      for (int i = 0; i < VB; ++i) v_base[i] += v_move;
+      v_move = -v_move;
+    }
+    if (j < count) {
+      step(std::true_type{}, std::integral_constant<int, 1>{}, j);
+      finish(std::integral_constant<int, 1>{});
+    } else {
+      finish(std::integral_constant<int, 0>{});
     }
   }
-  if (!wave_in) return;
-  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-  l = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
-  if (!in) return;
-  if (a.splits > 1) {
-    const int64_t part = (((int64_t)slot * a.kv_heads + kv_head) * a.splits + split) * CHUNK_ROWS + wave * CHUNK_WAVE_ROWS + n;
-    if (h == 0) a.part_ml[2 * part] = BENT || m == -INFINITY ? m : m * c, a.part_ml[2 * part + 1] = l;
+  __syncthreads();
+  if (strange) {
+    // What has been left out: an infinity or NaN for every row that sees its key, whatever the weight.
+#pragma nounroll
+    for (int j = 0; j < count; ++j) {
+      const int key0 = key_of(j);
+      if (key0 >= length) continue;
+      int page[2], in_page[2];
 #pragma unroll
-    for (int i = 0; i < IB; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const int at = 32 * i + 2 * r + 4 * h;
-        if (at < a.dim) *reinterpret_cast<f32x4 *>(a.part + part * a.dim + at) = f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
+      for (int u = 0; u < 2; ++u) {
+        const int group = min(key0 / 16 + u, (length - 1) / 16), entry = entry_of(group);
+        page[u] = uniform(table[entry]), in_page[u] = 16 * (group - entry * (a.page_size / 16));
       }
-    return;
-  }
-  const float inverse = l != 0.0f ? 1.0f / l : 0.0f;
-  uint16_t *const out = a.out + ruled_row(a, q_at, kv_head, row) * a.dim;
+      if (!edge_at(j, ((uint32_t)page[0] >= (uint32_t)a.pages) + 2 * ((uint32_t)page[1] >= (uint32_t)a.pages))) continue;
+#pragma nounroll
+      for (int x = 0; x < CHUNK_STEP; ++x) {
+        const int key = key0 + x, its_page = x < 16 ? page[0] : page[1], place = (x < 16 ? in_page[0] : in_page[1]) + x % 16;
+        if (key >= length || (uint32_t)its_page >= (uint32_t)a.pages) continue;
+        const int64_t at = its_page * a.page_bytes + (kv_head * a.head_bytes + (int64_t)(place * a.token_bytes));
 #pragma unroll
-  for (int i = 0; i < IB; ++i)
+        for (int i = 0; i < IB; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-      const int at = 32 * i + 2 * r + 4 * h;
-      if (at < a.dim)
-        *reinterpret_cast<bf16x4 *>(out + at) = bf16x4{(__bf16)(o[i][r] * inverse), (__bf16)(o[i][r + 1] * inverse),
-                                                       (__bf16)(o[i][r + 2] * inverse), (__bf16)(o[i][r + 3] * inverse)};
+          for (int r = 0; r < 16; r += 4) {
+            const int e = 32 * i + 2 * r + 4 * h;
+            if (e >= a.dim) continue;
+            uint32_t w[2];
+            if constexpr (FMT == FMT_BF16) {
+              w[0] = reinterpret_cast<const uint32_t *>(a.v + at)[e / 2], w[1] = reinterpret_cast<const uint32_t *>(a.v + at)[e / 2 + 1];
+            } else {
+              const float scale = __uint_as_float((uint32_t)a.v_scales[at / SCALE_OF + e / 32] << 23);
+              if constexpr (FMT == FMT_MXFP8) {
+                widen4(*reinterpret_cast<const uint32_t *>(a.v + at + e), scale, w[0], w[1]);
+              } else {
+                const u32x4 y = widen8(*reinterpret_cast<const uint16_t *>(a.v + at + e / 2), scale);
+                w[0] = y[0], w[1] = y[1];
+              }
+            }
+            const bool seen = (((uint32_t)(key - low) < (uint32_t)span) | (key < prefix)) & (m != -INFINITY);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const float y = bf16_bits_to_f32(w[q / 2] >> 16 * (q % 2) & 0xFFFFu);
+              if (seen && !(fabsf(y) < INFINITY)) o[i][r + q] += y;
+            }
+          }
+      }
     }
+  }
+  // (looked at anew from here on: what hangs on the row is not kept through the loop)
+  int late = lane;
+  asm volatile("" : "+v"(late));
+  const int n_late = late & 31, h_late = late >> 5;
+  {
+    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+  }
+  const int64_t part = (((int64_t)slot * a.kv_heads + kv_head) * a.splits + split) * a.tile_rows;
+  // four values of a row of the workgroup's
+  auto store = [&](int row, int i, f32x4 x, float top, float sum) {
+    if (row0 + row >= rows || i >= a.dim) return;
+    if (a.splits > 1) {
+      *reinterpret_cast<f32x4 *>(a.part + (part + row) * a.dim + i) = x;
+      if (i == 0) a.part_ml[2 * (part + row)] = top, a.part_ml[2 * (part + row) + 1] = sum;
+    } else {
+      x *= sum != 0.0f ? 1.0f / sum : 0.0f;
+      *reinterpret_cast<bf16x4 *>(a.out + ruled_row(a, q_at, kv_head, row0 + row) * a.dim + i) = bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+    }
+  };
+  // the groups' put together, 32 values of every row at a time
+  f32x4 *const mine = reinterpret_cast<f32x4 *>(lds);
+  float *const ml = reinterpret_cast<float *>(mine + KP * ROWS * PITCH);
+  const int mine_at = kp * ROWS + rp * 32 + n_late;
+  if (h_late == 0) ml[2 * mine_at] = m, ml[2 * mine_at + 1] = l;
+#pragma unroll
+  for (int i = 0; i < IB; ++i) {
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) mine[mine_at * PITCH + r / 2 + h_late] = f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
+    __syncthreads();
+    for (int x = tid; x < ROWS * 8; x += 256) {
+      const int row = x / 8, piece = x % 8;
+      float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < KP; ++w) top = fmaxf(top, ml[2 * (w * ROWS + row)]);
+      const float base = top == -INFINITY ? 0.0f : top;
+      f32x4 y = {0, 0, 0, 0};
+#pragma unroll
+      for (int w = 0; w < KP; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ml[2 * (w * ROWS + row)] - base);
+        sum += f * ml[2 * (w * ROWS + row) + 1];
+        y += f * mine[(w * ROWS + row) * PITCH + piece];
+      }
+      store(row, 32 * i + 4 * piece, y, top, sum);
+    }
+    if (i + 1 < IB) __syncthreads();
+  }
 }
 
-template <int DP>
-void go_chunk(const ChunkArgs &a, int format, bool bent, unsigned groups, hipStream_t stream) {
+// Kernels of one width: 128 rows of a workgroup (tall) or 64.
+template <int DP, int DV>
+void go_chunk(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream) {
+  auto of_rows = [&](auto of, auto with, auto waves) {
+    hipLaunchKernelGGL((chunk_attention_kernel<DP, DV, decltype(of)::value, decltype(with)::value, decltype(waves)::value>), dim3(groups), dim3(256), 0, stream, a);
+  };
+  auto of_scores = [&](auto of, auto with) {
+    if constexpr (DP < 256)
+      if (!tall) return of_rows(of, with, std::integral_constant<int, 2>{});
+    of_rows(of, with, std::integral_constant<int, 4>{});
+  };
   auto of_format = [&](auto of) {
-    constexpr int FMT = decltype(of)::value;
-    if (bent) hipLaunchKernelGGL((chunk_attention_kernel<DP, FMT, true>), dim3(groups), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((chunk_attention_kernel<DP, FMT, false>), dim3(groups), dim3(256), 0, stream, a);
+    if (bent) of_scores(of, std::true_type{});
+    else of_scores(of, std::false_type{});
   };
   if (format == FMT_BF16) of_format(std::integral_constant<int, FMT_BF16>{});
   else if (format == FMT_MXFP8) of_format(std::integral_constant<int, FMT_MXFP8>{});
   else of_format(std::integral_constant<int, FMT_MXFP4>{});
 }
-void go_chunk_256(const ChunkArgs &a, int format, bool bent, unsigned groups, hipStream_t stream);      // chunk_attention_256.hip
+void go_chunk_64(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream);     // chunk_attention_64.hip, ...
+void go_chunk_96(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream);
+void go_chunk_128(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream);
+void go_chunk_192(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream);
+void go_chunk_256(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream);
 
 }  // namespace torq

@@ -66,7 +66,8 @@ def values4(codes, scales):
     codes = codes.cpu().contiguous().numpy()
     nibbles = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], -1)
     v = np.where(nibbles >= 8, -E2M1[nibbles & 7], E2M1[nibbles & 7])
-    s = 2.0 ** (scales.contiguous().view(torch.uint8).cpu().numpy().astype(np.float64) - 127)
+    byte = scales.contiguous().view(torch.uint8).cpu().numpy().astype(np.float64)
+    s = np.where(byte == 255, np.nan, 2.0 ** (byte - 127))
     return torch.from_numpy(v * np.repeat(s, 32, -1))
 
 
@@ -412,3 +413,52 @@ def test_chunk_attention(tq, heads, kv_heads, dim, page, fresh, lengths, fmt, la
         got = tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, tables.to(DEV), lens.to(DEV), dim ** -0.5, most=max(fresh), scores=rule.on(tq), out=out)
         assert got is out and bool((out[-3:] == 7.0).all())                             # rows of no request
         check(got, *want, few(heads, kv_heads, max(fresh)))
+
+
+POISONED = [
+    # heads, kv_heads, head_dim, page, new tokens, tokens, format
+    (8, 2, 64, 16, [1, 1, 1], [40, 200, 33], "bf16"), (16, 1, 128, 16, [1, 1], [90, 150], "mxfp8"), (4, 4, 256, 16, [1, 1], [90, 150], "mxfp4"),
+    (48, 2, 128, 16, [1, 1], [90, 150], "bf16"), (16, 2, 96, 32, [3, 1, 4], [90, 40, 4], "mxfp4"), (8, 8, 128, 16, [20, 9], [20, 100], "bf16"),
+    (8, 2, 128, 16, [70, 9, 130], [70, 100, 200], "bf16"), (8, 2, 128, 16, [70, 9, 130], [70, 100, 200], "mxfp8"), (8, 2, 96, 16, [40, 9], [70, 100], "mxfp4"),
+    (4, 1, 64, 48, [150], [300], "bf16"), (8, 4, 256, 16, [50, 60], [80, 60], "mxfp8"), (6, 2, 160, 16, [30, 12], [80, 60], "bf16")]
+
+
+@gpu
+@pytest.mark.parametrize("rule", ["plain", "window 1", "window 50", "prefix", "first and last", "everything"])
+@pytest.mark.parametrize("heads,kv_heads,dim,page,fresh,lengths,fmt", POISONED)
+def test_what_a_query_does_not_see_takes_no_part(tq, heads, kv_heads, dim, page, fresh, lengths, fmt, rule):
+    """Tokens whose keys and values are not finite: rows that see them are not finite where those are, the others are as without."""
+    B = len(lengths)
+    rule = RULES[rule](heads, B)
+    cache, q, starts, tables, lens, pages = case(tq, fresh, lengths, heads, kv_heads, dim, page, fmt, "heads", 5)
+    g = rng(lengths, fresh, 9)
+    for b, n in enumerate(lengths):                  # in some places of values, and in whole keys
+        for t in sorted({0, n // 3, n // 2, n - 2, n - 1}):
+            if t < 0:
+                continue
+            entry, place, what = int(tables[b, t // page]), t % page, int(torch.randint(0, 3, (1,), generator=g))
+            i = int(torch.randint(0, dim, (1,), generator=g))
+            if fmt == "bf16":
+                cache.v[entry, :, place, i] = (math.nan, math.inf, -math.inf)[what]
+                if what == 0:
+                    cache.k[entry, :, place, i] = math.nan
+            elif fmt == "mxfp8" and what:
+                cache.v.view(torch.uint8)[entry, :, place, i] = 0x7F
+            else:
+                cache.v_scales.view(torch.uint8)[entry, :, place, i // 32] = 0xFF
+                cache.k_scales.view(torch.uint8)[entry, :, place, i // 32] = 0xFF
+    want, weight = reference(q, starts, values_of(cache, "k"), values_of(cache, "v"), tables, lens, dim ** -0.5, pages, rule)
+    there = torch.cat([torch.arange(int(starts[b]), int(starts[b + 1])) for b in range(B)])
+    if max(fresh) == 1:
+        got = tq.torq_paged_attention(q.to(DEV), cache, tables.to(DEV), lens.to(DEV), dim ** -0.5, scores=rule.on(tq))
+    else:
+        got = tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, tables.to(DEV), lens.to(DEV), dim ** -0.5, most=max(fresh), scores=rule.on(tq))
+    got, want, weight = got.cpu()[there], want[there], weight[there]
+    assert torch.equal(torch.isfinite(got), torch.isfinite(want)), (torch.isfinite(got) != torch.isfinite(want)).nonzero()[:5].tolist()
+    # an infinity comes through as itself, or as NaN where its weight is below 2^-126, fp32's least normal number, and so 0: 0 times infinity
+    infinite, nan = torch.isinf(want), torch.isnan(want)
+    assert bool(torch.isnan(got)[nan].all()) and bool(((got.double() == want) | torch.isnan(got))[infinite].all())
+    if rule.slopes is None:                          # (scores of a few units: no weight is that small)
+        assert torch.equal(torch.isnan(got), nan)
+    fine = torch.isfinite(want)
+    check(torch.where(fine, got.double(), 0.0), torch.where(fine, want, 0.0), torch.where(fine, weight, 1.0), few(heads, kv_heads, max(fresh)))
