@@ -10,10 +10,9 @@ namespace torq {
 // The parts of a row tile's rows put together in the order of the keys: a thread takes four values of a row.
 __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a) {
   const int kv_head = blockIdx.x % a.kv_heads, slot = blockIdx.x / a.kv_heads;
-  int b, row_tile;
-  if (!row_tile_of(a, slot, b, row_tile)) return;
-  const int2 there = rows_of_request(a, a.rule.starts[b], a.rule.starts[b + 1]);
-  const int rows = min(there.y - there.x, a.rule.most) * a.rule.heads_each, quads = a.dim / 4;
+  RowTile it;
+  if (!row_tile_of(a, slot, it)) return;
+  const int row_tile = it.tile, rows = min(it.rows_there, a.rule.most) * a.rule.heads_each, quads = a.dim / 4;
   const int64_t part0 = ((int64_t)slot * a.kv_heads + kv_head) * a.splits * a.tile_rows;
   for (int x = blockIdx.y * 256 + threadIdx.x; x < a.tile_rows * quads; x += gridDim.y * 256) {
     const int r = x / quads, c = x - r * quads;
@@ -31,7 +30,7 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a) {
       v += f * *reinterpret_cast<const f32x4 *>(a.part + part * a.dim + 4 * c);
     }
     v *= l != 0.0f ? 1.0f / l : 0.0f;
-    uint16_t *const out = a.out + ruled_row(a, there.x, kv_head, row_tile * a.tile_rows + r) * a.dim;
+    uint16_t *const out = a.out + ruled_row(a, it.q_at, kv_head, row_tile * a.tile_rows + r) * a.dim;
     *reinterpret_cast<bf16x4 *>(out + 4 * c) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
   }
 }
@@ -39,16 +38,21 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a) {
 namespace {
 // So few rows of a request that they are columns of the single token's kernels
 bool few_rows(const torq_kv_cache_t &cache, int heads, int most) { return (int64_t)(heads / cache.heads) * most <= 32; }
+// What the kernel does to scores ahead of the weights: a cap whose error in the short form, 2^-23 of it, is below 2^-15 of a weight, or slopes; any
+// other rule, and a scale of 0 or nearly (0 times minus infinity is none: times it ahead of the maximum) by the kernel that looks.
+int bend_of(float scale, const torq_scores_t *scores) {
+  const bool cap = scores && scores->cap > 0.0f, slopes = scores && scores->slopes;
+  if (cap) return slopes || scores->cap > 177.0f ? BEND_ANY : BEND_CAP;
+  return slopes ? BEND_SLOPES : std::fabs(scale) < 2.0f * FLT_MIN ? BEND_ANY : BEND_NONE;
+}
 struct ChunkPlan {
   int64_t slots, items;
   int splits, rows;
-  bool tall;
 };
 ChunkPlan chunk_plan(const torq_kv_cache_t &cache, int heads, int64_t tokens, int most, int64_t B, int width) {
   ChunkPlan p;
   const int64_t each = heads / cache.heads;
-  p.tall = most * each > 64 || cache.head_dim > 128;
-  p.rows = p.tall ? 128 : 64;
+  p.rows = most * each <= 64 && cache.head_dim <= 128 ? 64 : 128;
   p.slots = std::min(tokens * each / p.rows + std::min(B, tokens), B * ((most * each + p.rows - 1) / p.rows));
   p.items = p.slots * cache.heads;
   const int64_t steps = ((int64_t)width * cache.page_size + CHUNK_STEP - 1) / CHUNK_STEP, full = cache.head_dim <= 128 ? 512 : 256;
@@ -76,14 +80,18 @@ hipError_t launch_chunk_attention(const torq_kv_cache_t &cache, const void *q, i
                                                    out, scores, starts, most, tokens);
   a.part = (float *)workspace, a.part_ml = a.part + plan.items * plan.splits * plan.rows * cache.head_dim;
   a.c = std::fabs(a.scale_log2), a.flip = a.scale_log2 < 0.0f;
+  const int bend = bend_of(scale, scores);
+  a.any_cap = a.rule.cap_out > 0.0f;
+  if (a.any_cap) a.c = a.scale_log2 = a.rule.cap_out;
+  if (bend == BEND_CAP) a.c = 2.0f * a.rule.cap_out, a.rule.cap_in = std::max(-FLT_MAX, std::min(FLT_MAX, 2.88539008177792681472f * a.rule.cap_in));
+  if (bend >= BEND_SLOPES) a.c = 1.0f;
   a.slots = (int)plan.slots, a.splits = plan.splits, a.tile_rows = plan.rows;
-  const bool bent = a.rule.cap_out > 0.0f || a.rule.slopes || a.c < FLT_MIN;
   const unsigned groups = (unsigned)(plan.items * plan.splits);
   (cache.head_dim <= 64    ? go_chunk_64
    : cache.head_dim <= 96  ? go_chunk_96
    : cache.head_dim <= 128 ? go_chunk_128
    : cache.head_dim <= 192 ? go_chunk_192
-                           : go_chunk_256)(a, cache.format, bent, plan.tall, groups, stream);
+                           : go_chunk_256)(a, cache.format, bend, groups, stream);
   if (plan.splits > 1)
     hipLaunchKernelGGL(chunk_join_kernel, dim3((unsigned)plan.items, 8), dim3(256), 0, stream, a);
   return hipGetLastError();

@@ -3,8 +3,8 @@
 
 namespace torq {
 
-void go_chunk_256(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream) {
-  go_chunk<256, 256>(a, format, bent, tall, groups, stream);
+void go_chunk_256(const ChunkArgs &a, int format, int bend, unsigned groups, hipStream_t stream) {
+  go_chunk<256, 256>(a, format, bend, groups, stream);
 }
 
 }  // namespace torq

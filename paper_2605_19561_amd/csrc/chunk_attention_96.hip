@@ -3,8 +3,8 @@
 
 namespace torq {
 
-void go_chunk_96(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream) {
-  go_chunk<128, 96>(a, format, bent, tall, groups, stream);
+void go_chunk_96(const ChunkArgs &a, int format, int bend, unsigned groups, hipStream_t stream) {
+  go_chunk<128, 96>(a, format, bend, groups, stream);
 }
 
 }  // namespace torq

@@ -25,9 +25,11 @@
 namespace torq {
 
 constexpr int CHUNK_STEP = 32;         // keys of a step
+constexpr int BEND_NONE = 0, BEND_CAP = 1, BEND_SLOPES = 2, BEND_ANY = 3;
 
 struct ChunkArgs : AttentionArgs {
-  float c;                             // what scores are times in the exponent of 2
+  float c;                             // what (bent) scores are times in the exponent of 2
+  int any_cap;                         // (BEND_ANY) tanh of cap_in times the scores, ahead of scale_log2
   int flip;                            // q's signs (a scale below 0)
   int tile_rows;                       // rows of a workgroup
   int slots, splits;                   // row tiles of a key head at most; parts of the keys of one
@@ -49,40 +51,57 @@ __device__ __forceinline__ int v_place(int key, int piece) {
   return key * DP * 2 + (piece ^ by) * 16;
 }
 
-// The request and the tile of its rows that a slot is, the last tiles of a request first; the same in every lane.
-__device__ __forceinline__ bool row_tile_of(const ChunkArgs &a, int slot, int &b, int &row_tile) {
+// The request and the tile of its rows that a slot is, the last tiles of a request first, and what the kernel goes by of it: looked up by lanes, eight
+// requests each, all in one go.  The same in every lane.
+struct RowTile {
+  int b, tile, q_at, rows_there, length, prefix;
+};
+__device__ __forceinline__ bool row_tile_of(const ChunkArgs &a, int slot, RowTile &found) {
   const int lane = threadIdx.x & 63;
-  auto tiles_of = [&](int i) {
-    if (i >= a.B) return 0;
-    const int2 rows = rows_of_request(a, a.rule.starts[i], a.rule.starts[i + 1]);
-    return (int)(((int64_t)min(rows.y - rows.x, a.rule.most) * a.rule.heads_each + a.tile_rows - 1) / a.tile_rows);
-  };
-  int before = 0, found = -1, at_it = 0, there = 0;
-  for (int b0 = 0; b0 < a.B && found < 0; b0 += 512) {          // a lane adds up eight requests
-    int count[8], mine = 0;
+  int before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 512) {
+    int start[8], there[8], length[8], prefix[8], mine = 0;
+    const int per = min((a.B - b0 + 63) / 64, 8);
+    auto tiles_of = [&](int rows) { return (int)(((int64_t)min(rows, a.rule.most) * a.rule.heads_each + a.tile_rows - 1) / a.tile_rows); };
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mine += count[i] = tiles_of(b0 + lane * 8 + i);
+    for (int i = 0; i < 8; ++i) {
+      const int b = b0 + lane * per + i;
+      start[i] = there[i] = length[i] = prefix[i] = 0;
+      if (i < per && b < a.B) {
+        const int2 rows = rows_of_request(a, a.rule.starts[b], a.rule.starts[b + 1]);
+        start[i] = rows.x, there[i] = rows.y - rows.x, length[i] = a.lengths[b];
+        if (a.rule.prefix) prefix[i] = a.rule.prefix[b];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mine += tiles_of(there[i]);
     const int sum = before + wave_sum(mine);
     const uint64_t behind = __ballot(slot < sum);
     if (behind) {
       const int owner = __builtin_ctzll(behind);
       int at = __builtin_amdgcn_readlane(sum - mine, owner);
+      bool done = false;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int here = __builtin_amdgcn_readlane(count[i], owner);
-        if (found < 0 && slot < at + here) found = b0 + owner * 8 + i, at_it = at, there = here;
-        at += here;
+        const int rows = __builtin_amdgcn_readlane(there[i], owner), tiles = tiles_of(rows);
+        if (!done && slot < at + tiles) {
+          done = true;
+          found = RowTile{b0 + owner * per + i, tiles - 1 - (slot - at), __builtin_amdgcn_readlane(start[i], owner), rows,
+                          __builtin_amdgcn_readlane(length[i], owner), __builtin_amdgcn_readlane(prefix[i], owner)};
+        }
+        at += tiles;
       }
+      return true;
     }
     before = __builtin_amdgcn_readlane(sum, 63);
   }
-  b = __builtin_amdgcn_readfirstlane(found), row_tile = __builtin_amdgcn_readfirstlane(there - 1 - (slot - at_it));
-  return b >= 0;
+  return false;
 }
 
 // DP: values of a row in LDS, of which the first DV are multiplied.  RW: waves that share keys, each with 32 rows of its own; the other 4 / RW - 1 such
 // groups have the same rows and other keys.
-template <int DP, int DV, int FMT, bool BENT, int RW>
+// BEND: what is done to scores ahead of the weights; ANY looks what, and takes all steps one instruction after the other.
+template <int DP, int DV, int FMT, int BEND, int RW>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 256 || DP * (4 / RW) > 128 ? 1 : 2, DP == 256 || DP * (4 / RW) > 128 ? 1 : 2))) chunk_attention_kernel(ChunkArgs a) {
   constexpr bool SCALED = FMT != FMT_BF16;
   constexpr int BITS = FMT == FMT_BF16 ? 16 : FMT == FMT_MXFP8 ? 8 : 4;
@@ -102,18 +121,16 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
   const int rp = wave % RW, kp = wave / RW;
   char *const ring_k = lds + kp * SLOTS * (K::BYTES + SIDE), *const ring_v = ring_k + SLOTS * K::BYTES;
-  const uniform_ints lengths = (uniform_ints)(uintptr_t)a.lengths, starts = (uniform_ints)(uintptr_t)a.rule.starts;
   auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
 
   // the workgroup's key head, part and row tile (all key heads of a part side by side: with 8 of them one for each XCD's L2; the last rows of a request,
   // which have the most keys, first)
   const int kv_head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits, slot = rest / a.splits;
-  int b, row_tile;
-  if (!row_tile_of(a, slot, b, row_tile)) return;
-  const int2 rows_there = rows_of_request(a, starts[b], starts[b + 1]);
-  const int q_at = uniform(rows_there.x), fresh = uniform(min(rows_there.y - rows_there.x, a.rule.most)), each = a.rule.heads_each;
-  const int length = uniform(length_of(a, lengths[b])), first = uniform(lengths[b] - (rows_there.y - rows_there.x));
-  const int prefix = uniform(a.rule.prefix ? min(max(((uniform_ints)(uintptr_t)a.rule.prefix)[b], 0), length) : 0);
+  RowTile it;
+  if (!row_tile_of(a, slot, it)) return;
+  const int b = uniform(it.b), row_tile = uniform(it.tile), q_at = uniform(it.q_at), each = a.rule.heads_each;
+  const int fresh = uniform(min(it.rows_there, a.rule.most)), length = uniform(length_of(a, it.length)), first = uniform(it.length - it.rows_there);
+  const int prefix = uniform(min(max(it.prefix, 0), length));
   const int window = a.rule.window, rows = fresh * each, row0 = row_tile * a.tile_rows;
   auto low_of = [&](int p) { return window && p >= window ? p - window + 1 : 0; };
   auto position_of = [&](int row) { return first + min(row, rows - 1) / each; };
@@ -134,14 +151,14 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
   const int row = row0 + rp * 32 + n, token = row / each, head = kv_head * each + row - token * each;
   const bool wave_in = row0 + rp * 32 < rows, in = row < rows;
   const int position = first + token, low = low_of(position), span = max(min(position + 1, length) - low, 0);    // its window's keys: span from low on
-  const float slope = BENT && a.rule.slopes && in ? 1.44269504088896340736f * a.rule.slopes[head] : 0.0f;
+  const float slope = BEND >= BEND_SLOPES && a.rule.slopes && in ? 1.44269504088896340736f * a.rule.slopes[head] : 0.0f;
   bf16x8 q[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     const int i = 16 * s + 8 * h;
     u32x4 v = {0, 0, 0, 0};
     if (in && i < a.dim) v = *reinterpret_cast<const u32x4 *>(a.q + (int64_t)(q_at + token) * a.q_stride + (int64_t)head * a.q_head_stride + i);
-    if (!BENT && a.flip) v ^= 0x80008000u;
+    if (BEND == BEND_NONE && a.flip) v ^= 0x80008000u;
     q[s] = as_bf16(v);
   }
 
@@ -258,7 +275,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
   for (int i = 0; i < IB; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
-  const float c = BENT ? 1.0f : a.c;
+  const float c = a.c;
   // this lane's pieces of its key
   int k_base[2] = {K::at(n, h), K::at(n, h + (DP < 256 ? 2 : 0))};
   // where this lane's part of four keys' values lies, those of i = 0 ... 31 of the keys 4 h ... 4 h + 3
@@ -297,12 +314,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
 #pragma unroll
       for (int r = 4 * i; r < 4 * i + 4; ++r) {
         const int t = 8 * (r / 4) + r % 4;
-        if constexpr (BENT) {
-          float x = st[r] * a.scale_log2;
-          if (a.rule.cap_out > 0.0f) x = capped(st[r], a.rule.cap_in, a.rule.cap_out);
-          if (a.rule.slopes) x -= slope * fabsf((float)(position - from) - (float)t);
-          st[r] = x;
-        }
+        // (a row's scores are as good less a number of its own, so -1 / (1 + e^2y) does for tanh(y) / 2, to 2^-24)
+        if constexpr (BEND == BEND_CAP) st[r] = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(st[r] * a.rule.cap_in));
+        if constexpr (BEND == BEND_ANY) st[r] = (a.any_cap ? capped(st[r], a.rule.cap_in, 1.0f) : st[r]) * a.scale_log2;
+        if constexpr (BEND == BEND_SLOPES) st[r] = __builtin_fmaf(st[r], a.scale_log2, -slope * fabsf((float)(position - from) - (float)t));
+        if constexpr (BEND == BEND_ANY) st[r] -= slope * fabsf((float)(position - from) - (float)t);
         if constexpr (EDGE) {
           const bool seen = ((uint32_t)(from - low + t) < (uint32_t)span) | (from - prefix + t < 0);
           st[r] = (seen & !(lost >> (r / 8) & 1)) ? st[r] : -INFINITY;
@@ -398,14 +414,14 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
         before[1] = before[0], before[0] = now;
       }
       if (wave_in) {
-        constexpr int PRODUCTS = decltype(with_products)::value ? KS + 2 * IB : KS, AHEAD = 3;
+        constexpr int PRODUCTS = decltype(with_products)::value ? KS + 2 * IB : KS, AHEAD = 2;
         auto operand = [&](int i) { return i < KS ? k_operand(P ^ 1, i) : v_operand(P ^ 1, i - KS); };
         auto multiply = [&](bf16x8 x, int i) {
           if (i < KS) score(st[P ^ 1], x, i);
           else product(x, pt[P ^ 1], i - KS);
         };
         bf16x8 x[PRODUCTS];
-        if (edge) {                                 // (few steps: one after the other)
+        if (BEND == BEND_ANY || edge) {             // (few steps: one after the other)
           static_for<PIECES>([&](auto i) { piece(std::true_type{}, i, key0, lost, st[P], pt[P]); });
           static_for<PRODUCTS>([&](auto i) {
             if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);         // (two operands at a time, for the registers)
@@ -556,29 +572,31 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
   }
 }
 
-// Kernels of one width: 128 rows of a workgroup (tall) or 64.
+// Kernels of one width, by the rows of a workgroup: 128 or 64.
 template <int DP, int DV>
-void go_chunk(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream) {
+void go_chunk(const ChunkArgs &a, int format, int bend, unsigned groups, hipStream_t stream) {
   auto of_rows = [&](auto of, auto with, auto waves) {
     hipLaunchKernelGGL((chunk_attention_kernel<DP, DV, decltype(of)::value, decltype(with)::value, decltype(waves)::value>), dim3(groups), dim3(256), 0, stream, a);
   };
   auto of_scores = [&](auto of, auto with) {
     if constexpr (DP < 256)
-      if (!tall) return of_rows(of, with, std::integral_constant<int, 2>{});
+      if (a.tile_rows == 64) return of_rows(of, with, std::integral_constant<int, 2>{});
     of_rows(of, with, std::integral_constant<int, 4>{});
   };
   auto of_format = [&](auto of) {
-    if (bent) of_scores(of, std::true_type{});
-    else of_scores(of, std::false_type{});
+    if (bend == BEND_NONE) of_scores(of, std::integral_constant<int, BEND_NONE>{});
+    else if (bend == BEND_CAP) of_scores(of, std::integral_constant<int, BEND_CAP>{});
+    else if (bend == BEND_SLOPES) of_scores(of, std::integral_constant<int, BEND_SLOPES>{});
+    else of_scores(of, std::integral_constant<int, BEND_ANY>{});
   };
   if (format == FMT_BF16) of_format(std::integral_constant<int, FMT_BF16>{});
   else if (format == FMT_MXFP8) of_format(std::integral_constant<int, FMT_MXFP8>{});
   else of_format(std::integral_constant<int, FMT_MXFP4>{});
 }
-void go_chunk_64(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream);     // chunk_attention_64.hip, ...
-void go_chunk_96(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream);
-void go_chunk_128(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream);
-void go_chunk_192(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream);
-void go_chunk_256(const ChunkArgs &a, int format, bool bent, bool tall, unsigned groups, hipStream_t stream);
+void go_chunk_64(const ChunkArgs &a, int format, int bend, unsigned groups, hipStream_t stream);     // chunk_attention_64.hip, ...
+void go_chunk_96(const ChunkArgs &a, int format, int bend, unsigned groups, hipStream_t stream);
+void go_chunk_128(const ChunkArgs &a, int format, int bend, unsigned groups, hipStream_t stream);
+void go_chunk_192(const ChunkArgs &a, int format, int bend, unsigned groups, hipStream_t stream);
+void go_chunk_256(const ChunkArgs &a, int format, int bend, unsigned groups, hipStream_t stream);
 
 }  // namespace torq

@@ -462,3 +462,17 @@ def test_what_a_query_does_not_see_takes_no_part(tq, heads, kv_heads, dim, page,
         assert torch.equal(torch.isnan(got), nan)
     fine = torch.isfinite(want)
     check(torch.where(fine, got.double(), 0.0), torch.where(fine, want, 0.0), torch.where(fine, weight, 1.0), few(heads, kv_heads, max(fresh)))
+
+
+@gpu
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-30, 3.0])
+@pytest.mark.parametrize("cap", [0.0, 1e-3, 2.0, 170.0, 200.0, 1e5, 1e30])
+@pytest.mark.parametrize("fresh,dim", [([1, 1], 128), ([3, 2], 64), ([40, 70], 128), ([70, 80], 64), ([50, 33], 256)])
+def test_scales_and_caps_of_every_size(tq, fresh, dim, cap, scale):
+    lengths = [90, 100]
+    cache, q, starts, tables, lens, pages = case(tq, fresh, lengths, 4, 2, dim, 16, "bf16", "heads", 7, spread=1.0)
+    for slopes in (None, slopes_of(4)):
+        rule = Rule(cap=cap, slopes=slopes)
+        want = reference(q, starts, values_of(cache, "k"), values_of(cache, "v"), tables, lens, scale, pages, rule)
+        got = tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, tables.to(DEV), lens.to(DEV), scale, most=max(fresh), scores=rule.on(tq))
+        check(got, *want, few(4, 2, max(fresh)))
