@@ -52,10 +52,10 @@ struct ChunkPlan {
 ChunkPlan chunk_plan(const torq_kv_cache_t &cache, int heads, int64_t tokens, int most, int64_t B, int width) {
   ChunkPlan p;
   const int64_t each = heads / cache.heads;
-  p.rows = most * each <= 64 && cache.head_dim <= 128 ? 64 : 128;
+  p.rows = cache.head_dim > 128 ? 128 : most * each <= 64 ? 64 : most * each <= 128 ? 128 : 256;
   p.slots = std::min(tokens * each / p.rows + std::min(B, tokens), B * ((most * each + p.rows - 1) / p.rows));
   p.items = p.slots * cache.heads;
-  const int64_t steps = ((int64_t)width * cache.page_size + CHUNK_STEP - 1) / CHUNK_STEP, full = cache.head_dim <= 128 ? 512 : 256;
+  const int64_t steps = ((int64_t)width * cache.page_size + CHUNK_STEP - 1) / CHUNK_STEP, full = cache.head_dim <= 128 && p.rows == 128 ? 512 : 256;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(full + p.items - 1) / std::max<int64_t>(p.items, 1), steps / 8, 64}));
   return p;
 }

@@ -98,11 +98,136 @@ __device__ __forceinline__ bool row_tile_of(const ChunkArgs &a, int slot, RowTil
   return false;
 }
 
-// DP: values of a row in LDS, of which the first DV are multiplied.  RW: waves that share keys, each with 32 rows of its own; the other 4 / RW - 1 such
-// groups have the same rows and other keys.
+// O^T of a wave's NR blocks of 32 rows, IB pieces of 32 values each.  One block's lies in registers as the compiler takes them.  Two blocks' take all of
+// the accumulators' half from a0 on, by name: left to itself the compiler keeps copying O (or Q) between the halves, 230 moves a step and twice the time.
+// Nothing else in those kernels touches that half (a build test looks), and the waits between a product and what reads or writes O besides are kept here:
+// 8 passes and 11 cycles ahead, 4 behind.
+template <int NR, int IB>
+struct Sums {
+  f32x16 o[NR][IB];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int x = 0; x < NR; ++x)
+#pragma unroll
+      for (int i = 0; i < IB; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[x][i][r] = 0.0f;
+  }
+  template <int X, int I>
+  __device__ __forceinline__ void add_product(bf16x8 a, u32x4 b) {
+    o[X][I] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, b), o[X][I], 0, 0, 0);
+  }
+  template <int X, int I>
+  __device__ __forceinline__ void scale(float by) {
+    o[X][I] *= by;
+  }
+  template <int X, int I, int R>
+  __device__ __forceinline__ float get() {
+    return o[X][I][R];
+  }
+  template <int X, int I, int R>
+  __device__ __forceinline__ void put(float v) {
+    o[X][I][R] = v;
+  }
+  __device__ __forceinline__ void settle() {}
+};
+#define TORQ_SUMS_CLOBBERED \
+  "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", "a10", "a11", "a12", "a13", "a14", "a15", \
+  "a16", "a17", "a18", "a19", "a20", "a21", "a22", "a23", "a24", "a25", "a26", "a27", "a28", "a29", "a30", "a31", \
+  "a32", "a33", "a34", "a35", "a36", "a37", "a38", "a39", "a40", "a41", "a42", "a43", "a44", "a45", "a46", "a47", \
+  "a48", "a49", "a50", "a51", "a52", "a53", "a54", "a55", "a56", "a57", "a58", "a59", "a60", "a61", "a62", "a63", \
+  "a64", "a65", "a66", "a67", "a68", "a69", "a70", "a71", "a72", "a73", "a74", "a75", "a76", "a77", "a78", "a79", \
+  "a80", "a81", "a82", "a83", "a84", "a85", "a86", "a87", "a88", "a89", "a90", "a91", "a92", "a93", "a94", "a95", \
+  "a96", "a97", "a98", "a99", "a100", "a101", "a102", "a103", "a104", "a105", "a106", "a107", "a108", "a109", "a110", "a111", \
+  "a112", "a113", "a114", "a115", "a116", "a117", "a118", "a119", "a120", "a121", "a122", "a123", "a124", "a125", "a126", "a127"
+template <int IB>
+struct Sums<2, IB> {
+  template <int X, int I>
+  static constexpr int at = 16 * (X * IB + I);
+  __device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+  __device__ __forceinline__ void zero() {
+    static_for<32 * IB>([](auto r) { asm volatile("v_accvgpr_write_b32 a[%0], 0" ::"n"(decltype(r)::value) : TORQ_SUMS_CLOBBERED); });
+    settle();
+  }
+  template <int X, int I>
+  __device__ __forceinline__ void add_product(bf16x8 a, u32x4 b) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 a[%2:%2+15], %0, %1, a[%2:%2+15]" ::"v"(a), "v"(b), "n"(at<X, I>) : TORQ_SUMS_CLOBBERED);
+  }
+  template <int X, int I>
+  __device__ __forceinline__ void scale(float by) {
+    float t[16];
+    asm volatile(
+      "v_accvgpr_read_b32 %0, a[%17+0]\n\t"
+      "v_accvgpr_read_b32 %1, a[%17+1]\n\t"
+      "v_accvgpr_read_b32 %2, a[%17+2]\n\t"
+      "v_accvgpr_read_b32 %3, a[%17+3]\n\t"
+      "v_accvgpr_read_b32 %4, a[%17+4]\n\t"
+      "v_accvgpr_read_b32 %5, a[%17+5]\n\t"
+      "v_accvgpr_read_b32 %6, a[%17+6]\n\t"
+      "v_accvgpr_read_b32 %7, a[%17+7]\n\t"
+      "v_accvgpr_read_b32 %8, a[%17+8]\n\t"
+      "v_accvgpr_read_b32 %9, a[%17+9]\n\t"
+      "v_accvgpr_read_b32 %10, a[%17+10]\n\t"
+      "v_accvgpr_read_b32 %11, a[%17+11]\n\t"
+      "v_accvgpr_read_b32 %12, a[%17+12]\n\t"
+      "v_accvgpr_read_b32 %13, a[%17+13]\n\t"
+      "v_accvgpr_read_b32 %14, a[%17+14]\n\t"
+      "v_accvgpr_read_b32 %15, a[%17+15]\n\t"
+      "v_mul_f32 %0, %0, %16\n\t"
+      "v_mul_f32 %1, %1, %16\n\t"
+      "v_mul_f32 %2, %2, %16\n\t"
+      "v_mul_f32 %3, %3, %16\n\t"
+      "v_mul_f32 %4, %4, %16\n\t"
+      "v_mul_f32 %5, %5, %16\n\t"
+      "v_mul_f32 %6, %6, %16\n\t"
+      "v_mul_f32 %7, %7, %16\n\t"
+      "v_mul_f32 %8, %8, %16\n\t"
+      "v_mul_f32 %9, %9, %16\n\t"
+      "v_mul_f32 %10, %10, %16\n\t"
+      "v_mul_f32 %11, %11, %16\n\t"
+      "v_mul_f32 %12, %12, %16\n\t"
+      "v_mul_f32 %13, %13, %16\n\t"
+      "v_mul_f32 %14, %14, %16\n\t"
+      "v_mul_f32 %15, %15, %16\n\t"
+      "v_accvgpr_write_b32 a[%17+0], %0\n\t"
+      "v_accvgpr_write_b32 a[%17+1], %1\n\t"
+      "v_accvgpr_write_b32 a[%17+2], %2\n\t"
+      "v_accvgpr_write_b32 a[%17+3], %3\n\t"
+      "v_accvgpr_write_b32 a[%17+4], %4\n\t"
+      "v_accvgpr_write_b32 a[%17+5], %5\n\t"
+      "v_accvgpr_write_b32 a[%17+6], %6\n\t"
+      "v_accvgpr_write_b32 a[%17+7], %7\n\t"
+      "v_accvgpr_write_b32 a[%17+8], %8\n\t"
+      "v_accvgpr_write_b32 a[%17+9], %9\n\t"
+      "v_accvgpr_write_b32 a[%17+10], %10\n\t"
+      "v_accvgpr_write_b32 a[%17+11], %11\n\t"
+      "v_accvgpr_write_b32 a[%17+12], %12\n\t"
+      "v_accvgpr_write_b32 a[%17+13], %13\n\t"
+      "v_accvgpr_write_b32 a[%17+14], %14\n\t"
+      "v_accvgpr_write_b32 a[%17+15], %15\n\t"
+      "s_nop 4"
+      : "=&v"(t[0]), "=&v"(t[1]), "=&v"(t[2]), "=&v"(t[3]), "=&v"(t[4]), "=&v"(t[5]), "=&v"(t[6]), "=&v"(t[7]), "=&v"(t[8]), "=&v"(t[9]), "=&v"(t[10]), "=&v"(t[11]), "=&v"(t[12]), "=&v"(t[13]), "=&v"(t[14]), "=&v"(t[15])
+      : "v"(by), "n"(at<X, I>)
+      : TORQ_SUMS_CLOBBERED);
+  }
+  template <int X, int I, int R>
+  __device__ __forceinline__ float get() {
+    float v;
+    asm volatile("v_accvgpr_read_b32 %0, a[%1]" : "=v"(v) : "n"(at<X, I> + R));
+    return v;
+  }
+  template <int X, int I, int R>
+  __device__ __forceinline__ void put(float v) {
+    asm volatile("v_accvgpr_write_b32 a[%1], %0" ::"v"(v), "n"(at<X, I> + R) : TORQ_SUMS_CLOBBERED);
+  }
+};
+#undef TORQ_SUMS_CLOBBERED
+
+// DP: values of a row in LDS, of which the first DV are multiplied.  RW: waves that share keys, each with NR blocks of 32 rows of its own; the other
+// 4 / RW - 1 such groups have the same rows and other keys.
 // BEND: what is done to scores ahead of the weights; ANY looks what, and takes all steps one instruction after the other.
-template <int DP, int DV, int FMT, int BEND, int RW>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 256 || DP * (4 / RW) > 128 ? 1 : 2, DP == 256 || DP * (4 / RW) > 128 ? 1 : 2))) chunk_attention_kernel(ChunkArgs a) {
+template <int DP, int DV, int FMT, int BEND, int RW, int NR>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1 || DP * (4 / RW) > 128 ? 1 : 2, NR > 1 || DP * (4 / RW) > 128 ? 1 : 2))) chunk_attention_kernel(ChunkArgs a) {
   constexpr bool SCALED = FMT != FMT_BF16;
   constexpr int BITS = FMT == FMT_BF16 ? 16 : FMT == FMT_MXFP8 ? 8 : 4;
   constexpr int KP = 4 / RW, WK = CHUNK_STEP / RW;              // groups of waves with keys of their own; keys that a wave brings
@@ -115,7 +240,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
   typedef KLayout<DP> K;
   constexpr int SETS = 2;                                       // steps whose loads are on their way in registers
   static_assert(W >= 4 && 64 % PER == 0 && (64 / PER <= 16) && WK <= 16);
-  constexpr int SLOTS = 4, ROWS = 32 * RW, PITCH = 9, RING = KP * SLOTS * (K::BYTES + SIDE), JOIN = KP * ROWS * (PITCH * 16 + 8);
+  constexpr int SLOTS = 4, ROWS = 32 * NR * RW, PITCH = 9, RING = KP * SLOTS * (K::BYTES + SIDE), JOIN = KP * ROWS * (PITCH * 16 + 8);
   __shared__ __attribute__((aligned(1024))) char lds[RING > JOIN ? RING : JOIN];     // [keys' group][K, V][step by turns]; then what is put together
   __shared__ int strange;                                       // a value that is not finite has been left out
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
@@ -147,19 +272,25 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
     return step >= end ? length : (step < prefix_steps ? step : step + skip) * CHUNK_STEP;
   };
 
-  // this lane's row
-  const int row = row0 + rp * 32 + n, token = row / each, head = kv_head * each + row - token * each;
-  const bool wave_in = row0 + rp * 32 < rows, in = row < rows;
-  const int position = first + token, low = low_of(position), span = max(min(position + 1, length) - low, 0);    // its window's keys: span from low on
-  const float slope = BEND >= BEND_SLOPES && a.rule.slopes && in ? 1.44269504088896340736f * a.rule.slopes[head] : 0.0f;
-  bf16x8 q[KS];
+  // this lane's rows
+  const bool wave_in = row0 + rp * NR * 32 < rows;
+  int position[NR], low[NR], span[NR];              // the keys that a window holds: span of them from low on
+  float slope[NR];
+  bf16x8 q[NR][KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    const int i = 16 * s + 8 * h;
-    u32x4 v = {0, 0, 0, 0};
-    if (in && i < a.dim) v = *reinterpret_cast<const u32x4 *>(a.q + (int64_t)(q_at + token) * a.q_stride + (int64_t)head * a.q_head_stride + i);
-    if (BEND == BEND_NONE && a.flip) v ^= 0x80008000u;
-    q[s] = as_bf16(v);
+  for (int x = 0; x < NR; ++x) {
+    const int row = row0 + (rp * NR + x) * 32 + n, token = row / each, head = kv_head * each + row - token * each;
+    const bool in = row < rows;
+    position[x] = first + token, low[x] = low_of(position[x]), span[x] = max(min(position[x] + 1, length) - low[x], 0);
+    slope[x] = BEND >= BEND_SLOPES && a.rule.slopes && in ? 1.44269504088896340736f * a.rule.slopes[head] : 0.0f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int i = 16 * s + 8 * h;
+      u32x4 v = {0, 0, 0, 0};
+      if (in && i < a.dim) v = *reinterpret_cast<const u32x4 *>(a.q + (int64_t)(q_at + token) * a.q_stride + (int64_t)head * a.q_head_stride + i);
+      if (BEND == BEND_NONE && a.flip) v ^= 0x80008000u;
+      q[x][s] = as_bf16(v);
+    }
   }
 
   // Where the keys lie.  A lane looks up one of the 64 groups of 16 keys of 32 steps from w on, two windows ahead of their use: its page, then its place in
@@ -269,12 +400,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
       }
   };
 
-  f32x16 o[IB];
-  float m = -INFINITY, l = 0.0f;                    // m in the exponent of 2
+  Sums<NR, IB> o;
+  o.zero();
+  float m[NR], l[NR];                               // m in the exponent of 2
 #pragma unroll
-  for (int i = 0; i < IB; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
+  for (int x = 0; x < NR; ++x) m[x] = -INFINITY, l[x] = 0.0f;
   const float c = a.c;
   // this lane's pieces of its key
   int k_base[2] = {K::at(n, h), K::at(n, h + (DP < 256 ? 2 : 0))};
@@ -295,21 +425,26 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + 8 * DP * 2));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  auto score = [&](f32x16 &st, bf16x8 x, int s) {
-    if (s == 0)
+  auto score = [&](f32x16 (&st)[NR], bf16x8 operand, int s) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st[r] = 0.0f;
-    st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[s], st, 0, 0, 0);
+    for (int x = 0; x < NR; ++x) {
+      if (s == 0)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st[x][r] = 0.0f;
+      st[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand, q[x][s], st[x], 0, 0, 0);
+    }
   };
-  auto product = [&](bf16x8 x, const u32x4 (&pt)[2], int i) {
-    o[i % IB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, as_bf16(pt[i / IB]), o[i % IB], 0, 0, 0);
+  auto product = [&](bf16x8 operand, const u32x4 (&pt)[NR][2], auto number) {
+    constexpr int I = decltype(number)::value;
+    static_for<NR>([&](auto x) { o.template add_product<decltype(x)::value, I % IB>(operand, pt[x][I / IB]); });
   };
-  constexpr int PIECES = 13;
-  float top = 0.0f, base = 0.0f, alpha = 1.0f;
-  bool moved = false;
-  auto piece = [&](auto at_edge, int i, int key0, int lost, f32x16 &st, u32x4 (&pt)[2]) {
+  constexpr int PIECES = 13 * NR;                    // of each block of rows by turns
+  float top[NR], base[NR], alpha[NR];
+  bool moved[NR];
+  auto piece = [&](auto at_edge, int number, int key0, int lost, f32x16 (&scores)[NR], u32x4 (&weights)[NR][2]) {
     constexpr bool EDGE = decltype(at_edge)::value;
-    const int from = key0 + 4 * h;
+    const int x = number % NR, i = number / NR, from = key0 + 4 * h;
+    f32x16 &st = scores[x];
     if (i < 4) {
 #pragma unroll
       for (int r = 4 * i; r < 4 * i + 4; ++r) {
@@ -317,35 +452,35 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
         // (a row's scores are as good less a number of its own, so -1 / (1 + e^2y) does for tanh(y) / 2, to 2^-24)
         if constexpr (BEND == BEND_CAP) st[r] = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(st[r] * a.rule.cap_in));
         if constexpr (BEND == BEND_ANY) st[r] = (a.any_cap ? capped(st[r], a.rule.cap_in, 1.0f) : st[r]) * a.scale_log2;
-        if constexpr (BEND == BEND_SLOPES) st[r] = __builtin_fmaf(st[r], a.scale_log2, -slope * fabsf((float)(position - from) - (float)t));
-        if constexpr (BEND == BEND_ANY) st[r] -= slope * fabsf((float)(position - from) - (float)t);
+        if constexpr (BEND == BEND_SLOPES) st[r] = __builtin_fmaf(st[r], a.scale_log2, -slope[x] * fabsf((float)(position[x] - from) - (float)t));
+        if constexpr (BEND == BEND_ANY) st[r] -= slope[x] * fabsf((float)(position[x] - from) - (float)t);
         if constexpr (EDGE) {
-          const bool seen = ((uint32_t)(from - low + t) < (uint32_t)span) | (from - prefix + t < 0);
+          const bool seen = ((uint32_t)(from - low[x] + t) < (uint32_t)span[x]) | (from - prefix + t < 0);
           st[r] = (seen & !(lost >> (r / 8) & 1)) ? st[r] : -INFINITY;
         }
-        top = r ? fmaxf(top, st[r]) : st[r];
+        top[x] = r ? fmaxf(top[x], st[r]) : st[r];
       }
     } else if (i == 4) {
-      const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-      top = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1])) * c;
-      moved = top - m > 8.0f;
-      const float now = moved ? top : m;
-      alpha = moved ? __builtin_amdgcn_exp2f(m - now) : 1.0f;
-      m = now, base = now == -INFINITY ? 0.0f : now;
-      l *= alpha;
+      const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[x]), __float_as_uint(top[x]), false, false);
+      const float most = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1])) * c;
+      moved[x] = most - m[x] > 8.0f;
+      const float now = moved[x] ? most : m[x];
+      alpha[x] = moved[x] ? __builtin_amdgcn_exp2f(m[x] - now) : 1.0f;
+      m[x] = now, base[x] = now == -INFINITY ? 0.0f : now;
+      l[x] *= alpha[x];
     } else {
       const int r = 2 * (i - 5);
-      const bf16x2 pair = {(__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[r], c, -base)),
-                           (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[r + 1], c, -base))};
-      l = __builtin_amdgcn_fdot2_f32_bf16(pair, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l, false);
-      pt[r / 8][r % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
+      const bf16x2 pair = {(__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[r], c, -base[x])),
+                           (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[r + 1], c, -base[x]))};
+      l[x] = __builtin_amdgcn_fdot2_f32_bf16(pair, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l[x], false);
+      weights[x][r / 8][r % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
     }
   };
   // Step j: the scores of step j + 1, the weights of j and the products of j - 1, none of which needs another.  Meanwhile what later steps need is on its
   // way into LDS, step x into slot x % SLOTS: straight from memory K of j + 3 and V of j + 2, or through registers K of j + 2 and V of j, with the loads for
   // SETS steps later.
-  f32x16 st[2];
-  u32x4 pt[2][2];
+  f32x16 st[2][NR];
+  u32x4 pt[2][NR][2];
   if (tid == 0) strange = 0;
   if (count > 0) {
     constexpr int FAR = DIRECT ? 3 : 4;             // of the steps ahead, the one whose K sets out
@@ -416,9 +551,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
       if (wave_in) {
         constexpr int PRODUCTS = decltype(with_products)::value ? KS + 2 * IB : KS, AHEAD = 2;
         auto operand = [&](int i) { return i < KS ? k_operand(P ^ 1, i) : v_operand(P ^ 1, i - KS); };
-        auto multiply = [&](bf16x8 x, int i) {
-          if (i < KS) score(st[P ^ 1], x, i);
-          else product(x, pt[P ^ 1], i - KS);
+        auto multiply = [&](bf16x8 x, auto number) {
+          constexpr int I = decltype(number)::value;
+          if constexpr (I < KS) score(st[P ^ 1], x, I);
+          else product(x, pt[P ^ 1], std::integral_constant<int, I - KS>{});
         };
         bf16x8 x[PRODUCTS];
         if (BEND == BEND_ANY || edge) {             // (few steps: one after the other)
@@ -433,16 +569,20 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
           static_for<PRODUCTS>([&](auto i) {
             constexpr int I = decltype(i)::value;
             __builtin_amdgcn_sched_barrier(0);
-            multiply(x[I], I);
+            multiply(x[I], i);
             if constexpr (I + AHEAD < PRODUCTS) x[I + AHEAD] = operand(I + AHEAD);
             static_for<(I + 1) * PIECES / PRODUCTS - I * PIECES / PRODUCTS>(
                 [&](auto k) { piece(std::false_type{}, I * PIECES / PRODUCTS + decltype(k)::value, key0, lost, st[P], pt[P]); });
           });
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (__any(moved))
+        bool any = false;
 #pragma unroll
-          for (int i = 0; i < IB; ++i) o[i] *= alpha;
+        for (int x = 0; x < NR; ++x) any |= moved[x];
+        if (__any(any)) {
+          o.settle();
+          static_for<NR>([&](auto x) { static_for<IB>([&](auto i) { o.template scale<decltype(x)::value, decltype(i)::value>(alpha[x]); }); });
+        }
       }
       // (the loads of this step stay on their way)
       if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * DL) : "memory");
@@ -476,6 +616,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
       finish(std::integral_constant<int, 0>{});
     }
   }
+  o.settle();
   __syncthreads();
   if (strange) {
     // What has been left out: an infinity or NaN for every row that sees its key, whatever the weight.
@@ -495,41 +636,45 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
         const int key = key0 + x, its_page = x < 16 ? page[0] : page[1], place = (x < 16 ? in_page[0] : in_page[1]) + x % 16;
         if (key >= length || (uint32_t)its_page >= (uint32_t)a.pages) continue;
         const int64_t at = its_page * a.page_bytes + (kv_head * a.head_bytes + (int64_t)(place * a.token_bytes));
-#pragma unroll
-        for (int i = 0; i < IB; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; r += 4) {
-            const int e = 32 * i + 2 * r + 4 * h;
-            if (e >= a.dim) continue;
-            uint32_t w[2];
-            if constexpr (FMT == FMT_BF16) {
-              w[0] = reinterpret_cast<const uint32_t *>(a.v + at)[e / 2], w[1] = reinterpret_cast<const uint32_t *>(a.v + at)[e / 2 + 1];
+        static_for<IB * 4>([&](auto number) {
+          constexpr int I = decltype(number)::value / 4, R = decltype(number)::value % 4 * 4;
+          const int e = 32 * I + 2 * R + 4 * h;
+          if (e >= a.dim) return;
+          uint32_t y[2];
+          if constexpr (FMT == FMT_BF16) {
+            y[0] = reinterpret_cast<const uint32_t *>(a.v + at)[e / 2], y[1] = reinterpret_cast<const uint32_t *>(a.v + at)[e / 2 + 1];
+          } else {
+            const float scale = __uint_as_float((uint32_t)a.v_scales[at / SCALE_OF + e / 32] << 23);
+            if constexpr (FMT == FMT_MXFP8) {
+              widen4(*reinterpret_cast<const uint32_t *>(a.v + at + e), scale, y[0], y[1]);
             } else {
-              const float scale = __uint_as_float((uint32_t)a.v_scales[at / SCALE_OF + e / 32] << 23);
-              if constexpr (FMT == FMT_MXFP8) {
-                widen4(*reinterpret_cast<const uint32_t *>(a.v + at + e), scale, w[0], w[1]);
-              } else {
-                const u32x4 y = widen8(*reinterpret_cast<const uint16_t *>(a.v + at + e / 2), scale);
-                w[0] = y[0], w[1] = y[1];
-              }
-            }
-            const bool seen = (((uint32_t)(key - low) < (uint32_t)span) | (key < prefix)) & (m != -INFINITY);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const float y = bf16_bits_to_f32(w[q / 2] >> 16 * (q % 2) & 0xFFFFu);
-              if (seen && !(fabsf(y) < INFINITY)) o[i][r + q] += y;
+              const u32x4 wide = widen8(*reinterpret_cast<const uint16_t *>(a.v + at + e / 2), scale);
+              y[0] = wide[0], y[1] = wide[1];
             }
           }
+          static_for<NR>([&](auto block) {
+            constexpr int X = decltype(block)::value;
+            const bool seen = (((uint32_t)(key - low[X]) < (uint32_t)span[X]) | (key < prefix)) & (m[X] != -INFINITY);
+            static_for<4>([&](auto z) {
+              constexpr int Z = decltype(z)::value;
+              const float value = bf16_bits_to_f32(y[Z / 2] >> 16 * (Z % 2) & 0xFFFFu);
+              const bool add = seen && !(fabsf(value) < INFINITY);
+              if (__any(add)) o.template put<X, I, R + Z>(o.template get<X, I, R + Z>() + (add ? value : 0.0f));
+            });
+          });
+        });
       }
     }
+    o.settle();
   }
   // (looked at anew from here on: what hangs on the row is not kept through the loop)
   int late = lane;
   asm volatile("" : "+v"(late));
   const int n_late = late & 31, h_late = late >> 5;
-  {
-    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-    l = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[x]), __float_as_uint(l[x]), false, false);
+    l[x] = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
   }
   const int64_t part = (((int64_t)slot * a.kv_heads + kv_head) * a.splits + split) * a.tile_rows;
   // four values of a row of the workgroup's
@@ -546,12 +691,17 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
   // the groups' put together, 32 values of every row at a time
   f32x4 *const mine = reinterpret_cast<f32x4 *>(lds);
   float *const ml = reinterpret_cast<float *>(mine + KP * ROWS * PITCH);
-  const int mine_at = kp * ROWS + rp * 32 + n_late;
-  if (h_late == 0) ml[2 * mine_at] = m, ml[2 * mine_at + 1] = l;
+  const int mine_at = kp * ROWS + rp * NR * 32 + n_late;
 #pragma unroll
-  for (int i = 0; i < IB; ++i) {
-#pragma unroll
-    for (int r = 0; r < 16; r += 4) mine[mine_at * PITCH + r / 2 + h_late] = f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
+  for (int x = 0; x < NR; ++x)
+    if (h_late == 0) ml[2 * (mine_at + 32 * x)] = m[x], ml[2 * (mine_at + 32 * x) + 1] = l[x];
+  static_for<IB>([&](auto piece_number) {
+    constexpr int i = decltype(piece_number)::value;
+    static_for<NR * 4>([&](auto number) {
+      constexpr int X = decltype(number)::value / 4, R = decltype(number)::value % 4 * 4;
+      mine[(mine_at + 32 * X) * PITCH + R / 2 + h_late] =
+          f32x4{o.template get<X, i, R>(), o.template get<X, i, R + 1>(), o.template get<X, i, R + 2>(), o.template get<X, i, R + 3>()};
+    });
     __syncthreads();
     for (int x = tid; x < ROWS * 8; x += 256) {
       const int row = x / 8, piece = x % 8;
@@ -569,19 +719,25 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP == 
       store(row, 32 * i + 4 * piece, y, top, sum);
     }
     if (i + 1 < IB) __syncthreads();
-  }
+  });
 }
 
-// Kernels of one width, by the rows of a workgroup: 128 or 64.
+// Kernels of one width, by the rows of a workgroup: 256, 128 or 64.
 template <int DP, int DV>
 void go_chunk(const ChunkArgs &a, int format, int bend, unsigned groups, hipStream_t stream) {
-  auto of_rows = [&](auto of, auto with, auto waves) {
-    hipLaunchKernelGGL((chunk_attention_kernel<DP, DV, decltype(of)::value, decltype(with)::value, decltype(waves)::value>), dim3(groups), dim3(256), 0, stream, a);
+  auto of_rows = [&](auto of, auto with, auto waves, auto blocks) {
+    hipLaunchKernelGGL((chunk_attention_kernel<DP, DV, decltype(of)::value, decltype(with)::value, decltype(waves)::value, decltype(blocks)::value>), dim3(groups),
+                       dim3(256), 0, stream, a);
   };
   auto of_scores = [&](auto of, auto with) {
-    if constexpr (DP < 256)
-      if (a.tile_rows == 64) return of_rows(of, with, std::integral_constant<int, 2>{});
-    of_rows(of, with, std::integral_constant<int, 4>{});
+    constexpr std::integral_constant<int, 1> one{};
+    constexpr std::integral_constant<int, 2> two{};
+    constexpr std::integral_constant<int, 4> four{};
+    if constexpr (DP < 256) {
+      if (a.tile_rows == 64) return of_rows(of, with, two, one);
+      if (a.tile_rows == 256) return of_rows(of, with, four, two);
+    }
+    of_rows(of, with, four, one);
   };
   auto of_format = [&](auto of) {
     if (bend == BEND_NONE) of_scores(of, std::integral_constant<int, BEND_NONE>{});
