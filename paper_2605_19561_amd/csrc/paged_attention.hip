@@ -629,7 +629,8 @@ hipError_t launch_paged_attention(const torq_kv_cache_t &cache, const void *q, i
     of_hint(dp, of8, std::false_type{});
   };
   auto of_dim = [&](auto dp) { f8 ? of_format(dp, std::true_type{}) : of_format(dp, std::false_type{}); };
-  const bool ruled = scores || starts;
+  // (a rule that says nothing is none)
+  const bool ruled = starts || (scores && (scores->cap > 0.0f || scores->slopes || scores->window || scores->prefix));
   if (ruled) (cache.format == FMT_BF16 ? go_scored_bf16 : f8 ? go_scored_mxfp8 : go_scored_mxfp4)(plan, a, once, stream);
   else if (cache.format == FMT_MXFP4) go_attention4(plan, a, once, stream);
   else if (cache.head_dim <= 64) of_dim(std::integral_constant<int, 64>{});

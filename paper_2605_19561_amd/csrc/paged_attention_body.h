@@ -52,6 +52,7 @@ constexpr int ATT_WAYS_ITEMS = 768;
 // into runs, by the waves that take turns.  64 requests of 1 to 600 tokens, 64 / 8 heads, with 0, 4, 8, 16: 35.4, 24.1, 23.9, 23.7 us;
 // 16 of 1000 to 8192 58.6, 58.7, 59.1, 60.4; 77 x 20 heads, a wave each, with 0, 1, 2, 5: 89.6, 89.8, 92.8, 95.0.
 constexpr int att_setup(int ways) { return ways > 1 ? 4 : 1; }
+constexpr float ATT_SLACK = 8.0f;    // how far scores may pass the base of the weights, in the exponent of 2
 constexpr int ATT_FAR = 0x7FFFFF00;   // an offset past every buffer
 
 // What begins in a run and does not end there: a request, which of the columns that a workgroup works on at a time, the place of its first
@@ -390,8 +391,41 @@ __device__ __forceinline__ void attention_body(const AttentionArgs &a) {
     return p;
   };
   struct Place {
-    int count[2];
+    int count[2], bytes[2];                         // tokens; bytes of the cache from the first to the end of the last
     int64_t at[2];
+  };
+  // Where the groups of a wave's next 32 tiles of a segment lie, a lane each.  The lanes work out together what takes a wave alone 100 scalar
+  // instructions for a tile; the tile's own then reads it lane by lane.
+  struct Window {
+    int page, t16, left, count, bytes;
+    uint32_t at_lo, at_hi;
+  };
+  auto look_ahead = [&](const Segment &s, int tile0) {            // its first; the pages are on the way
+    Window w;
+    const int tile = tile0 + lane / 2 * WAYS;
+    w.t16 = 2 * tile_at(s, tile) + (lane & 1);
+    const int entry = (int)((uint64_t)(uint32_t)max(w.t16, 0) * (uint64_t)a.page16_magic >> 38);
+    const bool rows = RULED ? s.rows_at * ROWS < rows_in(s) && s.rows_at < a.row_groups : s.rows_at < a.row_groups;
+    w.left = tile < s.last && rows ? max(s.length - 16 * w.t16, 0) : 0;
+    w.page = w.left ? a.tables[s.b * a.table_stride + entry] : -1;
+    return w;
+  };
+  auto work_out = [&](const Segment &s, Window &w) {
+    const int entry = (int)((uint64_t)(uint32_t)max(w.t16, 0) * (uint64_t)a.page16_magic >> 38);
+    const bool there = (uint32_t)w.page < (uint32_t)a.pages;      // (a page that is none: as a number without a sign past all others)
+    w.count = there ? min(w.left, 16) : 0;
+    w.bytes = w.count ? (w.count - 1) * a.token_bytes + a.dim * BITS / 8 : 0;
+    const int64_t at = (there ? w.page : 0) * a.page_bytes + (s.kv_head * a.head_bytes + (int64_t)(16 * (w.t16 - entry * (a.page_size / 16)) * a.token_bytes));
+    w.at_lo = (uint32_t)at, w.at_hi = (uint32_t)(at >> 32);
+  };
+  auto place_at = [&](const Window &w, int i) {
+    Place p;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      p.count[u] = __builtin_amdgcn_readlane(w.count, 2 * i + u), p.bytes[u] = __builtin_amdgcn_readlane(w.bytes, 2 * i + u);
+      p.at[u] = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(w.at_hi, 2 * i + u) << 32 | (uint32_t)__builtin_amdgcn_readlane(w.at_lo, 2 * i + u));
+    }
+    return p;
   };
   auto place = [&](const Segment &s, int tile, const Pages &p) {
     Place w;
@@ -402,15 +436,16 @@ __device__ __forceinline__ void attention_body(const AttentionArgs &a) {
       const bool rows = RULED ? s.rows_at * ROWS < rows_in(s) && s.rows_at < a.row_groups : s.rows_at < a.row_groups;
       const int left = tile < s.last && (uint32_t)p.page[u] < (uint32_t)a.pages && rows ? s.length - t : 0;
       w.count[u] = max(min(left, 16), 0);
+      w.bytes[u] = w.count[u] ? (w.count[u] - 1) * a.token_bytes + a.dim * BITS / 8 : 0;
       w.at[u] = (left > 0 ? p.page[u] : 0) * a.page_bytes + (s.kv_head * a.head_bytes + (int64_t)(p.in_page[u] * a.token_bytes));
     }
     return w;
   };
   auto rows_of = [&](const char *base, const Place &p, int u) {
-    return records(base, p.at[u], p.count[u] ? (p.count[u] - 1) * a.token_bytes + a.dim * BITS / 8 : 0);
+    return records(base, p.at[u], p.bytes[u]);
   };
   auto scales_of = [&](const uint8_t *base, const Place &p, int u) {
-    return records(base, p.at[u] / SCALE_OF, p.count[u] ? (p.count[u] - 1) * (a.token_bytes / SCALE_OF) + a.dim / 32 : 0);
+    return records(base, p.at[u] / SCALE_OF, p.bytes[u] / SCALE_OF);
   };
   uint32_t k[2][KL][KW / 4];
   uint32_t v[2][NH][4][(VW + 3) / 4];
@@ -476,7 +511,8 @@ __device__ __forceinline__ void attention_body(const AttentionArgs &a) {
           seg.b, seg.column, seg.first == 0 && !whole ? 2 * run + second : -1, seg.end - seg.last + seg.tiles - 1, tiles_each, tiles_more};
     }
     Pages pages_behind = look_up(behind, behind.first + way);
-    pages = look_up(seg, seg.first + way + WAYS);
+    Window window = look_ahead(seg, seg.first + way + WAYS), window_behind = look_ahead(seg, seg.first + way + 33 * WAYS);
+    int window_at = 32;
     f32x4 o[RT][NH * E];
     float m[RT], l[RT];
 #pragma unroll
@@ -498,9 +534,12 @@ __device__ __forceinline__ void attention_body(const AttentionArgs &a) {
       for (int t = 0; t < KS; ++t) asm volatile("" : "+v"(q[rt][t]));
     for (int tile = seg.first + way; tile < seg.last; tile += WAYS) {
       Place next;
-      if (tile + WAYS < seg.last) next = place(seg, tile + WAYS, pages);
+      if (window_at == 32) {
+        if (tile != seg.first + way) window = window_behind, window_behind = look_ahead(seg, tile + 33 * WAYS);
+        work_out(seg, window), window_at = 0;
+      }
+      if (tile + WAYS < seg.last) next = place_at(window, window_at++);
       else next = place(behind, behind.first + way, pages_behind);
-      pages = look_up(seg, tile + 2 * WAYS);
       f32x4 st[RT][2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -551,27 +590,41 @@ __device__ __forceinline__ void attention_body(const AttentionArgs &a) {
         const int t = t0 + 16 * (e / 4) + e % 4;
         return (t <= position[rt] && t >= low[rt]) || t < seg.prefix;
       };
+      const bool masked = !seen || here.count[0] + here.count[1] < ATT_TILE;
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        float m_new = m[rt], p[8];
+        float p[8];
+        if (RULED && a.rule.cap_out > 0.0f) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if constexpr (RULED) {
-            float x = st[rt][e / 4][e % 4] * a.scale_log2;
-            if (a.rule.cap_out > 0.0f) x = capped(st[rt][e / 4][e % 4], a.rule.cap_in, a.rule.cap_out);
-            if (a.rule.slopes) x -= slope[rt] * fabsf((float)(position[rt] - (t0 + 16 * (e / 4) + e % 4)));
-            p[e] = 4 * g + e % 4 < here.count[e / 4] && (seen || sees(rt, e)) ? x : -INFINITY;
-          } else {
-            p[e] = 4 * g + e % 4 < here.count[e / 4] ? st[rt][e / 4][e % 4] * a.scale_log2 : -INFINITY;
-          }
-          m_new = fmaxf(m_new, p[e]);
+          for (int e = 0; e < 8; ++e) p[e] = capped(st[rt][e / 4][e % 4], a.rule.cap_in, a.rule.cap_out);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[e] = st[rt][e / 4][e % 4] * a.scale_log2;
         }
-        m_new = over_column(m_new, [](float x, float y) { return fmaxf(x, y); });
+        if (RULED && a.rule.slopes) {
+          const float from = (float)(position[rt] - t0);          // (both below 2^24, or their distance rounded, as it would be)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[e] -= slope[rt] * fabsf(from - (float)(16 * (e / 4) + e % 4));
+        }
+        if (masked) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[e] = 4 * g + e % 4 < here.count[e / 4] && (!RULED || seen || sees(rt, e)) ? p[e] : -INFINITY;
+        }
+        float top = p[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, p[e]);
+        top = over_column(top, [](float x, float y) { return fmaxf(x, y); });
+        // The weights' base moves where they would pass 2^ATT_SLACK, so that most tiles leave O alone; m is that base, which the joins know as the maximum.
+        const bool moves = top > m[rt] + ATT_SLACK;
+        if (__any(moves)) {
+          const float m_new = moves ? top : m[rt], alpha = moves ? __builtin_amdgcn_exp2f(m[rt] - top) : 1.0f;
+          m[rt] = m_new;
+          l[rt] *= alpha;
+#pragma unroll
+          for (int i = 0; i < NH * E; ++i) o[rt][i] *= alpha;
+        }
         // (nothing but masked tokens so far: everything below is 0)
-        const float base = m_new == -INFINITY ? 0.0f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m[rt] - base);
-        m[rt] = m_new;
-        l[rt] *= alpha;
+        const float base = m[rt] == -INFINITY ? 0.0f : m[rt];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           p[e] = __builtin_amdgcn_exp2f(p[e] - base);
@@ -584,8 +637,6 @@ __device__ __forceinline__ void attention_body(const AttentionArgs &a) {
           const bf16x2 rest = {(__bf16)(p[2 * c] - __uint_as_float(lo & 0xFFFF0000u)), (__bf16)(p[2 * c + 1] - __uint_as_float(hi & 0xFFFF0000u))};
           pt_rest[rt][c] = __builtin_bit_cast(uint32_t, rest);
         }
-#pragma unroll
-        for (int i = 0; i < NH * E; ++i) o[rt][i] *= alpha;
       }
       auto widen_v = [&](int h, uint32_t (&w)[8][E / 2]) {            // 8 tokens, E values each
 #pragma unroll

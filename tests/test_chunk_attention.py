@@ -415,6 +415,37 @@ def test_chunk_attention(tq, heads, kv_heads, dim, page, fresh, lengths, fmt, la
         check(got, *want, few(heads, kv_heads, max(fresh)))
 
 
+def lengthened(tables, page, most):
+    """The same tables with room for more tokens, in pages of nobody: 2048 beyond half of `most`, from which on a workgroup takes 256 rows."""
+    more = -(-(2048 + most) // page)
+    return torch.cat([tables, torch.full((tables.shape[0], more), -1, dtype=torch.int32)], 1)
+
+
+LONG = [c for c in CHUNKS if c[0] // c[1] * max(c[4]) > 128 and c[2] <= 128] + [
+    (32, 8, 128, 16, [65, 500, 3], [65, 2800, 40], "bf16", "heads"), (16, 2, 128, 64, [100, 0, 70], [2200, 30, 71], "mxfp8", "heads"),
+    (16, 2, 96, 16, [99, 64], [400, 2222], "mxfp4", "tokens"), (4, 4, 64, 32, [257, 150], [1030, 2100], "mxfp8", "pairs"),
+    (4, 4, 64, 32, [256, 129], [256, 129], "mxfp4", "heads"), (6, 2, 88, 16, [70, 300], [70, 310], "bf16", "heads")]
+
+
+@gpu
+@pytest.mark.parametrize("rule", ["plain", "slopes", "window 1", "prefix", "first and last", "slopes and all"])
+@pytest.mark.parametrize("heads,kv_heads,dim,page,fresh,lengths,fmt,layout", LONG)
+def test_chunk_attention_behind_long_tables(tq, heads, kv_heads, dim, page, fresh, lengths, fmt, layout, rule):
+    B = len(lengths)
+    if rule == "slopes and all":
+        rule = Rule(slopes=slopes_of(heads), window=2000 + max(fresh), prefix=torch.full((B,), 33, dtype=torch.int32))
+    else:
+        rule = RULES[rule](heads, B)
+    for ones in (False, True):
+        cache, q, starts, tables, lens, pages = case(tq, fresh, lengths, heads, kv_heads, dim, page, fmt, layout, 11, spread=2.0, ones=ones, gap=3)
+        tables = lengthened(tables, page, max(fresh))
+        want = reference(q, starts, values_of(cache, "k"), values_of(cache, "v"), tables, lens, dim ** -0.5, pages, rule)
+        out = torch.full(q.shape, 7.0, dtype=BF, device=DEV)
+        tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, tables.to(DEV), lens.to(DEV), dim ** -0.5, most=max(fresh), scores=rule.on(tq), out=out)
+        assert bool((out[-3:] == 7.0).all())
+        check(out, *want, False)
+
+
 POISONED = [
     # heads, kv_heads, head_dim, page, new tokens, tokens, format
     (8, 2, 64, 16, [1, 1, 1], [40, 200, 33], "bf16"), (16, 1, 128, 16, [1, 1], [90, 150], "mxfp8"), (4, 4, 256, 16, [1, 1], [90, 150], "mxfp4"),
@@ -424,13 +455,16 @@ POISONED = [
 
 
 @gpu
-@pytest.mark.parametrize("rule", ["plain", "window 1", "window 50", "prefix", "first and last", "everything"])
+@pytest.mark.parametrize("long", [False, True])
+@pytest.mark.parametrize("rule", ["plain", "window 1", "window 50", "prefix", "first and last", "slopes", "everything"])
 @pytest.mark.parametrize("heads,kv_heads,dim,page,fresh,lengths,fmt", POISONED)
-def test_what_a_query_does_not_see_takes_no_part(tq, heads, kv_heads, dim, page, fresh, lengths, fmt, rule):
+def test_what_a_query_does_not_see_takes_no_part(tq, heads, kv_heads, dim, page, fresh, lengths, fmt, rule, long):
     """Tokens whose keys and values are not finite: rows that see them are not finite where those are, the others are as without."""
     B = len(lengths)
     rule = RULES[rule](heads, B)
     cache, q, starts, tables, lens, pages = case(tq, fresh, lengths, heads, kv_heads, dim, page, fmt, "heads", 5)
+    if long:
+        tables = lengthened(tables, page, max(fresh))
     g = rng(lengths, fresh, 9)
     for b, n in enumerate(lengths):                  # in some places of values, and in whole keys
         for t in sorted({0, n // 3, n // 2, n - 2, n - 1}):
