@@ -58,8 +58,9 @@ int rows_of(const torq_kv_cache_t &cache, int heads, int most, int width, const 
   const int64_t rows = (int64_t)most * (heads / cache.heads);
   if (cache.head_dim > 128 || rows <= 128) return cache.head_dim > 128 || rows > 64 ? 128 : 64;
   int64_t keys = (int64_t)width * cache.page_size;
-  if (scores && scores->window) keys = std::min<int64_t>(keys, (int64_t)scores->window + most);
-  return keys - most / 2 >= 2048 && (bend == BEND_NONE || bend == BEND_SLOPES) ? 256 : 128;
+  keys -= most / 2;
+  if (scores && scores->window) keys = std::min<int64_t>(keys, scores->window);
+  return keys >= 2048 && (bend == BEND_NONE || bend == BEND_SLOPES) ? 256 : 128;
 }
 ChunkPlan chunk_plan(const torq_kv_cache_t &cache, int heads, int64_t tokens, int most, int64_t B, int width, int rows) {
   ChunkPlan p;

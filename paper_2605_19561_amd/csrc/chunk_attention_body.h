@@ -438,6 +438,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
     constexpr int I = decltype(number)::value;
     static_for<NR>([&](auto x) { o.template add_product<decltype(x)::value, I % IB>(operand, pt[x][I / IB]); });
   };
+  // One after the other at every step, where weights among the products would take more registers than two waves of a SIMD have (widened values at their
+  // full width, and scores that are bent at 128).  Mixed / in turn, 8 requests of 1024 tokens, 32 and 8 heads, us: of 128 in MXFP8 230 / 182, capped 279 / 199, with
+  // slopes 271 / 191; in MXFP4 178 / 173, 242 / 198, 285 / 189; in bf16 162 / 170, 210 / 187, 233 / 187; of 256 in MXFP8 532 / 452, 638 / 500, in bf16 339 / 388, 432 /
+  // 470; of 96 in MXFP8 136 / 163, 154 / 180; of 64 108 / 139, 129 / 156.
+  constexpr bool IN_TURN = BEND == BEND_ANY || (RW == 4 && NR == 1 && DV >= 128 && DV == DP && (SCALED || (DP == 128 && BEND != BEND_NONE)));
   constexpr int PIECES = 13 * NR;                    // of each block of rows by turns
   float top[NR], base[NR], alpha[NR];
   bool moved[NR];
@@ -557,7 +562,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
           else product(x, pt[P ^ 1], std::integral_constant<int, I - KS>{});
         };
         bf16x8 x[PRODUCTS];
-        if (BEND == BEND_ANY || edge) {             // (few steps: one after the other)
+        if (IN_TURN || edge) {                      // (few steps: one after the other)
           static_for<PIECES>([&](auto i) { piece(std::true_type{}, i, key0, lost, st[P], pt[P]); });
           static_for<PRODUCTS>([&](auto i) {
             if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);         // (two operands at a time, for the registers)
