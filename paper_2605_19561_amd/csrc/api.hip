@@ -874,6 +874,8 @@ bool chunk_sizes(const torq_kv_cache_t *c, int heads, int64_t tokens, int most, 
   const int64_t keys = (int64_t)width * c->page_size, rows = (int64_t)(heads / c->heads) * most;
   if (keys > (int64_t)1 << 30) return false;
   const int64_t columns = (rows + 15) / 16, left = 0x7FFFFFFF / (keys / 32 + 8);
+  // (workgroups of 64 rows at least, which are one launch)
+  if (rows > 32 && tokens * heads / 64 + std::min(B, tokens) * c->heads > torq::most_workgroups(256)) return false;
   return columns <= left && (B == 0 || columns * c->heads <= left / B);
 }
 bool scores_fine(const torq_scores_t *s) { return !s || (s->window >= 0 && s->cap >= 0.0f && s->cap <= 1e30f); }
