@@ -4,10 +4,25 @@
 // 32 keys x 16 values, and beside them by the vector instructions of the softmax (a fused multiply-add, an exponential, a maximum and halves of a
 // conversion and a sum for each score, 3 of the 8 cycles that a score's products take at head_dim 128, and 4 for the exponential).
 //
-// Work: the (token, head) pairs of a request under one key head are rows, 128 of them a workgroup's, 32 a wave's; its keys come in tiles of 64.  A wave
-// brings 16 of a tile's keys (they lie in one page) into registers while the tile before is worked on, widens them to bf16 and puts them into LDS,
-// two tiles of it, for all four waves.  Few rows over many keys: the tiles of a row tile are cut into equal parts, one for each workgroup, whose O, m
-// and l a second kernel joins in the order of the keys.
+// Work: the (token, head) pairs of a request under one key head are rows, 64, 128 or 256 of them a workgroup's (which: chunk_attention.hip); its keys come
+// in steps of 32.  Four waves:
+//   256 rows   two blocks of 32 each: what a wave reads of K and V in LDS serves 64 rows.  LDS gives 128 bytes a clock, which with 32 rows a wave is the bound
+//              (reading alone 268 of the 403 us that the products of 8192 tokens, 32 heads of 128, take at the matrix cores' best)
+//   128 rows   one block each, two workgroups on a CU
+//   64 rows    two waves for each half of the keys, put together in LDS at the end: few rows and many keys
+// A step's keys lie in a ring of four slots in LDS: bf16 comes straight from memory, three (K) and two (V) steps ahead; MXFP8 and MXFP4 through registers,
+// loaded two steps before they are widened to bf16 into it.  Few workgroups over many keys: the steps of a row tile are cut into equal parts, one for each
+// workgroup, whose O, m and l a second kernel joins in the order of the keys.
+//
+// A wave works on three steps at a time: the scores of step j + 1, the weights of j, the products with V of j - 1, none of which waits for another; the
+// softmax's instructions stand between the products piece by piece, so that both pipes have work.  (One after the other where that takes too many
+// registers: IN_TURN.)  Steps in which every row sees every key know no masks; the others, at the ends of windows, prefixes and lengths, do.  There 0 times
+// a value that is not finite would be no 0: such values are left out, and at the end a second pass puts them back for the rows that see them, a case that
+// costs a second look at the keys and is rare.
+//
+// Measured: one prompt of 8192 tokens, 32 / 8 heads of 128, bf16, 597 us = 920 TFLOP/s (a large bf16 product reaches 1363); 512 tokens behind 60000 in MXFP4,
+// 64 / 8 heads, 1075 us = 940.  Without the products the steps take 481 us of the 597, without the weights 485: what bounds them is issuing both, some 290
+// instructions and 32 products a step, from one wave on a SIMD.  The first version, 128 rows, tiles of 64 and no pipeline: 799 and 1303.
 //
 // A tile goes through the matrix cores transposed, and nothing of it passes between lanes but maxima between two halves of a wave:
 //   S^T [key][row] = K [key][i] Q^T [i][row]            v_mfma_f32_32x32x16_bf16
@@ -622,6 +637,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
     }
   }
   o.settle();
+  // (what the last steps have set out for steps that are none arrives before LDS is another's, and before the workgroup gives it back)
+  if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (strange) {
     // What has been left out: an infinity or NaN for every row that sees its key, whatever the weight.

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2605_19561_amd import binding
-from tests.test_chunk_attention import BF, DEV, E8, Rule, case, check, either_way, few, lengthened, make_cache, reference, rng, slopes_of, tq, values_of   # noqa: F401
+from test_chunk_attention import BF, DEV, E8, Rule, case, check, either_way, few, lengthened, make_cache, reference, rng, slopes_of, tq, values_of   # noqa: F401
 
 gpu = pytest.mark.gpu
 i32 = lambda *n: torch.tensor(n, dtype=torch.int32)
@@ -251,6 +251,30 @@ def test_the_same_bits_on_any_stream_and_in_a_graph(tq, heads, kv_heads, dim, fr
         torch.cuda.synchronize()
         assert all(torch.equal(o, w) for o, w in zip(outs, fresh_want))
         (q.float() @ q.float().transpose(1, 2)).sum().item()
+
+
+@gpu
+@long
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("dim,kv_heads,fmt", [(64, 8, "bf16"), (96, 4, "bf16"), (128, 8, "bf16"), (256, 2, "bf16"), (128, 8, "mxfp8"), (128, 8, "mxfp4")])
+def test_many_ragged_prompts_give_the_same_bits_every_time(tq, dim, kv_heads, fmt, slopes, long):
+    """Workgroups that follow one another on a CU while the loads of the ones before may still be on their way."""
+    g = rng(dim, kv_heads, fmt, 37)
+    fresh = torch.randint(1, 500, (33,), generator=g).tolist()
+    cache, q, starts, tables, lens, pages = case(tq, fresh, fresh, 16 * kv_heads, kv_heads, dim, 16, fmt, "tokens", 38)
+    if long:
+        tables = lengthened(tables, 16, max(fresh))
+    rule = tq.Scores(slopes=slopes_of(16 * kv_heads).to(DEV)) if slopes else None
+    q, starts, tables, lens = q.to(DEV), starts.to(DEV), tables.to(DEV), lens.to(DEV)
+    run = lambda: tq.torq_chunk_attention(q, starts, cache, tables, lens, 0.1, most=max(fresh), scores=rule)
+    want = run()
+    for _ in range(40):
+        assert torch.equal(run(), want)
+    # a request alone, whose workgroups follow no other's
+    for b in (0, 17):
+        at = slice(int(starts[b]), int(starts[b + 1]))
+        alone = tq.torq_chunk_attention(q[at], starts[b:b + 2] - starts[b], cache, tables[b:b + 1], lens[b:b + 1], 0.1, most=max(fresh), scores=rule)
+        assert float((alone.float() - want[at].float()).abs().max()) <= 2.0 ** -6 * float(want[at].float().abs().max())
 
 
 @gpu
