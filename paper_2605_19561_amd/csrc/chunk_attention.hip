@@ -51,9 +51,10 @@ struct ChunkPlan {
 };
 // Rows of a workgroup: 256, two blocks of 32 for each wave, where a row sees 2048 keys and more as far as the tables and the window tell (a request's
 // first new token sees `most` fewer than its last), else 128, whose items are sooner done and begun, and which share a CU by twos; and for scores under a
-// cap, whose tangent takes more registers than two blocks leave.  256 / 128, 32 query and 8 key heads of 128, us: requests of 512 tokens, 1, 16, 34.3 /
-// 28.2, 136 / 111; 8 of 1024 173 / 151; 4 of 2048 222 / 217; 2 of 4096 346 / 353, in MXFP8 4 of them 775 / 1162; one of 8192 598 / 629; 64 tokens behind 2048, 32
-// requests, 110 / 120; 256 behind 8192 in MXFP4, 16 of them, 629 / 878; a window of 512, 4 of 4096, 334 / 252; a cap, 4 of 4096, 1176 / 1017.
+// cap, whose tangent takes more registers than two blocks leave.  256 / 128, 32 query and 8 key heads of 128, us: requests of 512 tokens, 1, 16, 34.1 /
+// 27.6, 136 / 111; 8 of 1024 174 / 150, in MXFP8 188 / 175; 4 of 2048 221 / 219, of heads of 64 164 / 150; 2 of 4096 347 / 359, in MXFP8 4 of them 773 / 878; one of
+// 8192 599 / 638; 64 tokens behind 2048, 32 requests, 117 / 125; 256 behind 8192 in MXFP4, 16 of them, 631 / 831; a window of 512, 4 of 4096, 334 / 252; a cap, 4 of
+// 4096, 1176 / 924.
 int rows_of(const torq_kv_cache_t &cache, int heads, int most, int width, const torq_scores_t *scores, int bend) {
   const int64_t rows = (int64_t)most * (heads / cache.heads);
   if (cache.head_dim > 128 || rows <= 128) return cache.head_dim > 128 || rows > 64 ? 128 : 64;
