@@ -38,11 +38,13 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a) {
 namespace {
 // So few rows of a request that they are columns of the single token's kernels
 bool few_rows(const torq_kv_cache_t &cache, int heads, int most) { return (int64_t)(heads / cache.heads) * most <= 32; }
-// What the kernel does to scores ahead of the weights: a cap whose error in the short form, 2^-23 of it, is below 2^-15 of a weight, or slopes; any
-// other rule, and a scale of 0 or nearly (0 times minus infinity is none: times it ahead of the maximum) by the kernel that looks.
+// A cap whose tangent may be taken in the short form, off by 2^-23 of the cap: below 2^-15 of a weight.
+bool short_cap(const torq_scores_t *scores) { return scores->cap <= 177.0f; }
+// What the kernel does to scores ahead of the weights: such a cap, or slopes; any other rule, and a scale of 0 or nearly (0 times minus infinity is
+// none: times it ahead of the maximum) by the kernel that looks.
 int bend_of(float scale, const torq_scores_t *scores) {
   const bool cap = scores && scores->cap > 0.0f, slopes = scores && scores->slopes;
-  if (cap) return slopes || scores->cap > 177.0f ? BEND_ANY : BEND_CAP;
+  if (cap) return slopes || !short_cap(scores) ? BEND_ANY : BEND_CAP;
   return slopes ? BEND_SLOPES : std::fabs(scale) < 2.0f * FLT_MIN ? BEND_ANY : BEND_NONE;
 }
 struct ChunkPlan {
@@ -100,9 +102,13 @@ hipError_t launch_chunk_attention(const torq_kv_cache_t &cache, const void *q, i
                                                    out, scores, starts, most, tokens);
   a.part = (float *)workspace, a.part_ml = a.part + plan.items * plan.splits * plan.rows * cache.head_dim;
   a.c = std::fabs(a.scale_log2), a.flip = a.scale_log2 < 0.0f;
-  a.any_cap = a.rule.cap_out > 0.0f;
-  if (a.any_cap) a.c = a.scale_log2 = a.rule.cap_out;
-  if (bend == BEND_CAP) a.c = 2.0f * a.rule.cap_out, a.rule.cap_in = std::max(-FLT_MAX, std::min(FLT_MAX, 2.88539008177792681472f * a.rule.cap_in));
+  a.any_cap = 0;
+  if (a.rule.cap_out > 0.0f) {
+    a.any_cap = short_cap(scores) ? CAP_SHORT : CAP_LONG, a.scale_log2 = a.rule.cap_out;
+    if (a.any_cap == CAP_SHORT)
+      a.scale_log2 = 2.0f * a.rule.cap_out, a.rule.cap_in = std::max(-FLT_MAX, std::min(FLT_MAX, 2.88539008177792681472f * a.rule.cap_in));
+    a.c = a.scale_log2;
+  }
   if (bend >= BEND_SLOPES) a.c = 1.0f;
   a.slots = (int)plan.slots, a.splits = plan.splits, a.tile_rows = plan.rows;
   const unsigned groups = (unsigned)(plan.items * plan.splits);

@@ -41,10 +41,11 @@ namespace torq {
 
 constexpr int CHUNK_STEP = 32;         // keys of a step
 constexpr int BEND_NONE = 0, BEND_CAP = 1, BEND_SLOPES = 2, BEND_ANY = 3;
+constexpr int CAP_SHORT = 1, CAP_LONG = 2;
 
 struct ChunkArgs : AttentionArgs {
   float c;                             // what (bent) scores are times in the exponent of 2
-  int any_cap;                         // (BEND_ANY) tanh of cap_in times the scores, ahead of scale_log2
+  int any_cap;                         // (BEND_ANY) which form of the tangent is taken ahead of scale_log2: -1 / (1 + exp2(cap_in s)), or that of every cap
   int flip;                            // q's signs (a scale below 0)
   int tile_rows;                       // rows of a workgroup
   int slots, splits;                   // row tiles of a key head at most; parts of the keys of one
@@ -466,12 +467,24 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
     const int x = number % NR, i = number / NR, from = key0 + 4 * h;
     f32x16 &st = scores[x];
     if (i < 4) {
+      if constexpr (BEND == BEND_ANY) {
+        // (four at a time: which way is the same for all)
+        if (a.any_cap == CAP_SHORT) {
+#pragma unroll
+          for (int r = 4 * i; r < 4 * i + 4; ++r) st[r] = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(st[r] * a.rule.cap_in)) * a.scale_log2;
+        } else if (a.any_cap == CAP_LONG) {
+#pragma unroll
+          for (int r = 4 * i; r < 4 * i + 4; ++r) st[r] = capped(st[r], a.rule.cap_in, 1.0f) * a.scale_log2;
+        } else {
+#pragma unroll
+          for (int r = 4 * i; r < 4 * i + 4; ++r) st[r] *= a.scale_log2;
+        }
+      }
 #pragma unroll
       for (int r = 4 * i; r < 4 * i + 4; ++r) {
         const int t = 8 * (r / 4) + r % 4;
         // (a row's scores are as good less a number of its own, so -1 / (1 + e^2y) does for tanh(y) / 2, to 2^-24)
         if constexpr (BEND == BEND_CAP) st[r] = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(st[r] * a.rule.cap_in));
-        if constexpr (BEND == BEND_ANY) st[r] = (a.any_cap ? capped(st[r], a.rule.cap_in, 1.0f) : st[r]) * a.scale_log2;
         if constexpr (BEND == BEND_SLOPES) st[r] = __builtin_fmaf(st[r], a.scale_log2, -slope[x] * fabsf((float)(position[x] - from) - (float)t));
         if constexpr (BEND == BEND_ANY) st[r] -= slope[x] * fabsf((float)(position[x] - from) - (float)t);
         if constexpr (EDGE) {
@@ -578,7 +591,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
         };
         bf16x8 x[PRODUCTS];
         if (IN_TURN || edge) {                      // (few steps: one after the other)
-          static_for<PIECES>([&](auto i) { piece(std::true_type{}, i, key0, lost, st[P], pt[P]); });
+          if (!IN_TURN || edge) static_for<PIECES>([&](auto i) { piece(std::true_type{}, i, key0, lost, st[P], pt[P]); });
+          else static_for<PIECES>([&](auto i) { piece(std::false_type{}, i, key0, lost, st[P], pt[P]); });
           static_for<PRODUCTS>([&](auto i) {
             if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);         // (two operands at a time, for the registers)
             multiply(operand(i), i);
