@@ -51,24 +51,14 @@ struct ChunkPlan {
   int64_t slots, items;
   int splits, rows;
 };
-// Rows of a workgroup: 256, two blocks of 32 for each wave, where a row sees 2048 keys and more as far as the tables and the window tell (a request's
-// first new token sees `most` fewer than its last), else 128, whose items are sooner done and begun, and which share a CU by twos; and for scores under a
-// cap, whose tangent takes more registers than two blocks leave.  256 / 128, 32 query and 8 key heads of 128, us: requests of 512 tokens, 1, 16, 34.1 /
-// 27.6, 136 / 111; 8 of 1024 174 / 150, in MXFP8 188 / 175; 4 of 2048 221 / 219, of heads of 64 164 / 150; 2 of 4096 347 / 359, in MXFP8 4 of them 773 / 878; one of
-// 8192 599 / 638; 64 tokens behind 2048, 32 requests, 117 / 125; 256 behind 8192 in MXFP4, 16 of them, 631 / 831; a window of 512, 4 of 4096, 334 / 252; a cap, 4 of
-// 4096, 1176 / 924.
-int rows_of(const torq_kv_cache_t &cache, int heads, int most, int width, const torq_scores_t *scores, int bend) {
-  const int64_t rows = (int64_t)most * (heads / cache.heads);
-  if (cache.head_dim > 128 || rows <= 128) return cache.head_dim > 128 || rows > 64 ? 128 : 64;
-  int64_t keys = (int64_t)width * cache.page_size;
-  keys -= most / 2;
-  if (scores && scores->window) keys = std::min<int64_t>(keys, scores->window);
-  return keys >= 2048 && (bend == BEND_NONE || bend == BEND_SLOPES) ? 256 : 128;
+// Rows of a workgroup: 64 where a request has no more, whose four waves then share the keys out.
+int rows_of(const torq_kv_cache_t &cache, int heads, int most) {
+  return cache.head_dim <= 128 && (int64_t)most * (heads / cache.heads) <= 64 ? 64 : 128;
 }
-ChunkPlan chunk_plan(const torq_kv_cache_t &cache, int heads, int64_t tokens, int most, int64_t B, int width, int rows) {
+ChunkPlan chunk_plan(const torq_kv_cache_t &cache, int heads, int64_t tokens, int most, int64_t B, int width) {
   ChunkPlan p;
   const int64_t each = heads / cache.heads;
-  p.rows = rows;
+  p.rows = rows_of(cache, heads, most);
   p.slots = std::min(tokens * each / p.rows + std::min(B, tokens), B * ((most * each + p.rows - 1) / p.rows));
   p.items = p.slots * cache.heads;
   const int64_t steps = ((int64_t)width * cache.page_size + CHUNK_STEP - 1) / CHUNK_STEP, full = cache.head_dim <= 128 && p.rows == 128 ? 512 : 256;
@@ -79,13 +69,8 @@ ChunkPlan chunk_plan(const torq_kv_cache_t &cache, int heads, int64_t tokens, in
 
 size_t chunk_attention_workspace_bytes(const torq_kv_cache_t &cache, int heads, int64_t tokens, int most, int64_t B, int width) {
   if (few_rows(cache, heads, most)) return paged_attention_workspace_bytes(cache, heads * most, B, width);
-  size_t bytes = 0;                                 // whatever the scores
-  const int plain = rows_of(cache, heads, most, width, nullptr, BEND_NONE);
-  for (const int rows : {plain, std::min(plain, 128)}) {
-    const ChunkPlan p = chunk_plan(cache, heads, tokens, most, B, width, rows);
-    if (p.splits > 1) bytes = std::max(bytes, (size_t)p.items * p.splits * p.rows * (cache.head_dim + 2) * sizeof(float));
-  }
-  return bytes;
+  const ChunkPlan p = chunk_plan(cache, heads, tokens, most, B, width);
+  return p.splits == 1 ? 0 : (size_t)p.items * p.splits * p.rows * (cache.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_chunk_attention(const torq_kv_cache_t &cache, const void *q, int64_t q_stride, int64_t q_head_stride, int heads, int64_t tokens,
@@ -96,7 +81,7 @@ hipError_t launch_chunk_attention(const torq_kv_cache_t &cache, const void *q, i
     return launch_paged_attention(cache, q, q_stride, q_head_stride, heads, block_tables, table_stride, width, lengths, B, scale, out, workspace,
                                   scores, starts, most, tokens, stream);
   const int bend = bend_of(scale, scores);
-  const ChunkPlan plan = chunk_plan(cache, heads, tokens, most, B, width, rows_of(cache, heads, most, width, scores, bend));
+  const ChunkPlan plan = chunk_plan(cache, heads, tokens, most, B, width);
   ChunkArgs a;
   static_cast<AttentionArgs &>(a) = attention_args(cache, q, q_stride, q_head_stride, heads, block_tables, table_stride, width, lengths, B, scale,
                                                    out, scores, starts, most, tokens);

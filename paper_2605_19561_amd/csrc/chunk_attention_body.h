@@ -4,25 +4,24 @@
 // 32 keys x 16 values, and beside them by the vector instructions of the softmax (a fused multiply-add, an exponential, a maximum and halves of a
 // conversion and a sum for each score, 3 of the 8 cycles that a score's products take at head_dim 128, and 4 for the exponential).
 //
-// Work: the (token, head) pairs of a request under one key head are rows, 64, 128 or 256 of them a workgroup's (which: chunk_attention.hip); its keys come
-// in steps of 32.  Four waves:
-//   256 rows   two blocks of 32 each: what a wave reads of K and V in LDS serves 64 rows.  LDS gives 128 bytes a clock, which with 32 rows a wave is the bound
-//              (reading alone 268 of the 403 us that the products of 8192 tokens, 32 heads of 128, take at the matrix cores' best)
-//   128 rows   one block each, two workgroups on a CU
-//   64 rows    two waves for each half of the keys, put together in LDS at the end: few rows and many keys
+// Work: the (token, head) pairs of a request under one key head are rows, 128 or 64 of them a workgroup's, 32 a wave's; its keys come in steps of 32. 128 rows:
+// four waves with the same keys, two workgroups on a CU where the registers allow it (up to 128 values). 64 rows: two waves for each half of the keys, put
+// together in LDS at the end: few rows and many keys.
+//
 // A step's keys lie in a ring of four slots in LDS: bf16 comes straight from memory, three (K) and two (V) steps ahead; MXFP8 and MXFP4 through registers,
 // loaded two steps before they are widened to bf16 into it.  Few workgroups over many keys: the steps of a row tile are cut into equal parts, one for each
 // workgroup, whose O, m and l a second kernel joins in the order of the keys.
 //
-// A wave works on three steps at a time: the scores of step j + 1, the weights of j, the products with V of j - 1, none of which waits for another; the
-// softmax's instructions stand between the products piece by piece, so that both pipes have work.  (One after the other where that takes too many
-// registers: IN_TURN.)  Steps in which every row sees every key know no masks; the others, at the ends of windows, prefixes and lengths, do.  There 0 times
-// a value that is not finite would be no 0: such values are left out, and at the end a second pass puts them back for the rows that see them, a case that
-// costs a second look at the keys and is rare.
+// A wave has three steps in hand at a time: the scores of step j + 1, the weights of j, the products with V of j - 1, none of which waits for another. With
+// two waves on a SIMD the softmax comes first and then the products, and one wave's instructions fill the other's gaps; a wave alone (64 rows) has its
+// softmax between its products piece by piece (IN_TURN, below).  Steps in which every row sees every key know no masks; the others, at the ends of windows,
+// prefixes and lengths, do.  There 0 times a value that is not finite would be no 0: such values are left out, and at the end a second pass puts
+// them back for the rows that see them, a case that costs a second look at the keys and is rare.
 //
-// Measured: one prompt of 8192 tokens, 32 / 8 heads of 128, bf16, 597 us = 920 TFLOP/s (a large bf16 product reaches 1363); 512 tokens behind 60000 in MXFP4,
-// 64 / 8 heads, 1075 us = 940.  Without the products the steps take 481 us of the 597, without the weights 485: what bounds them is issuing both, some 290
-// instructions and 32 products a step, from one wave on a SIMD.  The first version, 128 rows, tiles of 64 and no pipeline: 799 and 1303.
+// Measured: one prompt of 8192 tokens, 32 / 8 heads of 128, bf16, 600 us = 916 TFLOP/s (a large bf16 product reaches 1363); 512 tokens behind 60000 in MXFP4,
+// 64 / 8 heads, 1067 us = 946; 4 prompts of 4096 in MXFP8 687 us.  What bounds it is the issue of products and softmax together: LDS reads alone take 268 us of the
+// 600, the products at their best 403.  The first version, tiles of 64 keys and no steps in hand: 799 and 1303.  Not taken: 64 rows a wave, whose
+// O then fills the accumulators' half of the registers by name (less LDS traffic, one wave a SIMD): 624, 1076, 772.
 //
 // A tile goes through the matrix cores transposed, and nothing of it passes between lanes but maxima between two halves of a wave:
 //   S^T [key][row] = K [key][i] Q^T [i][row]            v_mfma_f32_32x32x16_bf16
@@ -114,136 +113,11 @@ __device__ __forceinline__ bool row_tile_of(const ChunkArgs &a, int slot, RowTil
   return false;
 }
 
-// O^T of a wave's NR blocks of 32 rows, IB pieces of 32 values each.  One block's lies in registers as the compiler takes them.  Two blocks' lie in the
-// accumulators' half from a128 on, by name: left to itself the compiler keeps copying O (or Q) between the halves, 230 moves a step and twice the time.
-// What it needs of that half itself it takes from a0 up (tests/test_chunk_isa.py looks that it never comes so far), and the waits between a product and what reads or writes O besides are kept here:
-// 8 passes and 11 cycles ahead, 4 behind.
-template <int NR, int IB>
-struct Sums {
-  f32x16 o[NR][IB];
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int x = 0; x < NR; ++x)
-#pragma unroll
-      for (int i = 0; i < IB; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[x][i][r] = 0.0f;
-  }
-  template <int X, int I>
-  __device__ __forceinline__ void add_product(bf16x8 a, u32x4 b) {
-    o[X][I] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, b), o[X][I], 0, 0, 0);
-  }
-  template <int X, int I>
-  __device__ __forceinline__ void scale(float by) {
-    o[X][I] *= by;
-  }
-  template <int X, int I, int R>
-  __device__ __forceinline__ float get() {
-    return o[X][I][R];
-  }
-  template <int X, int I, int R>
-  __device__ __forceinline__ void put(float v) {
-    o[X][I][R] = v;
-  }
-  __device__ __forceinline__ void settle() {}
-};
-#define TORQ_SUMS_CLOBBERED \
-  "a128", "a129", "a130", "a131", "a132", "a133", "a134", "a135", "a136", "a137", "a138", "a139", "a140", "a141", "a142", "a143", \
-  "a144", "a145", "a146", "a147", "a148", "a149", "a150", "a151", "a152", "a153", "a154", "a155", "a156", "a157", "a158", "a159", \
-  "a160", "a161", "a162", "a163", "a164", "a165", "a166", "a167", "a168", "a169", "a170", "a171", "a172", "a173", "a174", "a175", \
-  "a176", "a177", "a178", "a179", "a180", "a181", "a182", "a183", "a184", "a185", "a186", "a187", "a188", "a189", "a190", "a191", \
-  "a192", "a193", "a194", "a195", "a196", "a197", "a198", "a199", "a200", "a201", "a202", "a203", "a204", "a205", "a206", "a207", \
-  "a208", "a209", "a210", "a211", "a212", "a213", "a214", "a215", "a216", "a217", "a218", "a219", "a220", "a221", "a222", "a223", \
-  "a224", "a225", "a226", "a227", "a228", "a229", "a230", "a231", "a232", "a233", "a234", "a235", "a236", "a237", "a238", "a239", \
-  "a240", "a241", "a242", "a243", "a244", "a245", "a246", "a247", "a248", "a249", "a250", "a251", "a252", "a253", "a254", "a255"
-template <int IB>
-struct Sums<2, IB> {
-  template <int X, int I>
-  static constexpr int at = 128 + 16 * (X * IB + I);
-  __device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
-  __device__ __forceinline__ void zero() {
-    static_for<32 * IB>([](auto r) { asm volatile("v_accvgpr_write_b32 a[%0], 0" ::"n"(128 + decltype(r)::value) : TORQ_SUMS_CLOBBERED); });
-    settle();
-  }
-  template <int X, int I>
-  __device__ __forceinline__ void add_product(bf16x8 a, u32x4 b) {
-    asm volatile("v_mfma_f32_32x32x16_bf16 a[%2:%2+15], %0, %1, a[%2:%2+15]" ::"v"(a), "v"(b), "n"(at<X, I>) : TORQ_SUMS_CLOBBERED);
-  }
-  template <int X, int I>
-  __device__ __forceinline__ void scale(float by) {
-    float t[16];
-    asm volatile(
-      "v_accvgpr_read_b32 %0, a[%17+0]\n\t"
-      "v_accvgpr_read_b32 %1, a[%17+1]\n\t"
-      "v_accvgpr_read_b32 %2, a[%17+2]\n\t"
-      "v_accvgpr_read_b32 %3, a[%17+3]\n\t"
-      "v_accvgpr_read_b32 %4, a[%17+4]\n\t"
-      "v_accvgpr_read_b32 %5, a[%17+5]\n\t"
-      "v_accvgpr_read_b32 %6, a[%17+6]\n\t"
-      "v_accvgpr_read_b32 %7, a[%17+7]\n\t"
-      "v_accvgpr_read_b32 %8, a[%17+8]\n\t"
-      "v_accvgpr_read_b32 %9, a[%17+9]\n\t"
-      "v_accvgpr_read_b32 %10, a[%17+10]\n\t"
-      "v_accvgpr_read_b32 %11, a[%17+11]\n\t"
-      "v_accvgpr_read_b32 %12, a[%17+12]\n\t"
-      "v_accvgpr_read_b32 %13, a[%17+13]\n\t"
-      "v_accvgpr_read_b32 %14, a[%17+14]\n\t"
-      "v_accvgpr_read_b32 %15, a[%17+15]\n\t"
-      "v_mul_f32 %0, %0, %16\n\t"
-      "v_mul_f32 %1, %1, %16\n\t"
-      "v_mul_f32 %2, %2, %16\n\t"
-      "v_mul_f32 %3, %3, %16\n\t"
-      "v_mul_f32 %4, %4, %16\n\t"
-      "v_mul_f32 %5, %5, %16\n\t"
-      "v_mul_f32 %6, %6, %16\n\t"
-      "v_mul_f32 %7, %7, %16\n\t"
-      "v_mul_f32 %8, %8, %16\n\t"
-      "v_mul_f32 %9, %9, %16\n\t"
-      "v_mul_f32 %10, %10, %16\n\t"
-      "v_mul_f32 %11, %11, %16\n\t"
-      "v_mul_f32 %12, %12, %16\n\t"
-      "v_mul_f32 %13, %13, %16\n\t"
-      "v_mul_f32 %14, %14, %16\n\t"
-      "v_mul_f32 %15, %15, %16\n\t"
-      "v_accvgpr_write_b32 a[%17+0], %0\n\t"
-      "v_accvgpr_write_b32 a[%17+1], %1\n\t"
-      "v_accvgpr_write_b32 a[%17+2], %2\n\t"
-      "v_accvgpr_write_b32 a[%17+3], %3\n\t"
-      "v_accvgpr_write_b32 a[%17+4], %4\n\t"
-      "v_accvgpr_write_b32 a[%17+5], %5\n\t"
-      "v_accvgpr_write_b32 a[%17+6], %6\n\t"
-      "v_accvgpr_write_b32 a[%17+7], %7\n\t"
-      "v_accvgpr_write_b32 a[%17+8], %8\n\t"
-      "v_accvgpr_write_b32 a[%17+9], %9\n\t"
-      "v_accvgpr_write_b32 a[%17+10], %10\n\t"
-      "v_accvgpr_write_b32 a[%17+11], %11\n\t"
-      "v_accvgpr_write_b32 a[%17+12], %12\n\t"
-      "v_accvgpr_write_b32 a[%17+13], %13\n\t"
-      "v_accvgpr_write_b32 a[%17+14], %14\n\t"
-      "v_accvgpr_write_b32 a[%17+15], %15\n\t"
-      "s_nop 4"
-      : "=&v"(t[0]), "=&v"(t[1]), "=&v"(t[2]), "=&v"(t[3]), "=&v"(t[4]), "=&v"(t[5]), "=&v"(t[6]), "=&v"(t[7]), "=&v"(t[8]), "=&v"(t[9]), "=&v"(t[10]), "=&v"(t[11]), "=&v"(t[12]), "=&v"(t[13]), "=&v"(t[14]), "=&v"(t[15])
-      : "v"(by), "n"(at<X, I>)
-      : TORQ_SUMS_CLOBBERED);
-  }
-  template <int X, int I, int R>
-  __device__ __forceinline__ float get() {
-    float v;
-    asm volatile("v_accvgpr_read_b32 %0, a[%1]" : "=v"(v) : "n"(at<X, I> + R));
-    return v;
-  }
-  template <int X, int I, int R>
-  __device__ __forceinline__ void put(float v) {
-    asm volatile("v_accvgpr_write_b32 a[%1], %0" ::"v"(v), "n"(at<X, I> + R) : TORQ_SUMS_CLOBBERED);
-  }
-};
-#undef TORQ_SUMS_CLOBBERED
-
-// DP: values of a row in LDS, of which the first DV are multiplied.  RW: waves that share keys, each with NR blocks of 32 rows of its own; the other
+// DP: values of a row in LDS, of which the first DV are multiplied.  RW: waves that share keys, each with 32 rows of its own; the other
 // 4 / RW - 1 such groups have the same rows and other keys.
 // BEND: what is done to scores ahead of the weights; ANY looks what, and takes all steps one instruction after the other.
-template <int DP, int DV, int FMT, int BEND, int RW, int NR>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1 || DP * (4 / RW) > 128 ? 1 : 2, NR > 1 || DP * (4 / RW) > 128 ? 1 : 2))) chunk_attention_kernel(ChunkArgs a) {
+template <int DP, int DV, int FMT, int BEND, int RW>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP * (4 / RW) > 128 ? 1 : 2, DP * (4 / RW) > 128 ? 1 : 2))) chunk_attention_kernel(ChunkArgs a) {
   constexpr bool SCALED = FMT != FMT_BF16;
   constexpr int BITS = FMT == FMT_BF16 ? 16 : FMT == FMT_MXFP8 ? 8 : 4;
   constexpr int KP = 4 / RW, WK = CHUNK_STEP / RW;              // groups of waves with keys of their own; keys that a wave brings
@@ -256,7 +130,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
   typedef KLayout<DP> K;
   constexpr int SETS = 2;                                       // steps whose loads are on their way in registers
   static_assert(W >= 4 && 64 % PER == 0 && (64 / PER <= 16) && WK <= 16);
-  constexpr int SLOTS = 4, ROWS = 32 * NR * RW, PITCH = 9, RING = KP * SLOTS * (K::BYTES + SIDE), JOIN = KP * ROWS * (PITCH * 16 + 8);
+  constexpr int SLOTS = 4, ROWS = 32 * RW, PITCH = 9, RING = KP * SLOTS * (K::BYTES + SIDE), JOIN = KP * ROWS * (PITCH * 16 + 8);
   __shared__ __attribute__((aligned(1024))) char lds[RING > JOIN ? RING : JOIN];     // [keys' group][K, V][step by turns]; then what is put together
   __shared__ int strange;                                       // a value that is not finite has been left out
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
@@ -288,25 +162,20 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
     return step >= end ? length : (step < prefix_steps ? step : step + skip) * CHUNK_STEP;
   };
 
-  // this lane's rows
-  const bool wave_in = row0 + rp * NR * 32 < rows;
-  int position[NR], low[NR], span[NR];              // the keys that a window holds: span of them from low on
-  float slope[NR];
-  bf16x8 q[NR][KS];
+  // this lane's row
+  const bool wave_in = row0 + rp * 32 < rows;
+  const int row = row0 + rp * 32 + n, token = row / each, head = kv_head * each + row - token * each;
+  const bool in = row < rows;
+  const int position = first + token, low = low_of(position), span = max(min(position + 1, length) - low, 0);     // it sees the window's `span` keys from low on
+  const float slope = BEND >= BEND_SLOPES && a.rule.slopes && in ? 1.44269504088896340736f * a.rule.slopes[head] : 0.0f;
+  bf16x8 q[KS];
 #pragma unroll
-  for (int x = 0; x < NR; ++x) {
-    const int row = row0 + (rp * NR + x) * 32 + n, token = row / each, head = kv_head * each + row - token * each;
-    const bool in = row < rows;
-    position[x] = first + token, low[x] = low_of(position[x]), span[x] = max(min(position[x] + 1, length) - low[x], 0);
-    slope[x] = BEND >= BEND_SLOPES && a.rule.slopes && in ? 1.44269504088896340736f * a.rule.slopes[head] : 0.0f;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int i = 16 * s + 8 * h;
-      u32x4 v = {0, 0, 0, 0};
-      if (in && i < a.dim) v = *reinterpret_cast<const u32x4 *>(a.q + (int64_t)(q_at + token) * a.q_stride + (int64_t)head * a.q_head_stride + i);
-      if (BEND == BEND_NONE && a.flip) v ^= 0x80008000u;
-      q[x][s] = as_bf16(v);
-    }
+  for (int s = 0; s < KS; ++s) {
+    const int i = 16 * s + 8 * h;
+    u32x4 v = {0, 0, 0, 0};
+    if (in && i < a.dim) v = *reinterpret_cast<const u32x4 *>(a.q + (int64_t)(q_at + token) * a.q_stride + (int64_t)head * a.q_head_stride + i);
+    if (BEND == BEND_NONE && a.flip) v ^= 0x80008000u;
+    q[s] = as_bf16(v);
   }
 
   // Where the keys lie.  A lane looks up one of the 64 groups of 16 keys of 32 steps from w on, two windows ahead of their use: its page, then its place in
@@ -416,11 +285,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
       }
   };
 
-  Sums<NR, IB> o;
-  o.zero();
-  float m[NR], l[NR];                               // m in the exponent of 2
+  f32x16 o[IB];                                     // O^T, 32 values each
 #pragma unroll
-  for (int x = 0; x < NR; ++x) m[x] = -INFINITY, l[x] = 0.0f;
+  for (int i = 0; i < IB; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
+  float m = -INFINITY, l = 0.0f;                    // m in the exponent of 2
   const float c = a.c;
   // this lane's pieces of its key
   int k_base[2] = {K::at(n, h), K::at(n, h + (DP < 256 ? 2 : 0))};
@@ -441,31 +311,27 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + 8 * DP * 2));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  auto score = [&](f32x16 (&st)[NR], bf16x8 operand, int s) {
+  auto score = [&](f32x16 &st, bf16x8 operand, int s) {
+    if (s == 0)
 #pragma unroll
-    for (int x = 0; x < NR; ++x) {
-      if (s == 0)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) st[x][r] = 0.0f;
-      st[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand, q[x][s], st[x], 0, 0, 0);
-    }
+      for (int r = 0; r < 16; ++r) st[r] = 0.0f;
+    st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand, q[s], st, 0, 0, 0);
   };
-  auto product = [&](bf16x8 operand, const u32x4 (&pt)[NR][2], auto number) {
+  auto product = [&](bf16x8 operand, const u32x4 (&pt)[2], auto number) {
     constexpr int I = decltype(number)::value;
-    static_for<NR>([&](auto x) { o.template add_product<decltype(x)::value, I % IB>(operand, pt[x][I / IB]); });
+    o[I % IB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand, as_bf16(pt[I / IB]), o[I % IB], 0, 0, 0);
   };
-  // One after the other at every step, where weights among the products would take more registers than two waves of a SIMD have (widened values at their
-  // full width, and scores that are bent at 128).  Mixed / in turn, 8 requests of 1024 tokens, 32 and 8 heads, us: of 128 in MXFP8 230 / 182, capped 279 / 199, with
-  // slopes 271 / 191; in MXFP4 178 / 173, 242 / 198, 285 / 189; in bf16 162 / 170, 210 / 187, 233 / 187; of 256 in MXFP8 532 / 452, 638 / 500, in bf16 339 / 388, 432 /
-  // 470; of 96 in MXFP8 136 / 163, 154 / 180; of 64 108 / 139, 129 / 156.
-  constexpr bool IN_TURN = BEND == BEND_ANY || (RW == 4 && NR == 1 && DV >= 128 && DV == DP && (SCALED || (DP == 128 && BEND != BEND_NONE)));
-  constexpr int PIECES = 13 * NR;                    // of each block of rows by turns
-  float top[NR], base[NR], alpha[NR];
-  bool moved[NR];
-  auto piece = [&](auto at_edge, int number, int key0, int lost, f32x16 (&scores)[NR], u32x4 (&weights)[NR][2]) {
+  // One after the other at every step where the workgroup's waves have 32 rows of their own: two waves a SIMD fill one another's gaps, and weights among the
+  // products take registers that two of them do not have (or gain nothing).  Mixed / in turn, 8 requests of 1024 tokens, 32 and 8 heads, us: of 128 in bf16
+  // 152 / 143, MXFP8 230 / 153, capped 279 / 176, with slopes 271 / 171; of 256 in MXFP8 532 / 402; of 96 in bf16 120 / 118, of 64 100 / 100, of 192 282 / 287.  Not with one
+  // wave a SIMD: 32 requests of 5 tokens in MXFP4 139 / 182.
+  constexpr bool IN_TURN = BEND == BEND_ANY || RW == 4;
+  constexpr int PIECES = 13;
+  float top, base, alpha;
+  bool moved = false;
+  auto piece = [&](auto at_edge, int number, int key0, int lost, f32x16 &st, u32x4 (&weights)[2]) {
     constexpr bool EDGE = decltype(at_edge)::value;
-    const int x = number % NR, i = number / NR, from = key0 + 4 * h;
-    f32x16 &st = scores[x];
+    const int i = number, from = key0 + 4 * h;
     if (i < 4) {
       if constexpr (BEND == BEND_ANY) {
         // (four at a time: which way is the same for all)
@@ -485,35 +351,35 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
         const int t = 8 * (r / 4) + r % 4;
         // (a row's scores are as good less a number of its own, so -1 / (1 + e^2y) does for tanh(y) / 2, to 2^-24)
         if constexpr (BEND == BEND_CAP) st[r] = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(st[r] * a.rule.cap_in));
-        if constexpr (BEND == BEND_SLOPES) st[r] = __builtin_fmaf(st[r], a.scale_log2, -slope[x] * fabsf((float)(position[x] - from) - (float)t));
-        if constexpr (BEND == BEND_ANY) st[r] -= slope[x] * fabsf((float)(position[x] - from) - (float)t);
+        if constexpr (BEND == BEND_SLOPES) st[r] = __builtin_fmaf(st[r], a.scale_log2, -slope * fabsf((float)(position - from) - (float)t));
+        if constexpr (BEND == BEND_ANY) st[r] -= slope * fabsf((float)(position - from) - (float)t);
         if constexpr (EDGE) {
-          const bool seen = ((uint32_t)(from - low[x] + t) < (uint32_t)span[x]) | (from - prefix + t < 0);
+          const bool seen = ((uint32_t)(from - low + t) < (uint32_t)span) | (from - prefix + t < 0);
           st[r] = (seen & !(lost >> (r / 8) & 1)) ? st[r] : -INFINITY;
         }
-        top[x] = r ? fmaxf(top[x], st[r]) : st[r];
+        top = r ? fmaxf(top, st[r]) : st[r];
       }
     } else if (i == 4) {
-      const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[x]), __float_as_uint(top[x]), false, false);
+      const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
       const float most = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1])) * c;
-      moved[x] = most - m[x] > 8.0f;
-      const float now = moved[x] ? most : m[x];
-      alpha[x] = moved[x] ? __builtin_amdgcn_exp2f(m[x] - now) : 1.0f;
-      m[x] = now, base[x] = now == -INFINITY ? 0.0f : now;
-      l[x] *= alpha[x];
+      moved = most - m > 8.0f;
+      const float now = moved ? most : m;
+      alpha = moved ? __builtin_amdgcn_exp2f(m - now) : 1.0f;
+      m = now, base = now == -INFINITY ? 0.0f : now;
+      l *= alpha;
     } else {
       const int r = 2 * (i - 5);
-      const bf16x2 pair = {(__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[r], c, -base[x])),
-                           (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[r + 1], c, -base[x]))};
-      l[x] = __builtin_amdgcn_fdot2_f32_bf16(pair, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l[x], false);
-      weights[x][r / 8][r % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
+      const bf16x2 pair = {(__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[r], c, -base)),
+                           (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(st[r + 1], c, -base))};
+      l = __builtin_amdgcn_fdot2_f32_bf16(pair, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l, false);
+      weights[r / 8][r % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
     }
   };
   // Step j: the scores of step j + 1, the weights of j and the products of j - 1, none of which needs another.  Meanwhile what later steps need is on its
   // way into LDS, step x into slot x % SLOTS: straight from memory K of j + 3 and V of j + 2, or through registers K of j + 2 and V of j, with the loads for
   // SETS steps later.
-  f32x16 st[2][NR];
-  u32x4 pt[2][NR][2];
+  f32x16 st[2];
+  u32x4 pt[2][2];
   if (tid == 0) strange = 0;
   if (count > 0) {
     constexpr int FAR = DIRECT ? 3 : 4;             // of the steps ahead, the one whose K sets out
@@ -610,12 +476,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
           });
           __builtin_amdgcn_sched_barrier(0);
         }
-        bool any = false;
+        if (__any(moved)) {
 #pragma unroll
-        for (int x = 0; x < NR; ++x) any |= moved[x];
-        if (__any(any)) {
-          o.settle();
-          static_for<NR>([&](auto x) { static_for<IB>([&](auto i) { o.template scale<decltype(x)::value, decltype(i)::value>(alpha[x]); }); });
+          for (int i = 0; i < IB; ++i) o[i] *= alpha;
         }
       }
       // (the loads of this step stay on their way)
@@ -650,7 +513,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
       finish(std::integral_constant<int, 0>{});
     }
   }
-  o.settle();
   // (what the last steps have set out for steps that are none arrives before LDS is another's, and before the workgroup gives it back)
   if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -688,30 +550,22 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
               y[0] = wide[0], y[1] = wide[1];
             }
           }
-          static_for<NR>([&](auto block) {
-            constexpr int X = decltype(block)::value;
-            const bool seen = (((uint32_t)(key - low[X]) < (uint32_t)span[X]) | (key < prefix)) & (m[X] != -INFINITY);
-            static_for<4>([&](auto z) {
-              constexpr int Z = decltype(z)::value;
-              const float value = bf16_bits_to_f32(y[Z / 2] >> 16 * (Z % 2) & 0xFFFFu);
-              const bool add = seen && !(fabsf(value) < INFINITY);
-              if (__any(add)) o.template put<X, I, R + Z>(o.template get<X, I, R + Z>() + (add ? value : 0.0f));
-            });
+          const bool seen = (((uint32_t)(key - low) < (uint32_t)span) | (key < prefix)) & (m != -INFINITY);
+          static_for<4>([&](auto z) {
+            constexpr int Z = decltype(z)::value;
+            const float value = bf16_bits_to_f32(y[Z / 2] >> 16 * (Z % 2) & 0xFFFFu);
+            o[I][R + Z] += seen && !(fabsf(value) < INFINITY) ? value : 0.0f;
           });
         });
       }
     }
-    o.settle();
   }
   // (looked at anew from here on: what hangs on the row is not kept through the loop)
   int late = lane;
   asm volatile("" : "+v"(late));
   const int n_late = late & 31, h_late = late >> 5;
-#pragma unroll
-  for (int x = 0; x < NR; ++x) {
-    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[x]), __float_as_uint(l[x]), false, false);
-    l[x] = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
-  }
+  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
   const int64_t part = (((int64_t)slot * a.kv_heads + kv_head) * a.splits + split) * a.tile_rows;
   // four values of a row of the workgroup's
   auto store = [&](int row, int i, f32x4 x, float top, float sum) {
@@ -727,17 +581,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
   // the groups' put together, 32 values of every row at a time
   f32x4 *const mine = reinterpret_cast<f32x4 *>(lds);
   float *const ml = reinterpret_cast<float *>(mine + KP * ROWS * PITCH);
-  const int mine_at = kp * ROWS + rp * NR * 32 + n_late;
-#pragma unroll
-  for (int x = 0; x < NR; ++x)
-    if (h_late == 0) ml[2 * (mine_at + 32 * x)] = m[x], ml[2 * (mine_at + 32 * x) + 1] = l[x];
+  const int mine_at = kp * ROWS + rp * 32 + n_late;
+  if (h_late == 0) ml[2 * mine_at] = m, ml[2 * mine_at + 1] = l;
   static_for<IB>([&](auto piece_number) {
     constexpr int i = decltype(piece_number)::value;
-    static_for<NR * 4>([&](auto number) {
-      constexpr int X = decltype(number)::value / 4, R = decltype(number)::value % 4 * 4;
-      mine[(mine_at + 32 * X) * PITCH + R / 2 + h_late] =
-          f32x4{o.template get<X, i, R>(), o.template get<X, i, R + 1>(), o.template get<X, i, R + 2>(), o.template get<X, i, R + 3>()};
-    });
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) mine[mine_at * PITCH + r / 2 + h_late] = f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
     __syncthreads();
     for (int x = tid; x < ROWS * 8; x += 256) {
       const int row = x / 8, piece = x % 8;
@@ -758,23 +607,16 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR > 1
   });
 }
 
-// Kernels of one width, by the rows of a workgroup: 256, 128 or 64.
+// Kernels of one width, by the rows of a workgroup: 128 or 64.
 template <int DP, int DV>
 void go_chunk(const ChunkArgs &a, int format, int bend, unsigned groups, hipStream_t stream) {
-  auto of_rows = [&](auto of, auto with, auto waves, auto blocks) {
-    hipLaunchKernelGGL((chunk_attention_kernel<DP, DV, decltype(of)::value, decltype(with)::value, decltype(waves)::value, decltype(blocks)::value>), dim3(groups),
-                       dim3(256), 0, stream, a);
+  auto of_rows = [&](auto of, auto with, auto waves) {
+    hipLaunchKernelGGL((chunk_attention_kernel<DP, DV, decltype(of)::value, decltype(with)::value, decltype(waves)::value>), dim3(groups), dim3(256), 0, stream, a);
   };
   auto of_scores = [&](auto of, auto with) {
-    constexpr std::integral_constant<int, 1> one{};
-    constexpr std::integral_constant<int, 2> two{};
-    constexpr std::integral_constant<int, 4> four{};
-    if constexpr (DP < 256) {
-      if (a.tile_rows == 64) return of_rows(of, with, two, one);
-      if constexpr (decltype(with)::value == BEND_NONE || decltype(with)::value == BEND_SLOPES)
-        if (a.tile_rows == 256) return of_rows(of, with, four, two);
-    }
-    of_rows(of, with, four, one);
+    if constexpr (DP < 256)
+      if (a.tile_rows == 64) return of_rows(of, with, std::integral_constant<int, 2>{});
+    of_rows(of, with, std::integral_constant<int, 4>{});
   };
   auto of_format = [&](auto of) {
     if (bend == BEND_NONE) of_scores(of, std::integral_constant<int, BEND_NONE>{});

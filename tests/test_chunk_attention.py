@@ -416,7 +416,7 @@ def test_chunk_attention(tq, heads, kv_heads, dim, page, fresh, lengths, fmt, la
 
 
 def lengthened(tables, page, most):
-    """The same tables with room for more tokens, in pages of nobody: 2048 beyond half of `most`, from which on a workgroup takes 256 rows."""
+    """The same tables with room for many more tokens, in pages of nobody: what is chosen by the tables' width is chosen otherwise."""
     more = -(-(2048 + most) // page)
     return torch.cat([tables, torch.full((tables.shape[0], more), -1, dtype=torch.int32)], 1)
 
