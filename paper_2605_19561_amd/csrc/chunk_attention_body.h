@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP * (
           else product(x, pt[P ^ 1], std::integral_constant<int, I - KS>{});
         };
         bf16x8 x[PRODUCTS];
-        if (IN_TURN || edge) {                      // (few steps: one after the other)
+        if (IN_TURN || edge) {                      // one after the other (edges are few)
           if (!IN_TURN || edge) static_for<PIECES>([&](auto i) { piece(std::true_type{}, i, key0, lost, st[P], pt[P]); });
           else static_for<PIECES>([&](auto i) { piece(std::false_type{}, i, key0, lost, st[P], pt[P]); });
           static_for<PRODUCTS>([&](auto i) {
