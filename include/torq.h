@@ -364,8 +364,9 @@ int torq_paged_attention_scores(const torq_kv_cache_t *cache, const void *q_bf16
  *                 as they were in out
  *   most          new tokens of a request at most, at least 1; of a request with more the first `most` are computed, the others' rows left
  *   block_tables, lengths, width, out_bf16 ([tokens][heads][head_dim], contiguous), scale: as above, lengths[b] the tokens after the step;
- *                 B * cache->heads * ceil(heads * most / cache->heads / 16) * (width * page_size / 32 + 8) below 2^31, and tokens * heads below 2^31;
- *                 where heads * most / cache->heads passes 32, tokens * heads / 64 + min(B, tokens) * cache->heads below 2^24
+ *                 width * page_size and B at most 2^30, tokens * heads below 2^31, heads * most / cache->heads (a request's rows) below 2^32; where a
+ *                 request has up to 32 rows, B * cache->heads * ceil(rows / 16) * (width * page_size / 32 + 8) below 2^31, else
+ *                 tokens * heads / 64 + min(B, tokens) * cache->heads below 2^24
  *   workspace     16-byte aligned, torq_chunk_attention_workspace_bytes() of the same sizes; contents do not matter
  * Products of bf16 values with fp32 sums, statistics in fp32.  Where few rows (heads * most / cache->heads up to 32) see the keys the weights are
  * two bf16 parts as above, else one, rounded to nearest, whose sum they are divided by.  The same inputs give the same bits. */

@@ -867,16 +867,17 @@ bool attention_sizes(const torq_kv_cache_t *c, int heads, int64_t B, int width) 
   return most <= (int64_t)1 << 30 && columns <= 0x7FFFFFFF / (most / 32 + 8);
 }
 
-// the same for `tokens` new tokens, up to `most` of a request, whose heads are then the query heads
+// `tokens` new tokens, up to `most` of a request.  Up to 32 rows under a key head are the columns of the single token's kernels, whose numbers of tiles
+// they then are.  More of them: workgroups of 64 rows at least, which are one launch and know keys by request and step; requests are counted 512
+// at a time.
 bool chunk_sizes(const torq_kv_cache_t *c, int heads, int64_t tokens, int most, int64_t B, int width) {
   if (heads <= 0 || heads % c->heads || heads > (1 << 20) || tokens < 0 || tokens > 0x7FFFFFFF / heads || most <= 0 || B < 0 || width < 0) return false;
-  if (B > 0x7FFFFFFF) return false;
+  if (B > (int64_t)1 << 30) return false;
   const int64_t keys = (int64_t)width * c->page_size, rows = (int64_t)(heads / c->heads) * most;
-  if (keys > (int64_t)1 << 30) return false;
-  const int64_t columns = (rows + 15) / 16, left = 0x7FFFFFFF / (keys / 32 + 8);
-  // (workgroups of 64 rows at least, which are one launch)
-  if (rows > 32 && tokens * heads / 64 + std::min(B, tokens) * c->heads > torq::most_workgroups(256)) return false;
-  return columns <= left && (B == 0 || columns * c->heads <= left / B);
+  if (keys > (int64_t)1 << 30 || rows > 0xFFFFFFFF) return false;
+  if (rows > 32) return tokens * heads / 64 + std::min(B, tokens) * c->heads <= torq::most_workgroups(256);
+  const int64_t columns = (rows + 15) / 16 * c->heads, left = 0x7FFFFFFF / (keys / 32 + 8);
+  return B == 0 || columns <= left / B;
 }
 bool scores_fine(const torq_scores_t *s) { return !s || (s->window >= 0 && s->cap >= 0.0f && s->cap <= 1e30f); }
 bool scores_misaligned(const torq_scores_t *s) { return s && (misaligned_to(s->slopes, 4) || misaligned_to(s->prefix, 4)); }

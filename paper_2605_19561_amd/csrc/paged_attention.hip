@@ -588,7 +588,7 @@ AttentionArgs attention_args(const torq_kv_cache_t &cache, const void *q, int64_
   a.pages = (int)cache.pages, a.page_size = cache.page_size, a.page16_magic = ((int64_t)1 << 38) / (cache.page_size / 16) + 1;
   a.q = (const uint16_t *)q, a.q_stride = q_stride, a.q_head_stride = q_head_stride, a.out = (uint16_t *)out;
   a.tables = block_tables, a.lengths = lengths, a.table_stride = table_stride, a.most = (int64_t)width * cache.page_size;
-  a.B = (int)B, a.kv_heads = cache.heads, a.group = each * most, a.dim = cache.head_dim, a.scale_log2 = scale * log2e;
+  a.B = (int)B, a.kv_heads = cache.heads, a.group = (int)std::min<int64_t>((int64_t)each * most, 0x7FFFFFFF), a.dim = cache.head_dim, a.scale_log2 = scale * log2e;
   a.rule = ScoreArgs{0.0f, 0.0f, rule.slopes, rule.prefix, starts, rule.window, most, each, tokens};
   if (rule.cap > 0.0f) a.rule.cap_in = std::max(-FLT_MAX, std::min(FLT_MAX, scale / rule.cap)), a.rule.cap_out = rule.cap * log2e;
   return a;

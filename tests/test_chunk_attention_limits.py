@@ -1,0 +1,54 @@
+"""The sizes that torq_chunk_attention takes and refuses, and calls of sizes that only many requests or long tables have."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2605_19561_amd import binding
+from test_chunk_attention import DEV, Rule, case, check, reference, tq, values_of   # noqa: F401
+
+gpu = pytest.mark.gpu
+
+
+def answer(heads, kv_heads, tokens, most, B, keys, page=16):
+    """What the call says to such sizes, with a query that is not aligned (looked at behind the sizes), so that nothing runs."""
+    L, p, odd = binding.lib(), C.c_void_p(0x1000), C.c_void_p(0x1004)
+    cache = C.byref(binding._KVCacheStruct(0x1000, 0x2000, 0x3000, 0x4000, 10, kv_heads * page * 128, page * 128, 128, binding.TORQ_FMT_MXFP4, kv_heads, 128, page))
+    width = keys // page
+    return L.torq_chunk_attention(cache, odd, heads * 128, 128, heads, tokens, p, most, p, width, width, p, B, 1.0, None, p, p, 1 << 40, None)
+
+
+TAKEN = [
+    # heads, kv_heads, new tokens, of a request at most, requests, tokens that the tables hold
+    (64, 8, 8192, 8192, 32, 131072), (64, 8, 8192, 8192, 16, 131072), (64, 8, 8192 + 31, 8192, 32, 65536), (64, 8, 4096, 4096, 64, 32768),
+    (64, 8, 2048, 2048, 256, 32768), (32, 8, 1 << 20, 1 << 20, 1024, 1 << 20), (8, 8, 1 << 16, 33, 1 << 16, 1 << 30),
+    # up to 32 rows: tiles of 32 tokens below 2^31
+    (64, 8, 128, 4, 16368, 1 << 18), (64, 8, 128, 2, 65408, 1 << 17),
+    # workgroups of 64 rows below 2^24
+    (64, 64, (1 << 24) - 65, 33, 1, 64), (64, 64, 1 << 17, 33, 1 << 17, 64), (8, 8, 99, 1 << 24, 1 << 30, 16), (1, 1, 99, 2 ** 31 - 1, 5, 16)]
+REFUSED = [
+    (64, 8, 128, 4, 16369, 1 << 18), (64, 8, 128, 2, 65409, 1 << 17), (64, 8, 128, 4, 1 << 30, 1 << 18), (64, 64, (1 << 24) - 64, 33, 1, 64), (64, 64, 1 << 18, 33, 1 << 18, 64),
+    (8, 8, 99, 33, (1 << 30) + 1, 16), (64, 8, 8192, 8192, 32, (1 << 30) + 16), (64, 1, 99, 1 << 26, 5, 16), (64, 8, 1 << 25, 99, 1, 64)]
+
+
+@pytest.mark.parametrize("heads,kv_heads,tokens,most,B,keys", TAKEN)
+def test_sizes_that_are_taken(heads, kv_heads, tokens, most, B, keys):
+    assert answer(heads, kv_heads, tokens, most, B, keys) == binding.TORQ_EALIGN
+
+
+@pytest.mark.parametrize("heads,kv_heads,tokens,most,B,keys", REFUSED)
+def test_sizes_that_are_refused(heads, kv_heads, tokens, most, B, keys):
+    assert answer(heads, kv_heads, tokens, most, B, keys) == binding.TORQ_EINVAL
+
+
+@gpu
+@pytest.mark.parametrize("fmt,dim", [("bf16", 128), ("mxfp4", 64), ("mxfp8", 256)])
+def test_places_for_long_prompts_behind_long_tables(tq, fmt, dim):
+    """32 requests that might bring 8192 tokens each over tables for 131072: what a batch is laid out for, not what it has."""
+    fresh, lengths = [3, 0, 70, 1] * 8, [300, 20, 70, 45] * 8
+    cache, q, starts, tables, lens, pages = case(tq, fresh, lengths, 64, 8, dim, 16, fmt, "heads", 51)
+    want = reference(q, starts, values_of(cache, "k"), values_of(cache, "v"), tables, lens, 0.1, pages, Rule())
+    wide = torch.full((32, 131072 // 16), -1, dtype=torch.int32)
+    wide[:, :tables.shape[1]] = tables
+    got = tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, wide.to(DEV), lens.to(DEV), 0.1, most=8192)
+    check(got, *want, False)
