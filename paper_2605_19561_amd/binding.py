@@ -802,6 +802,8 @@ class Scores:
             raise ValueError("window must be at least 0 (none) and below 2^31")
         self._tensors = slopes, prefix
         self._struct = _ScoresStruct(cap, window, *(None if t is None else t.data_ptr() for t in self._tensors))
+        if cap > 0 and self._struct.cap == 0:        # (0 is none)
+            raise ValueError("cap must be 0 (none) or a number that fp32 holds")
         self.scores_handle = C.c_void_p(C.addressof(self._struct))
 
     def check(self, heads: int, B: int, device):

@@ -52,3 +52,23 @@ def test_places_for_long_prompts_behind_long_tables(tq, fmt, dim):
     wide[:, :tables.shape[1]] = tables
     got = tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, wide.to(DEV), lens.to(DEV), 0.1, most=8192)
     check(got, *want, False)
+
+
+def test_a_cap_that_fp32_does_not_hold_is_refused():
+    """Not taken for 0, which is none."""
+    for cap in (1e-46, 5e-324, 7e-46):               # (2^-150, half of fp32's least number, and what is below: 0 in fp32)
+        with pytest.raises(ValueError):
+            binding.Scores(cap=cap)
+    assert binding.Scores(cap=1e-45).cap == 2.0 ** -149 and binding.Scores(cap=0.0).cap == 0.0 and binding.Scores(cap=1e30).cap > 0
+
+
+@gpu
+@pytest.mark.parametrize("fresh", [[1, 1], [3, 2], [20, 9], [70, 33]])
+@pytest.mark.parametrize("cap", [2.0 ** -149, 1e-40, 1e-30])
+def test_the_least_caps_weigh_all_keys_alike(tq, fresh, cap):
+    cache, q, starts, tables, lens, pages = case(tq, fresh, [90, 100], 4, 2, 128, 16, "bf16", "heads", 52)
+    for scale in (1.0, -1e30):
+        rule = Rule(cap=cap)
+        want = reference(q, starts, values_of(cache, "k"), values_of(cache, "v"), tables, lens, scale, pages, rule)
+        got = tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, tables.to(DEV), lens.to(DEV), scale, most=max(fresh), scores=rule.on(tq))
+        check(got, *want, 2 * max(fresh) <= 32)
