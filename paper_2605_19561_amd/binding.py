@@ -902,7 +902,13 @@ def torq_paged_attention(q, cache: KVCache, block_tables, lengths, scale: float,
 
 
 def torq_chunk_attention_workspace_bytes(cache: KVCache, heads: int, tokens: int, most: int, B: int, width: int) -> int:
-    return int(lib().torq_chunk_attention_workspace_bytes(C.addressof(cache._struct), heads, tokens, most, B, width))
+    return int(lib().torq_chunk_attention_workspace_bytes(C.addressof(cache._struct), heads, tokens, _most(most), B, width))
+
+
+def _most(most):
+    if not -1 << 31 <= int(most) < 1 << 31:          # (ctypes would take what is left of it in 32 bits)
+        raise ValueError("most must be below 2^31")
+    return int(most)
 
 
 def torq_chunk_attention(q, starts, cache: KVCache, block_tables, lengths, scale: float, most=None, scores=None, out=None, workspace=None,
@@ -920,7 +926,7 @@ def torq_chunk_attention(q, starts, cache: KVCache, block_tables, lengths, scale
     if dim != cache.head_dim or starts.shape != (B + 1,) or lengths.shape != (B,):
         raise ValueError("q must be [tokens, heads, head_dim], starts [B + 1], block_tables [B, width], lengths [B]")
     rule = _scores(scores, heads, B, q.device)
-    most = max(T, 1) if most is None else int(most)
+    most = max(T, 1) if most is None else _most(most)
     if workspace is None:
         workspace = _scratch(q, max(torq_chunk_attention_workspace_bytes(cache, heads, T, most, B, width), 16), stream)
     if out is None:

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2605_19561_amd import binding
-from test_chunk_attention import DEV, Rule, case, check, reference, tq, values_of   # noqa: F401
+from test_chunk_attention import DEV, Rule, case, check, either_way, reference, tq, values_of   # noqa: F401
 
 gpu = pytest.mark.gpu
 
@@ -72,3 +72,23 @@ def test_the_least_caps_weigh_all_keys_alike(tq, fresh, cap):
         want = reference(q, starts, values_of(cache, "k"), values_of(cache, "v"), tables, lens, scale, pages, rule)
         got = tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, tables.to(DEV), lens.to(DEV), scale, most=max(fresh), scores=rule.on(tq))
         check(got, *want, 2 * max(fresh) <= 32)
+
+
+@pytest.mark.parametrize("most", [1 << 31, (1 << 32) + 1, (1 << 32) + 40, -(1 << 32) + 3])
+def test_a_most_that_is_no_int_of_the_library_is_refused(most):
+    """Not taken for what is left of it in 32 bits."""
+    t = torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16)
+    cache = binding.KVCache(t, t.clone())
+    with pytest.raises(ValueError):
+        binding.torq_chunk_attention_workspace_bytes(cache, 4, 99, most, 2, 4000)
+
+
+@gpu
+def test_a_call_with_a_most_that_is_no_int_of_the_library_is_refused(tq, either_way):
+    cache, q, starts, tables, lens, _ = case(tq, [3, 2], [30, 20], 4, 2, 64, 16, "mxfp4", "heads", 53)
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device=DEV)
+    for most in (1 << 31, (1 << 32) + 1):
+        with pytest.raises(ValueError):
+            tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, tables.to(DEV), lens.to(DEV), 0.1, most=most, out=out)
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
