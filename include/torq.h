@@ -335,7 +335,7 @@ int torq_paged_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64
 
 /* How a model gives its scores, beyond s = scale * q . k, for a query at position p of its request and a key at position t:
  *   cap      > 0, at most 1e30: s -> cap * tanh(s / cap); 0: as they are
- *   slopes   [heads] fp32 on the device, finite: s -> s - slopes[h] * |p - t|, behind the cap; NULL: none
+ *   slopes   [heads] fp32 on the device, finite (beyond 1e28 in magnitude as 1e28): s -> s - slopes[h] * |p - t|, behind the cap; NULL: none
  *   window   > 0: a query sees the keys p - window < t <= p; 0: all of t <= p
  *   prefix   [B] int32 on the device: a query of request b sees the keys t < prefix[b] besides, whatever its own position (a prompt whose tokens
  *            see one another, or, with a window, the first tokens of a text); below 0 counts as 0; NULL: none

@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP * (
   const int row = row0 + rp * 32 + n, token = row / each, head = kv_head * each + row - token * each;
   const bool in = row < rows;
   const int position = first + token, low = low_of(position), span = max(min(position + 1, length) - low, 0);     // it sees the window's `span` keys from low on
-  const float slope = BEND >= BEND_SLOPES && a.rule.slopes && in ? 1.44269504088896340736f * a.rule.slopes[head] : 0.0f;
+  const float slope = BEND >= BEND_SLOPES && a.rule.slopes && in ? slope_of(a, head) : 0.0f;
   bf16x8 q[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {

@@ -165,6 +165,11 @@ __device__ __forceinline__ float capped(float x, float in, float out) {
   const float large = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.88539008177792681472f * y));
   return out * (fabsf(y) < 0.125f ? small : large);
 }
+// A head's slope to base 2.  Magnitudes beyond 1e28 are taken for that: either leaves all the weight to the nearest (or farthest) key, and times 2^31
+// tokens it is still finite, where infinities would be NaN at distance 0 or beside one another.
+__device__ __forceinline__ float slope_of(const AttentionArgs &a, int head) {
+  return 1.44269504088896340736f * fminf(fmaxf(a.rule.slopes[head], -1e28f), 1e28f);
+}
 typedef const __attribute__((address_space(4))) int *uniform_ints;      // read by scalar loads
 
 // `bytes` bytes from p as a raw buffer; all three the same in every lane
@@ -372,7 +377,7 @@ __device__ __forceinline__ void attention_body(const AttentionArgs &a) {
         const int token = row / a.rule.heads_each, head = s.kv_head * a.rule.heads_each + row - token * a.rule.heads_each;
         position[rt] = s.position + token;
         low[rt] = a.rule.window && position[rt] >= a.rule.window ? position[rt] - a.rule.window + 1 : 0;
-        slope[rt] = a.rule.slopes && row < rows_in(s) ? 1.44269504088896340736f * a.rule.slopes[head] : 0.0f;
+        slope[rt] = a.rule.slopes && row < rows_in(s) ? slope_of(a, head) : 0.0f;
         from = a.q + (int64_t)(s.q_at + token) * a.q_stride + (int64_t)head * a.q_head_stride;
       }
 #pragma unroll

@@ -92,3 +92,17 @@ def test_a_call_with_a_most_that_is_no_int_of_the_library_is_refused(tq, either_
             tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, tables.to(DEV), lens.to(DEV), 0.1, most=most, out=out)
     torch.cuda.synchronize()
     assert bool((out == 7.0).all())
+
+
+@gpu
+@pytest.mark.parametrize("heads,kv_heads,dim,fresh,fmt", [(4, 2, 64, [1, 1], "bf16"), (8, 2, 128, [1, 1], "mxfp4"), (4, 2, 64, [3, 2], "mxfp8"), (4, 2, 128, [20, 9], "bf16"),
+                                                          (4, 2, 96, [70, 33], "mxfp4"), (4, 2, 256, [70, 33], "bf16")])
+@pytest.mark.parametrize("prefix,cap", [(0, 0.0), (77, 0.0), (0, 5.0)])
+def test_slopes_of_any_finite_size(tq, heads, kv_heads, dim, fresh, fmt, prefix, cap):
+    """Whose product with a distance fp32 does not hold: the nearest key, or the farthest, has all of the weight."""
+    cache, q, starts, tables, lens, pages = case(tq, fresh, [90, 100], heads, kv_heads, dim, 16, fmt, "heads", 54)
+    slopes = torch.tensor(([3.4e38, -3.4e38, 2.4e38, -1e38, 1e30, -1e36, 0.0, 1e-38])[:heads])
+    rule = Rule(cap=cap, slopes=slopes, prefix=torch.full((2,), prefix, dtype=torch.int32))
+    want = reference(q, starts, values_of(cache, "k"), values_of(cache, "v"), tables, lens, 0.1, pages, rule)
+    got = tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, tables.to(DEV), lens.to(DEV), 0.1, most=max(fresh), scores=rule.on(tq))
+    check(got, *want, heads // kv_heads * max(fresh) <= 32)
