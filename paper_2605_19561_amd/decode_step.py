@@ -49,14 +49,14 @@ class Pages:
                              slots=self.slots, cursor_out=self.cursor)
 
     def admit(self, tokens: torch.Tensor, total: int, most: int) -> Fresh:
-        """tokens[b] (int32, `total` in all, at most `most`) more for every request, a prompt or a piece of one: their pages and slots."""
+        """tokens[b] (int32, `total` in all or fewer, at most `most`) more for every request, a prompt or a piece of one: their pages and slots."""
         self.held.copy_(self.lengths)
         self.lengths.add_(tokens)
         slots, _ = tq.torq_block_tables(self.held, self.lengths, self.free, self.cursor, self.tables, self.page_size, total, cursor_out=self.cursor)
         ends = tokens.cumsum(0, dtype=torch.int32)
         starts = torch.cat([ends.new_zeros(1), ends])
         rows = torch.arange(total, dtype=torch.int32, device=tokens.device)
-        b = torch.searchsorted(ends, rows, right=True)
+        b = torch.searchsorted(ends, rows, right=True).clamp_(max=len(ends) - 1)          # (rows behind the last token: of no request, without a slot)
         return Fresh(starts, self.held[b] + rows - starts[b], slots, most)
 
 
