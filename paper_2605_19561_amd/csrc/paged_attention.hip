@@ -1,5 +1,11 @@
-// torq_paged_attention: one new token of each request over its pages (and what torq_chunk_attention runs for few rows).  The mathematics, the
-// layout and what was measured stand in paged_attention_body.h; here are its kernels for bf16 and MXFP8 caches, the join, and who runs which.
+// torq_paged_attention: one new token of each request over its pages (and what torq_chunk_attention runs for few rows): its kernels for bf16 and
+// MXFP8 caches without a rule, the joins, and who runs which.
+//
+// The mathematics, the layout and what was measured stand in paged_attention_body.h, whose kernels run MXFP4 and rules.  This one is apart from those and
+// differs in two things: the weights' base is the maximum so far, so that it moves and O is multiplied with every tile, and a tile's pages are looked up by
+// scalar instructions, a tile ahead.  It stays since the outputs that callers have of these formats stay so to the bit, and the other way would gain
+// little where a tile is two or four times the bytes: this one / that one, us, 16 requests of 1000 to 8192 tokens 55.5 / 54.8, one of 131072 87.9 /
+// 87.2, 77 with 20 heads of 80 86.3 / 86.2, 45 in MXFP8 313 / 306, one of 333 6.2 / 6.2.  A fault of one is to be looked for in the other.
 #include <algorithm>
 #include <cfloat>
 
@@ -429,53 +435,10 @@ __global__ void __launch_bounds__(256) paged_attention_kernel(AttentionArgs a) {
   }
 }
 
-// What is not whole within a run, put together in the order of the tokens.  A thread takes four values of a query head and every
-// so many-th of its parts, in one pass like the waves above; a workgroup's threads for the same values are put together in LDS.
-// many: values, by fours, that a workgroup takes.
+// The joins of parts, without a rule (those of every format) and with one.
 __global__ void __launch_bounds__(ATT_JOIN) paged_attention_join_kernel(AttentionArgs a, int together, int many) {
-  __shared__ f32x4 values[ATT_JOIN];
-  __shared__ float m_all[ATT_JOIN], l_all[ATT_JOIN];
-  const Cut cut = a.cuts[blockIdx.x];
-  if (cut.place < 0) return;
-  const int parts = Runs(cut.each, cut.more).of(cut.last_tile) - cut.place / 2 + 1;
-  const int tid = threadIdx.x, quads = a.dim / 4, rows = min(a.rows, a.group);
-  const int all = together * rows * quads, here = min(all, many), ways = blockDim.x / here, way = tid / here;
-  const int x = blockIdx.y * many + (tid - way * here), c = x % quads, r = x / quads % rows, w = x / quads / rows;
-  const int column = cut.column * together + w, kv_head = column / a.row_groups, row = (column - kv_head * a.row_groups) * a.rows + r;
-  const bool real = x < all && way < ways && row < a.group && kv_head < a.kv_heads;
-  float m = -INFINITY, l = 0.0f;
-  f32x4 v = {0, 0, 0, 0};
-  if (real) {
-#pragma unroll 4
-    for (int i = way; i < parts; i += ways) {
-      const int64_t at = ((int64_t)(i ? (cut.place / 2 + i) * 2 : cut.place) * together + w) * a.rows + r;
-      const float mi = a.part_ml[2 * at], li = a.part_ml[2 * at + 1];
-      const f32x4 vi = *reinterpret_cast<const f32x4 *>(a.part + at * a.dim + 4 * c);
-      const float top = fmaxf(m, mi), base = top == -INFINITY ? 0.0f : top;
-      const float f = __builtin_amdgcn_exp2f(m - base), fi = __builtin_amdgcn_exp2f(mi - base);
-      m = top;
-      l = l * f + li * fi;
-      v = v * f + vi * fi;
-    }
-  }
-  m_all[tid] = m, l_all[tid] = l, values[tid] = v;
-  __syncthreads();
-  if (!real || way > 0) return;
-  float top = m;
-  for (int i = 1; i < ways; ++i) top = fmaxf(top, m_all[tid + i * here]);
-  const float base = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - base);
-  l *= f;
-  v *= f;
-  for (int i = 1; i < ways; ++i) {
-    const float fi = __builtin_amdgcn_exp2f(m_all[tid + i * here] - base);
-    l += l_all[tid + i * here] * fi;
-    v += values[tid + i * here] * fi;
-  }
-  v *= l != 0.0f ? 1.0f / l : 0.0f;
-  uint16_t *const out = a.out + ((int64_t)(cut.b * a.kv_heads + kv_head) * a.group + row) * a.dim;
-  *reinterpret_cast<bf16x4 *>(out + 4 * c) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+  attention_join_body<false>(a, together, many);
 }
-
 __global__ void __launch_bounds__(ATT_JOIN) scored_attention_join_kernel(AttentionArgs a, int together, int many) {
   attention_join_body<true>(a, together, many);
 }

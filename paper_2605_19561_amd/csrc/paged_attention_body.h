@@ -1,5 +1,6 @@
 // The attention of one or a few new tokens of each request over its pages, out = softmax(scale q K^T) V for each head, as the kernels of
-// paged_attention.hip, paged_attention_mxfp4.hip and paged_attention_scores*.hip run it.
+// paged_attention_mxfp4.hip and paged_attention_scores*.hip run it.  (paged_attention.hip has a kernel of its own for bf16 and MXFP8 without a rule, of the
+// same mathematics and work but for the weights' base and the way to the pages: see there.  Arguments, products' operands and joins are these.)
 //
 // The query heads of a key head are the columns of one matrix product, up to 16, or of two side by side, up to 32, so K and V are
 // read once for all of them: HBM-bound, 2 (bf16) or 1 1/32 (MXFP8) bytes for 2 heads / kv_heads flops.
@@ -33,11 +34,11 @@
 // The tiles between the prefix and the first window are left out of the row of tiles; masks are looked at only in tiles that some row does not see whole, and
 // there values that are not finite take a row at a time.
 //
-// The weights are taken against a base that moves only when a score passes it by 2^8, so most tiles leave O alone, and where the groups of 16 tokens lie is
-// worked out by the lanes for 32 tiles at a time: with a base that always moves and places by scalar instructions, 45 requests in MXFP4 (as below) took
+// Here (not in paged_attention.hip) the weights are taken against a base that moves only when a score passes it by 2^8, so most tiles leave O alone, and
+// where the groups of 16 tokens lie is worked out by the lanes for 32 tiles at a time: with a base that always moves and places by scalar instructions, 45 requests in MXFP4 (as below) took
 // 304 us instead of 189, 77 with slopes 116 instead of 98: in MXFP4 a tile is 4.3 KB, and its 400 instructions were the bound, not its bytes.
 //
-// Measured (without a rule, bf16 where not said; called in turn over three caches, 303 MB to 1.9 GB; 7.1 TB/s is what reading alone reaches): 16 requests of 1000 to 8192 tokens, 64 query
+// Measured (paged_attention.hip's, bf16 where not said; called in turn over three caches, 303 MB to 1.9 GB; 7.1 TB/s is what reading alone reaches): 16 requests of 1000 to 8192 tokens, 64 query
 // and 8 key heads of 128, 55.2 us = 5.5 TB/s; one of 131072 87.6 us = 6.1; 45 of 8000 to 32768 in MXFP8 312 us = 6.2; 77 with 20 heads of 80 each, 85.9 us = 4.9.  The traffic
 // is what has to be read (counters within 1 %); vector instructions take a third (bf16) to half (MXFP8) of the time.  What is left over HBM's time: 5 to 7 us until
 // the first tiles are there, 5 for the join and its launch.  One request of 333 tokens 6.2 us, one launch: three rounds that
