@@ -369,7 +369,13 @@ int torq_paged_attention_scores(const torq_kv_cache_t *cache, const void *q_bf16
  *                 tokens * heads / 64 + min(B, tokens) * cache->heads below 2^24
  *   workspace     16-byte aligned, torq_chunk_attention_workspace_bytes() of the same sizes; contents do not matter
  * Products of bf16 values with fp32 sums, statistics in fp32.  Where few rows (heads * most / cache->heads up to 32) see the keys the weights are
- * two bf16 parts as above, else one, rounded to nearest, whose sum they are divided by.  The same inputs give the same bits. */
+ * two bf16 parts as above, else one, rounded to nearest, whose sum they are divided by (a weight is then off by 2^-8 of itself at most, the output by
+ * 2^-8 (sum_t p_t |v_t| + |out|) beside its own rounding), and scores under a cap up to 177 are off by 2^-23 of the cap, 2^-15 of a weight.  So a row's
+ * last bits depend on which side of 32 `most` puts it.  The same inputs give the same bits.
+ * The kernel is chosen, and the keys are shared out over workgroups, by `most` and the tables' width, not by the lengths, which are the device's: beside one
+ * long prompt, requests with a single new token each take a prompt's workgroup and go through their keys there alone.  Where many of those have long contexts, two
+ * calls are faster, one for the prompts and one (torq_paged_attention_scores, or this one with its own `most`) for the others: a prompt of 2048 tokens beside 31
+ * single ones of 8000, 64 / 8 heads of 128, MXFP8, 343 us in one call and 205 in two; of 512 beside 15 of 500, 32 / 8 heads, bf16, 34 and 37. */
 size_t torq_chunk_attention_workspace_bytes(const torq_kv_cache_t *cache, int heads, int64_t tokens, int most, int64_t B, int width);
 int torq_chunk_attention(const torq_kv_cache_t *cache, const void *q_bf16, int64_t q_stride, int64_t q_head_stride, int heads, int64_t tokens,
                          const int32_t *starts, int most, const int32_t *block_tables, int64_t table_stride, int width,

@@ -915,8 +915,8 @@ def torq_chunk_attention(q, starts, cache: KVCache, block_tables, lengths, scale
                          stream=None):
     """q [tokens, heads, head_dim] bf16 (a view will do), rows starts[b] ... starts[b + 1] - 1 the last tokens of request b, each over the keys up
     to its own (or by `scores`) among the first lengths[b] tokens, which block_tables [B, width] finds in the cache; starts [B + 1] int32.  most: no
-    request has more new tokens (all of them, if not given: what is known goes into the choice of the kernel).  Returns out [tokens, heads,
-    head_dim] bf16, where rows of no request are left as they were."""
+    request has more new tokens (all of them, if not given: what is known goes into the choice of the kernel; a prompt beside many single tokens of long
+    contexts is better two calls).  Returns out [tokens, heads, head_dim] bf16, where rows of no request are left as they were."""
     y = (_host or _native()).chunk_attention(q, starts, cache, block_tables, lengths, scale, most, scores, out, workspace, stream)
     if y is not None:
         return y

@@ -13,15 +13,19 @@
 // workgroup, whose O, m and l a second kernel joins in the order of the keys.
 //
 // A wave has three steps in hand at a time: the scores of step j + 1, the weights of j, the products with V of j - 1, none of which waits for another. With
-// two waves on a SIMD the softmax comes first and then the products, and one wave's instructions fill the other's gaps; a wave alone (64 rows) has its
-// softmax between its products piece by piece (IN_TURN, below).  Steps in which every row sees every key know no masks; the others, at the ends of windows,
+// two waves on a SIMD the softmax comes first and then the products, and one wave's instructions fill the other's gaps; so it does in the one wave of
+// head_dim over 128, which has no registers for more; a wave of 64 rows, alone on its SIMD too, has its softmax between its products piece by piece (IN_TURN, below).  Steps in which every row sees every key know no masks; the others, at the ends of windows,
 // prefixes and lengths, do.  There 0 times a value that is not finite would be no 0: such values are left out, and at the end a second pass puts
 // them back for the rows that see them, a case that costs a second look at the keys and is rare.
 //
-// Measured: one prompt of 8192 tokens, 32 / 8 heads of 128, bf16, 600 us = 916 TFLOP/s (a large bf16 product reaches 1363); 512 tokens behind 60000 in MXFP4,
-// 64 / 8 heads, 1067 us = 946; 4 prompts of 4096 in MXFP8 687 us.  What bounds it is the issue of products and softmax together: LDS reads alone take 268 us of the
+// Measured: one prompt of 8192 tokens, 32 / 8 heads of 128, bf16, 600 to 618 us from one card to another = 890 to 916 TFLOP/s (a large bf16 product reaches
+// 1363); 512 tokens behind 60000 in MXFP4, 64 / 8 heads, 1067 to 1095 us = 922 to 946; 4 prompts of 4096 in MXFP8 687 to 709 us; 8 of 1024 by head_dim and format: see
+// IN_TURN.  What bounds it is the issue of products and softmax together: LDS reads alone take 268 us of the
 // 600, the products at their best 403.  The first version, tiles of 64 keys and no steps in hand: 799 and 1303.  Not taken: 64 rows a wave, whose
 // O then fills the accumulators' half of the registers by name (less LDS traffic, one wave a SIMD): 624, 1076, 772.
+// Short items (61 capped prompts of up to 1024 tokens, a window of 512, in MXFP8: 7960 of 10.0 steps on average, 433 us; without the cap 382; without the window, 11.3
+// steps, 460): half of the time or more is what an item costs besides its steps, that is starts and lengths, table, first keys and first scores, each
+// waiting for the one before, and the output's way through LDS.
 //
 // A tile goes through the matrix cores transposed, and nothing of it passes between lanes but maxima between two halves of a wave:
 //   S^T [key][row] = K [key][i] Q^T [i][row]            v_mfma_f32_32x32x16_bf16
@@ -113,6 +117,7 @@ __device__ __forceinline__ bool row_tile_of(const ChunkArgs &a, int slot, RowTil
   return false;
 }
 
+// (256 values, plain, over MXFP8 and MXFP4: 8 and 20 bytes of scratch a lane beside all 512 registers.)
 // DP: values of a row in LDS, of which the first DV are multiplied.  RW: waves that share keys, each with 32 rows of its own; the other
 // 4 / RW - 1 such groups have the same rows and other keys.
 // BEND: what is done to scores ahead of the weights; ANY looks what, and takes all steps one instruction after the other.
@@ -321,10 +326,16 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP * (
     constexpr int I = decltype(number)::value;
     o[I % IB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand, as_bf16(pt[I / IB]), o[I % IB], 0, 0, 0);
   };
-  // One after the other at every step where the workgroup's waves have 32 rows of their own: two waves a SIMD fill one another's gaps, and weights among the
-  // products take registers that two of them do not have (or gain nothing).  Mixed / in turn, 8 requests of 1024 tokens, 32 and 8 heads, us: of 128 in bf16
-  // 152 / 143, MXFP8 230 / 153, capped 279 / 176, with slopes 271 / 171; of 256 in MXFP8 532 / 402; of 96 in bf16 120 / 118, of 64 100 / 100, of 192 282 / 287.  Not with one
-  // wave a SIMD: 32 requests of 5 tokens in MXFP4 139 / 182.
+  // One after the other at every step where a workgroup's four waves share the keys: weights among the products take registers that two waves a SIMD (up to
+  // 128 values) do not have, nor one of 256 values over 8 bits, and two waves fill one another's gaps without that.  Mixed / in turn, 8 prompts of 1024
+  // tokens, 32 and 8 heads, us:
+  //   values  bf16         MXFP8        MXFP4
+  //   64      94.2 / 95.6  102 / 104    102 / 103
+  //   96      114 / 115    126 / 126    124 / 125
+  //   128     151 / 133    222 / 145    179 / 142     capped, MXFP8: 542 / 174, with slopes: 302 / 171
+  //   192     279 / 286    309 / 319    313 / 318
+  //   256     339 / 338    530 / 403    419 / 401
+  // (64 and 192 lose up to 3 % by it.)  Not with 64 rows, one wave a SIMD whose registers hold both: 32 requests of 5 tokens in MXFP4 139 / 182.
   constexpr bool IN_TURN = BEND == BEND_ANY || RW == 4;
   constexpr int PIECES = 13;
   float top, base, alpha;
