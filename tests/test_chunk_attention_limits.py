@@ -106,3 +106,28 @@ def test_slopes_of_any_finite_size(tq, heads, kv_heads, dim, fresh, fmt, prefix,
     want = reference(q, starts, values_of(cache, "k"), values_of(cache, "v"), tables, lens, 0.1, pages, rule)
     got = tq.torq_chunk_attention(q.to(DEV), starts.to(DEV), cache, tables.to(DEV), lens.to(DEV), 0.1, most=max(fresh), scores=rule.on(tq))
     check(got, *want, heads // kv_heads * max(fresh) <= 32)
+
+
+@gpu
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp4"])
+def test_prompts_whose_rows_pass_4_gib(tq, fmt):
+    """34 prompts of 8192 tokens at once: q and out of 4.6 GB each.  (The requests share their pages, each in an order of its own, and see 70 tokens.)"""
+    B, n, heads, kv_heads, dim, page = 34, 8192, 64, 8, 128, 16
+    cache = tq.KVCache.empty(n // page, kv_heads, page, dim, getattr(tq, "TORQ_FMT_" + fmt.upper()), device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(55)
+    x = torch.randn((n, 2, kv_heads, dim), generator=g, device=DEV).to(torch.bfloat16)
+    tq.torq_cache_append(cache, x[:, 0], x[:, 1], torch.arange(n, device=DEV))
+    tables = torch.stack([torch.randperm(n // page, generator=g, device=DEV) for _ in range(B)]).int()
+    q = torch.randn((B * n, heads, dim), generator=g, device=DEV, dtype=torch.bfloat16)
+    starts, lens = torch.arange(B + 1, dtype=torch.int32, device=DEV) * n, torch.full((B,), n, dtype=torch.int32, device=DEV)
+    rule = Rule(window=70)
+    out = tq.torq_chunk_attention(q, starts, cache, tables, lens, 0.1, most=n, scores=rule.on(tq))
+    assert q.numel() * 2 > 1 << 32
+    k, v = values_of(cache, "k"), values_of(cache, "v")
+    for b in (0, 15, 16, 31, 32, B - 1):
+        rows = slice(b * n, (b + 1) * n)
+        alone = tq.torq_chunk_attention(q[rows], starts[:2], cache, tables[b:b + 1], lens[:1], 0.1, most=n, scores=rule.on(tq))
+        assert torch.equal(out[rows], alone)
+        # its last rows, as the last of a request that has no others
+        want = reference(q[rows][-3:].cpu(), torch.tensor([0, 3]), k, v, tables[b:b + 1].cpu(), lens[:1].cpu(), 0.1, n // page, rule)
+        check(out[rows][-3:], *want, False)
